@@ -204,7 +204,7 @@ def prepare(case, seed):
         s["out"] = empty(torch.bfloat16, c["B"], c["d"])
     elif c["kind"] == "grad":
         s["out"] = empty(DTYPES[c["grad"]], c["V"], c["d"])
-        s["scratch"] = fm.EmbedGradScratch(c["T"], c["d"])
+        s["scratch"] = fm.EmbedGradScratch(c["T"], c["V"])
     elif c["kind"] == "route":
         s["out"] = (empty(DTYPES[c["probs"]], c["T"], c["E"]), empty(torch.int32, c["T"], c["K"]),
                     empty(torch.float32, c["T"], c["K"]), empty(torch.int64, c["T"]))
