@@ -78,10 +78,12 @@ typedef enum { FM_PRI_PREFETCH = 0, FM_PRI_EVICT = 1, FM_PRI_ENUM_INT32_ = 0x7ff
 
 /* Sticky device-side flags reported by fm_store_check. */
 #define FM_FLAG_DEPTH_CLAMPED 0x1u   /* a trajectory depth was outside [1, max_depth] and was clamped */
-#define FM_FLAG_INDEX_RANGE   0x2u   /* fm_select_prefetch met an index >= the store size (row skipped) */
+#define FM_FLAG_INDEX_RANGE   0x2u   /* fm_select_prefetch met an index >= the store size (row skipped); the model
+                                        operators met a token, expert or slot past its range (left out) */
 #define FM_FLAG_STATE_STALE   0x4u   /* fm_traj_step: the store size changed since layer 0, or layers out of order */
 #define FM_FLAG_VALUE_RANGE   0x8u   /* a float32 map or trajectory-query value exceeds 8 in magnitude (gate
                                         probabilities lie in [0, 1]); float32 trajectory scores are then unspecified */
+#define FM_FLAG_EXPERT_MISSING 0x10u /* fm_moe_experts: an expert that a token takes is in no slot (left out) */
 
 typedef struct fm_store fm_store;   /* opaque host-side handle */
 
@@ -342,6 +344,114 @@ size_t fm_traj_state_bytes(int32_t cap, int32_t B_max);
 fm_status fm_traj_step(fm_store* store, void* state, size_t state_bytes, const void* q_layer, int32_t layer,
                        int32_t B, int32_t k, int32_t* idx_out, float* score_out, void* workspace,
                        size_t workspace_bytes, void* stream);
+
+/* ---- Model operators around the search -------------------------------
+ *
+ * What the search works on and for: token embeddings (the semantic queries of
+ * Section 4.2.1), the gate of an MoE layer (a row of an expert map and of a
+ * trajectory query, Sections 4.1 and 4.2.2), and the chosen experts' products
+ * on experts that a cache holds (the prefetched ones of Section 4.3).  They
+ * take no store: work is enqueued on the current device, which must hold every
+ * buffer; T <= 2^24 tokens, B <= 65536 requests, d <= 16384.  flags, where a call takes it, is a device uint32 that collects
+ * sticky FM_FLAG_* bits, or NULL.  Sizes of zero tokens or requests are
+ * no-ops.  All sums are float32; bf16 inputs are widened exactly and results
+ * rounded once, to nearest even.  Results do not depend on timing: the same
+ * inputs give the same bits. */
+
+/* Embedding lookup: out[t] = scale * table[tokens[t]].  table: device [V][d]
+ * of dtype; tokens: device [T] int32; out: device [T][d] of dtype, apart from
+ * the table.  A negative token is padding and gives a row of zeros, and so
+ * does a token >= V, which also sets FM_FLAG_INDEX_RANGE.  Pointers are
+ * aligned to their elements. */
+fm_status fm_embed_lookup(const void* table, int32_t V, int32_t d, fm_dtype dtype, const int32_t* tokens, int32_t T,
+                          float scale, void* out, uint32_t* flags, void* stream);
+
+/* Mean embedding of each request, the query form of fm_match_semantic:
+ * out[b] = scale * mean of table[tokens[t]] over the tokens of request b that
+ * select a row, offsets[b] <= t < offsets[b + 1] (padding and tokens >= V are
+ * left out of the sum and of the count); a request without any gives zeros.
+ * offsets: device [B + 1] int32, clamped to [0, T] (an end before its start
+ * is an empty request); tokens: device [T]; out: device [B][d] bf16.
+ * Otherwise as fm_embed_lookup. */
+fm_status fm_embed_pool(const void* table, int32_t V, int32_t d, fm_dtype dtype, const int32_t* tokens, int32_t T,
+                        const int32_t* offsets, int32_t B, float scale, void* out, uint32_t* flags, void* stream);
+
+/* Bytes of scratch (device memory owned by the caller, 256-byte aligned) for
+ * fm_embed_grad calls of up to T_max tokens on a table of V rows: two int32
+ * per row, one per token, and the list of frequent tokens.  Returns 0 unless
+ * 1 <= V <= 2^24 and 0 <= T_max <= 2^24. */
+size_t fm_embed_grad_scratch_bytes(int32_t T_max, int32_t V);
+
+/* Gradient of fm_embed_lookup with respect to the table:
+ * dtable[v] = scale * sum of dout[t] over tokens[t] == v, summed in float32 in
+ * an order fixed by the tokens.  dout: device [T][d] of dtype; dtable: device
+ * [V][d] of grad_dtype.  accumulate == 0 writes every row (zeros where no
+ * token selects it); otherwise the sum is added to the rows that tokens
+ * select and no other row is touched.  Padding and tokens >= V contribute
+ * nothing.  T == 0 with accumulate == 0 writes zeros.  scratch: at least
+ * fm_embed_grad_scratch_bytes(T, V) bytes, rewritten by the call. */
+fm_status fm_embed_grad(const void* dout, fm_dtype dtype, const int32_t* tokens, int32_t T, int32_t V, int32_t d,
+                        float scale, int32_t accumulate, void* dtable, fm_dtype grad_dtype, void* scratch,
+                        size_t scratch_bytes, uint32_t* flags, void* stream);
+
+/* The gate of one MoE layer: logits l[t][e] = x[t] . gate[e], probabilities
+ * p = softmax over e (float32), and each token's K experts with the largest
+ * logits (lower index first on equal logits, NaN last).  x: device [T][d],
+ * gate: device [E][d], both of dtype and 16-byte aligned, d a multiple of 8;
+ * active: device [T] uint8 or NULL: a token with 0 has no request (its
+ * probabilities and weights are 0, its experts -1, its mask 0).
+ * probs_out: row t at probs_out + t * probs_stride elements of probs_dtype
+ * (probs_stride >= E), so that a layer's probabilities land in the rows
+ * [t][layer] of a batch of maps or trajectory queries; ids_out: device [T][K]
+ * int32, by falling logit; weight_out: device [T][K] float32, the chosen
+ * probabilities, divided by their sum if renorm != 0; mask_out: device [T]
+ * uint64 (bit e = expert e chosen, as the masks of fm_select_prefetch) or
+ * NULL.  1 <= E <= 64, 1 <= K <= min(8, E). */
+fm_status fm_moe_route(const void* x, const void* gate, fm_dtype dtype, int32_t T, int32_t d, int32_t E, int32_t K,
+                       int32_t renorm, const uint8_t* active, void* probs_out, fm_dtype probs_dtype,
+                       int64_t probs_stride, int32_t* ids_out, float* weight_out, uint64_t* mask_out, void* stream);
+
+/* A layer's experts as an expert cache holds them.  slots: device
+ * [n_slots][3 d f] of dtype, 16-byte aligned; a slot is one expert's weights
+ * as one block, so that loading it is one copy: the gate projection [f][d],
+ * the up projection [f][d], the down projection [d][f].  slot_of: device [E]
+ * int32, the slot of each expert (-1: in no slot). */
+typedef struct {
+    int32_t E;           /* experts of the layer, 1..64 */
+    int32_t n_slots;     /* >= 1 */
+    int32_t d;           /* hidden size, a positive multiple of 8 */
+    int32_t f;           /* expert width, a positive multiple of 8, up to 65536 */
+    fm_dtype dtype;      /* of the weights, inputs and outputs */
+    const void* slots;
+    const int32_t* slot_of;
+} fm_expert_cache;
+
+/* Bytes of workspace (device memory owned by the caller, 256-byte aligned)
+ * for fm_moe_experts calls of up to T_max tokens of K experts each: the
+ * activated products of one launch (up to 256 tokens) and its partial sums.
+ * Returns 0 for sizes that fm_moe_experts refuses or T_max < 1. */
+size_t fm_moe_workspace_bytes(int32_t d, int32_t f, fm_dtype dtype, int32_t T_max, int32_t K);
+
+/* The chosen experts' products of one MoE layer:
+ *   out[t] = residual[t] + sum over k of
+ *            weight[t][k] * Down_e (silu(Gate_e x[t]) * (Up_e x[t])),  e = ids[t][k],
+ * silu(z) = z / (1 + exp(-z)).  x, residual (or NULL: zeros) and out: device
+ * [T][d] of the cache's dtype, 16-byte aligned; out may be x or residual
+ * (not overlap them otherwise); ids: device [T][K] int32, weight: device [T][K] float32, as written by
+ * fm_moe_route.  An expert of -1 contributes nothing; an expert that is in no
+ * slot contributes nothing and sets FM_FLAG_EXPERT_MISSING; experts >= E and
+ * slots >= n_slots contribute nothing and set FM_FLAG_INDEX_RANGE.  An expert
+ * that a token lists twice counts with the sum of its weights.  An expert
+ * that every token takes (a shared expert of m times the width) is m experts
+ * in every token's list.  Made for the few tokens of a decode iteration: a
+ * launch takes up to 256 tokens and reads each expert in use once; longer
+ * batches take several launches.  1 <= K <= 8.  The weights of one slot must
+ * not exceed 0xF0000000 bytes.  workspace: at least
+ * fm_moe_workspace_bytes(d, f, dtype, T, K) bytes, rewritten by the call;
+ * calls sharing one must be ordered. */
+fm_status fm_moe_experts(const fm_expert_cache* cache, const void* x, const int32_t* ids, const float* weight,
+                         int32_t T, int32_t K, const void* residual, void* out, uint32_t* flags, void* workspace,
+                         size_t workspace_bytes, void* stream);
 
 /* Test support: the dense float32 score matrix of a trajectory (q, depth
  * non-NULL) or semantic (q_sem non-NULL) search, written to scores_out device

@@ -17,6 +17,15 @@ been built.
     mask, count = select_prefetch(store, idx, score, layer_begin, layer_end,
                                   tau=0.8, k_min=1, k_max=8)   # Eq. 6-8
     order, pri, n = priority_order(store, idx, score, mask, l_now=l_now)  # Section 4.5
+
+and the model operators around it (paper_2502_05370_amd/model.py):
+
+    x = embed_lookup(table, tokens, scale)              # token embeddings
+    q_sem = embed_pool(table, tokens, offsets, scale)   # a request's semantic query
+    dtable = embed_grad(dx, tokens, V, scale)           # the table's gradient
+    probs, ids, w, mask = moe_route(x, gate, k=4)       # a layer's gate: one row of an expert map
+    cache = ExpertCache(slots, E, d, f)                 # experts on the GPU
+    y = moe_experts(cache, x, ids, w, residual=x)       # the chosen experts' products
 """
 from __future__ import annotations
 
@@ -27,7 +36,7 @@ import torch
 
 from . import _lib
 from ._lib import (FM_BF16, FM_BLEND_NONE, FM_BLEND_SCORE, FM_F32, FM_FLAG_DEPTH_CLAMPED,  # noqa: F401
-                   FM_FLAG_INDEX_RANGE, FM_FLAG_STATE_STALE, FM_PRI_EVICT, FM_PRI_PREFETCH, FM_TAU_DYNAMIC, FM_TAU_FIXED, FmError, SelectParams)
+                   FM_FLAG_EXPERT_MISSING, FM_FLAG_INDEX_RANGE, FM_FLAG_STATE_STALE, FM_PRI_EVICT, FM_PRI_PREFETCH, FM_TAU_DYNAMIC, FM_TAU_FIXED, FmError, SelectParams)
 
 _lib.load()
 
@@ -35,6 +44,8 @@ __all__ = ["Store", "Workspace", "match_semantic", "match_trajectory", "match_tr
            "miss_count",
            "debug_scores", "debug_scan_name",
            "map_bytes", "store_bytes", "workspace_bytes", "dedup_scratch_bytes", "traj_state_bytes", "TrajPass",
+           "embed_lookup", "embed_pool", "embed_grad", "embed_grad_scratch_bytes", "EmbedGradScratch", "moe_route",
+           "ExpertCache", "MoeWorkspace", "moe_workspace_bytes", "moe_experts",
            "FmError"]
 
 _DTYPES = {"f32": FM_F32, "bf16": FM_BF16}
@@ -490,3 +501,7 @@ def debug_scan_name(L: int, E: int, n: int, B: int, k: int = 1, map_dtype: str =
     if name is None:
         raise ValueError(f"no match call takes L={L} E={E} n={n} B={B} k={k} d_emb={d_emb} max_depth={depth}")
     return name.decode()
+
+
+from .model import (EmbedGradScratch, ExpertCache, MoeWorkspace, embed_grad, embed_grad_scratch_bytes,  # noqa: E402
+                    embed_lookup, embed_pool, moe_experts, moe_route, moe_workspace_bytes)

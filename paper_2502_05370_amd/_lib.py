@@ -22,6 +22,7 @@ FM_FLAG_DEPTH_CLAMPED = 0x1
 FM_FLAG_INDEX_RANGE = 0x2
 FM_FLAG_STATE_STALE = 0x4
 FM_FLAG_VALUE_RANGE = 0x8
+FM_FLAG_EXPERT_MISSING = 0x10
 
 STATUS_NAMES = {0: "FM_OK", 1: "FM_ERR_INVALID", 2: "FM_ERR_UNSUPPORTED", 3: "FM_ERR_FULL",
                 4: "FM_ERR_HIP", 5: "FM_ERR_DEVICE"}
@@ -40,6 +41,11 @@ class StoreDesc(C.Structure):
 class SelectParams(C.Structure):
     _fields_ = [("mode", C.c_int), ("tau", C.c_float), ("k_min", C.c_int32), ("k_max", C.c_int32),
                 ("blend", C.c_int)]
+
+
+class ExpertCacheDesc(C.Structure):
+    _fields_ = [("E", C.c_int32), ("n_slots", C.c_int32), ("d", C.c_int32), ("f", C.c_int32), ("dtype", C.c_int),
+                ("slots", C.c_void_p), ("slot_of", C.c_void_p)]
 
 
 SIGNATURES = {
@@ -66,6 +72,15 @@ SIGNATURES = {
                                     _vp]),
     "fm_traj_state_bytes": (_sz, [_i32, _i32]),
     "fm_traj_step": (C.c_int, [_vp, _vp, _sz, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "fm_embed_lookup": (C.c_int, [_vp, _i32, _i32, C.c_int, _vp, _i32, C.c_float, _vp, _vp, _vp]),
+    "fm_embed_pool": (C.c_int, [_vp, _i32, _i32, C.c_int, _vp, _i32, _vp, _i32, C.c_float, _vp, _vp, _vp]),
+    "fm_embed_grad_scratch_bytes": (_sz, [_i32, _i32]),
+    "fm_embed_grad": (C.c_int, [_vp, C.c_int, _vp, _i32, _i32, _i32, C.c_float, _i32, _vp, C.c_int, _vp, _sz, _vp,
+                                _vp]),
+    "fm_moe_route": (C.c_int, [_vp, _vp, C.c_int, _i32, _i32, _i32, _i32, _i32, _vp, _vp, C.c_int, C.c_int64, _vp, _vp,
+                               _vp, _vp]),
+    "fm_moe_workspace_bytes": (_sz, [_i32, _i32, C.c_int, _i32, _i32]),
+    "fm_moe_experts": (C.c_int, [C.POINTER(ExpertCacheDesc), _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "fm_debug_scores": (C.c_int, [_vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _sz, _vp]),
     "fm_debug_scan_name": (C.c_char_p, [_i32, _i32, _i32, C.c_int, _i32, _i32, _i32, _i32]),
     "fm_debug_scan_events": (C.c_int, [_vp, _vp]),

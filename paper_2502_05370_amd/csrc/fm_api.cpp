@@ -12,9 +12,11 @@
 
 #include "fm_internal.h"
 
-namespace {
+namespace fm {
 
+namespace {
 thread_local std::string g_error;
+}
 
 fm_status fail(fm_status st, const char* fmt, ...) {
   char buf[512];
@@ -35,9 +37,18 @@ fm_status hip_fail(hipError_t e, const char* what) {
   return fail(FM_ERR_HIP, "%s: %s (%d)", what, hipGetErrorString(e), static_cast<int>(e));
 }
 
-size_t elem_size(fm_dtype t) { return t == FM_BF16 ? 2 : 4; }
-
 bool valid_dtype(int t) { return t == FM_F32 || t == FM_BF16; }
+
+}  // namespace fm
+
+namespace {
+
+using fm::fail;
+using fm::hip_fail;
+using fm::ok;
+using fm::valid_dtype;
+
+size_t elem_size(fm_dtype t) { return t == FM_BF16 ? 2 : 4; }
 
 constexpr size_t kMaxGroupBytes = 0xF0000000u;
 
@@ -171,9 +182,9 @@ struct DeviceGuard {
 
 extern "C" {
 
-int32_t fm_version(void) { return (1 << 16) | 0; }
+int32_t fm_version(void) { return (1 << 16) | 1; }
 
-const char* fm_last_error(void) { return g_error.c_str(); }
+const char* fm_last_error(void) { return fm::g_error.c_str(); }
 
 size_t fm_map_bytes(int32_t cap, int32_t L, int32_t E, fm_dtype map_dtype) {
   Layout ly;

@@ -17,6 +17,13 @@ constexpr int kChunkB = 1024;        // queries per scan launch
 constexpr int kMaxPartials = 256;    // partial top-k lists per query (workgroups per query group)
 constexpr size_t kAlign = 256;
 
+// Error reporting of the ABI layer (fm_api.cpp): the thread's message and the
+// status to return.
+fm_status fail(fm_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+fm_status ok();
+fm_status hip_fail(hipError_t e, const char* what);
+bool valid_dtype(int t);
+
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // Map planes are tiled: plane l holds the maps in tiles of 16 consecutive maps;
@@ -190,5 +197,35 @@ hipError_t launch_select(const StoreView& s, const int32_t* idx, const float* sc
                          int32_t k, const int32_t* lb, const int32_t* le,
                          const fm_select_params& p, uint64_t* mask_out, uint8_t* count_out,
                          hipStream_t st);
+
+// Model operators (fm_embed.hip, fm_route.hip, fm_moe.hip; arguments checked
+// by fm_model_api.cpp).
+hipError_t launch_embed_lookup(const void* table, int32_t V, int32_t d, fm_dtype dt, const int32_t* tokens, int32_t T,
+                               float scale, void* out, uint32_t* flags, hipStream_t st);
+hipError_t launch_embed_pool(const void* table, int32_t V, int32_t d, fm_dtype dt, const int32_t* tokens, int32_t T,
+                             const int32_t* offsets, int32_t B, float scale, uint16_t* out, uint32_t* flags,
+                             hipStream_t st);
+size_t embed_grad_scratch_bytes(int32_t T, int32_t V);
+hipError_t launch_embed_grad(const void* dout, fm_dtype dt, const int32_t* tokens, int32_t T, int32_t V, int32_t d,
+                             float scale, bool accumulate, void* dtable, fm_dtype gdt, void* scratch, uint32_t* flags,
+                             hipStream_t st);
+struct RouteArgs {
+  const void* x;           // [T][d]
+  const void* gate;        // [E][d]
+  int32_t T, d, E, K;
+  bool renorm;
+  const uint8_t* active;   // [T] or null
+  void* probs;             // rows of stride probs_stride
+  int64_t probs_stride;
+  int32_t* ids;            // [T][K]
+  float* weight;           // [T][K]
+  uint64_t* mask;          // [T] or null
+};
+hipError_t launch_moe_route(const RouteArgs& a, fm_dtype dt, fm_dtype probs_dt, hipStream_t st);
+constexpr int kMoeTokens = 256;   // tokens of one launch of the experts' products
+size_t moe_workspace_bytes(int32_t d, int32_t f, fm_dtype dt, int32_t T, int32_t K);
+hipError_t launch_moe_experts(const fm_expert_cache& c, const void* x, const int32_t* ids, const float* weight,
+                              int32_t T, int32_t K, const void* residual, void* out, uint32_t* flags, void* ws,
+                              hipStream_t st);
 
 }  // namespace fm

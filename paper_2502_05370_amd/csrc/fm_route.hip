@@ -1,0 +1,161 @@
+// The gate of an MoE layer: logits x[t] . gate[e], their softmax over the
+// layer's experts and the K largest.  The probabilities are a row of an expert
+// map (Section 4.1) or of a trajectory query (Section 4.2.2) and are written
+// there.
+//
+// A batch of decode tokens is bound by latency (one workgroup reads E d values,
+// 246 KB for 60 experts of 2,048), a prefill by reading x.  A workgroup takes 16
+// tokens per tile; its wavefronts split d, so that every load of a decode call
+// is in flight at once, and join their sums in LDS in a fixed order.  One
+// wavefront then holds one token's logits, an expert per lane.
+#include "fm_internal.h"
+#include "fm_mma.h"
+
+namespace fm {
+
+namespace {
+
+// Larger float -> larger key; -0 as +0; NaN lowest.
+__device__ __forceinline__ uint32_t logit_key(float l) {
+  if (l != l) return 0u;
+  const uint32_t u = __float_as_uint(l + 0.0f);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+template <typename T, int TT, int NE, int NW>
+__global__ void __launch_bounds__(NW * kWave) k_route(RouteArgs a, bool probs_bf16) {
+  constexpr int kLd = NE * 16 + 1;   // (an odd row length keeps the tile's rows apart)
+  __shared__ float red[NW][16 * TT][kLd];
+  const int lane = threadIdx.x % kWave;
+  const int wv = threadIdx.x / kWave;
+  const int c = lane % 16;
+  const int g = lane / 16;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * (16 * TT);
+  const int n_tok = a.T - t0 < 16 * TT ? static_cast<int>(a.T - t0) : 16 * TT;
+  const uint32_t rb = static_cast<uint32_t>(a.d) * sizeof(T);
+  // rows past the batch and past the experts lie past the buffers' ends
+  const __amdgpu_buffer_rsrc_t rs_x =
+      row_buffer(static_cast<const char*>(a.x) + t0 * rb, static_cast<uint32_t>(n_tok) * rb);
+  const __amdgpu_buffer_rsrc_t rs_g = row_buffer(a.gate, static_cast<uint32_t>(a.E) * rb);
+  floatx4 acc[TT][NE];
+#pragma unroll
+  for (int i = 0; i < TT; ++i)
+#pragma unroll
+    for (int j = 0; j < NE; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  constexpr int S = 2;    // k-steps of a load group: one 128-byte line of every row
+  constexpr int PD = 2;   // load groups in flight
+  uint32x4 fx[PD][S][TT], fg[PD][S][NE];
+  auto load = [&](int p, uint32_t k) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const uint32_t kk = k + s * kStepBytes + g * 16;
+#pragma unroll
+      for (int i = 0; i < TT; ++i) fx[p][s][i] = load_step(rs_x, (16u * i + c) * rb, kk, rb);
+#pragma unroll
+      for (int j = 0; j < NE; ++j) fg[p][s][j] = load_step(rs_g, (16u * j + c) * rb, kk, rb);
+    }
+  };
+  const uint32_t stride = NW * S * kStepBytes;
+  const uint32_t k0 = static_cast<uint32_t>(wv) * (S * kStepBytes);
+#pragma unroll
+  for (int p = 0; p < PD; ++p) load(p, k0 + p * stride);
+  for (uint32_t k = k0; k < rb; k += PD * stride) {
+#pragma unroll
+    for (int p = 0; p < PD; ++p) {
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int i = 0; i < TT; ++i)
+#pragma unroll
+          for (int j = 0; j < NE; ++j) acc[i][j] = mma_step<T>(fx[p][s][i], fg[p][s][j], acc[i][j]);
+      load(p, k + (p + PD) * stride);
+    }
+  }
+  // lane 16 g + c of a tile holds tokens 4 g .. 4 g + 3 of expert c
+#pragma unroll
+  for (int i = 0; i < TT; ++i)
+#pragma unroll
+    for (int j = 0; j < NE; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) red[wv][16 * i + 4 * g + r][16 * j + c] = acc[i][j][r];
+  __syncthreads();
+
+  for (int i = wv; i < n_tok; i += NW) {
+    const int64_t t = t0 + i;
+    const bool expert = lane < a.E;
+    float l = 0.0f;
+    if (lane < NE * 16) {
+#pragma unroll
+      for (int w = 0; w < NW; ++w) l += red[w][i][lane];
+    }
+    const bool on = a.active == nullptr || a.active[t] != 0;
+    float top = expert ? l : -__builtin_inff();
+#pragma unroll
+    for (int m = kWave / 2; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, kWave));
+    const float e = expert ? expf(l - top) : 0.0f;
+    float sum = e;
+#pragma unroll
+    for (int m = kWave / 2; m >= 1; m >>= 1) sum += __shfl_xor(sum, m, kWave);
+    const float p = e / sum;
+    // place in the order by logit: the experts before this one
+    const uint32_t key = logit_key(l);
+    int rank = expert ? 0 : kMaxE;
+    for (int j = 0; j < a.E; ++j) {
+      const uint32_t o = __builtin_amdgcn_readlane(key, j);
+      rank += o > key || (o == key && j < lane) ? 1 : 0;
+    }
+    const bool chosen = rank < a.K;
+    float w = chosen ? p : 0.0f;
+    if (a.renorm) {
+      float kept = w;
+#pragma unroll
+      for (int m = kWave / 2; m >= 1; m >>= 1) kept += __shfl_xor(kept, m, kWave);
+      w = w / kept;
+    }
+    const uint64_t mask = __ballot(chosen);
+    if (expert) {
+      const float v = on ? p : 0.0f;
+      if (probs_bf16)
+        static_cast<__bf16*>(a.probs)[t * a.probs_stride + lane] = static_cast<__bf16>(v);
+      else
+        static_cast<float*>(a.probs)[t * a.probs_stride + lane] = v;
+    }
+    if (chosen) {
+      a.ids[t * a.K + rank] = on ? lane : -1;
+      a.weight[t * a.K + rank] = on ? w : 0.0f;
+    }
+    if (lane == 0 && a.mask != nullptr) a.mask[t] = on ? mask : 0ull;
+  }
+}
+
+template <typename T, int NE>
+void route(const RouteArgs& a, bool probs_bf16, hipStream_t st) {
+  if (a.T <= 2048) {
+    const unsigned grid = static_cast<unsigned>((a.T + 15) / 16);
+    constexpr int NW = NE == 4 ? 8 : 16;   // (the sums of 16 wavefronts of 64 experts would not fit 64 KB)
+    k_route<T, 1, NE, NW><<<grid, NW * kWave, 0, st>>>(a, probs_bf16);
+  } else {
+    const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.T) + 31) / 32);
+    k_route<T, 2, NE, 4><<<grid, 4 * kWave, 0, st>>>(a, probs_bf16);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_moe_route(const RouteArgs& a, fm_dtype dt, fm_dtype probs_dt, hipStream_t st) {
+  const bool pb = probs_dt == FM_BF16;
+  const int ne = (a.E + 15) / 16;
+  if (dt == FM_BF16) {
+    if (ne == 1) route<uint16_t, 1>(a, pb, st);
+    else if (ne == 2) route<uint16_t, 2>(a, pb, st);
+    else route<uint16_t, 4>(a, pb, st);
+  } else {
+    if (ne == 1) route<float, 1>(a, pb, st);
+    else if (ne == 2) route<float, 2>(a, pb, st);
+    else route<float, 4>(a, pb, st);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace fm

@@ -1,0 +1,257 @@
+"""The model operators around the expert-map search: token embeddings and their
+gradient, the gate of an MoE layer, and the chosen experts' products on experts
+that a cache holds (fm_embed_*, fm_moe_* of include/finemoe_map.h).
+
+Argument marshalling only, as the rest of the binding: every step runs in the
+library's HIP kernels.  Tensors must be contiguous, on one GPU and of the stated
+type; outputs are created unless ``out`` gives them.  Work goes to the current
+stream, or to ``stream``.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+from typing import Optional, Tuple
+
+import torch
+
+from . import _DTYPES, _TORCH, _aligned_bytes, _lib, _need, _ptr, _stream
+
+_CODE = {torch.float32: _lib.FM_F32, torch.bfloat16: _lib.FM_BF16}
+_NO_GUARD = contextlib.nullcontext()
+
+
+def _on(device: torch.device):
+    """The calls enqueue on the current device: make it the tensors'."""
+    if device.type != "cuda":
+        raise ValueError(f"tensors are on {device}, not on a GPU")
+    return _NO_GUARD if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _float_rows(t, name: str, shape) -> torch.Tensor:
+    """A float32 or bfloat16 tensor; later tensors are checked against its device."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
+    if t.dtype not in _CODE:
+        raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+    return _need(t, name, t.dtype, shape, t.device)
+
+
+def _flags(flags, dev):
+    return None if flags is None else _need(flags, "flags", torch.int32, (1,), dev).data_ptr()
+
+
+def embed_lookup(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                 flags: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """scale * table[tokens]: table [V][d], tokens [T] int32 (negative: padding, a row of zeros) -> [T][d]."""
+    _float_rows(table, "table", (None, None))
+    V, d = table.shape
+    dev = table.device
+    _need(tokens, "tokens", torch.int32, (None,), dev)
+    T = tokens.shape[0]
+    if out is None:
+        out = torch.empty((T, d), dtype=table.dtype, device=dev)
+    else:
+        _need(out, "out", table.dtype, (T, d), dev)
+    fl = _flags(flags, dev)
+    with _on(dev):
+        _lib.check(_lib.load().fm_embed_lookup(table.data_ptr(), V, d, _CODE[table.dtype], tokens.data_ptr(), T, scale,
+                                               out.data_ptr(), fl, _stream(stream)), "fm_embed_lookup")
+    return out
+
+
+def embed_pool(table: torch.Tensor, tokens: torch.Tensor, offsets: torch.Tensor, scale: float = 1.0,
+               out: Optional[torch.Tensor] = None, flags: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Mean embedding of each request, times scale: offsets [B + 1] int32 into tokens -> [B][d] bfloat16, the
+    queries of match_semantic."""
+    _float_rows(table, "table", (None, None))
+    V, d = table.shape
+    dev = table.device
+    _need(tokens, "tokens", torch.int32, (None,), dev)
+    _need(offsets, "offsets", torch.int32, (None,), dev)
+    B = offsets.shape[0] - 1
+    if B < 0:
+        raise ValueError("offsets must hold at least one element")
+    if out is None:
+        out = torch.empty((B, d), dtype=torch.bfloat16, device=dev)
+    else:
+        _need(out, "out", torch.bfloat16, (B, d), dev)
+    fl = _flags(flags, dev)
+    with _on(dev):
+        _lib.check(_lib.load().fm_embed_pool(table.data_ptr(), V, d, _CODE[table.dtype], tokens.data_ptr(),
+                                             tokens.shape[0], offsets.data_ptr(), B, scale, out.data_ptr(),
+                                             fl, _stream(stream)), "fm_embed_pool")
+    return out
+
+
+def embed_grad_scratch_bytes(T_max: int, V: int) -> int:
+    return int(_lib.load().fm_embed_grad_scratch_bytes(T_max, V))
+
+
+class EmbedGradScratch:
+    """Device scratch for embed_grad calls of up to T_max tokens on a table of V
+    rows (every call rewrites what it reads).  Calls sharing one must be ordered."""
+
+    def __init__(self, T_max: int, V: int, device="cuda"):
+        self.nbytes = embed_grad_scratch_bytes(T_max, V)
+        if self.nbytes == 0:
+            raise ValueError(f"invalid scratch request T_max={T_max} V={V}")
+        self.buf = _aligned_bytes(self.nbytes, device)
+
+
+def embed_grad(dout: torch.Tensor, tokens: torch.Tensor, V: int, scale: float = 1.0,
+               grad_dtype: Optional[torch.dtype] = None, accumulate: bool = False, out: Optional[torch.Tensor] = None,
+               scratch: Optional[EmbedGradScratch] = None, flags: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """Gradient of embed_lookup with respect to the table: dout [T][d], tokens [T] int32 -> [V][d] of grad_dtype
+    (float32 by default, or out's).  accumulate adds to the rows of ``out`` that tokens select."""
+    _float_rows(dout, "dout", (None, None))
+    T, d = dout.shape
+    dev = dout.device
+    _need(tokens, "tokens", torch.int32, (T,), dev)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty((V, d), dtype=torch.float32 if grad_dtype is None else grad_dtype, device=dev)
+    if grad_dtype is not None and out.dtype != grad_dtype:
+        raise ValueError(f"out must be {grad_dtype}, got {out.dtype}")
+    _float_rows(out, "out", (V, d))
+    _need(out, "out", out.dtype, (V, d), dev)
+    fl = _flags(flags, dev)
+    with _on(dev):
+        if scratch is None:
+            scratch = EmbedGradScratch(T, V, dev)
+        _need(scratch.buf, "scratch", torch.uint8, (scratch.nbytes,), dev)
+        _lib.check(_lib.load().fm_embed_grad(dout.data_ptr(), _CODE[dout.dtype], tokens.data_ptr(), T, V, d, scale,
+                                             1 if accumulate else 0, out.data_ptr(), _CODE[out.dtype],
+                                             scratch.buf.data_ptr(), scratch.nbytes, fl,
+                                             _stream(stream)), "fm_embed_grad")
+    return out
+
+
+def moe_route(x: torch.Tensor, gate: torch.Tensor, k: int, renorm: bool = False,
+              active: Optional[torch.Tensor] = None, probs_dtype: torch.dtype = torch.float32,
+              out: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor, Optional[torch.Tensor]]] = None,
+              stream=None):
+    """The gate of one MoE layer: x [T][d], gate [E][d], active [T] uint8 or None -> (probs [T][E], ids [T][k] int32,
+    weight [T][k] float32, mask [T] int64 holding uint64 bits).  ``out`` may give probs as a layer's rows of a batch of
+    maps or trajectory queries (q[:, layer]): its rows need not follow each other; mask may be None there."""
+    _float_rows(x, "x", (None, None))
+    T, d = x.shape
+    dev = x.device
+    _need(gate, "gate", x.dtype, (None, d), dev)
+    E = gate.shape[0]
+    if active is not None:
+        _need(active, "active", torch.uint8, (T,), dev)
+    if out is None:
+        out = (torch.empty((T, E), dtype=probs_dtype, device=dev), torch.empty((T, k), dtype=torch.int32, device=dev),
+               torch.empty((T, k), dtype=torch.float32, device=dev), torch.empty((T,), dtype=torch.int64, device=dev))
+    probs, ids, weight, mask = out
+    if not isinstance(probs, torch.Tensor) or probs.dtype not in _CODE or probs.shape != (T, E) or probs.device != dev \
+            or (E > 1 and probs.stride(1) != 1) or (T > 1 and probs.stride(0) < E):
+        raise ValueError(f"out[0] (probs) must be a float32 or bfloat16 [{T}x{E}] tensor on {dev} with contiguous rows")
+    _need(ids, "out[1] (ids)", torch.int32, (T, k), dev)
+    _need(weight, "out[2] (weight)", torch.float32, (T, k), dev)
+    if mask is not None:
+        _need(mask, "out[3] (mask)", torch.int64, (T,), dev)
+    with _on(dev):
+        _lib.check(_lib.load().fm_moe_route(x.data_ptr(), gate.data_ptr(), _CODE[x.dtype], T, d, E, k,
+                                            1 if renorm else 0, _ptr(active), probs.data_ptr(), _CODE[probs.dtype],
+                                            probs.stride(0) if T > 1 else E, ids.data_ptr(), weight.data_ptr(),
+                                            _ptr(mask), _stream(stream)), "fm_moe_route")
+    return out
+
+
+class ExpertCache:
+    """Experts of one MoE layer held on the GPU: ``weights`` [slots][3 d f] (a slot is one expert's gate and up
+    projections [f][d], then its down projection [d][f], one block), ``slot_of`` [E] int32 (-1: not held).  Both are
+    plain tensors that the owner may also fill itself."""
+
+    def __init__(self, slots: int, E: int, d: int, f: int, dtype: str = "bf16", device="cuda"):
+        self.slots, self.E, self.d, self.f = int(slots), int(E), int(d), int(f)
+        self.dtype = _TORCH[_DTYPES[dtype]]
+        self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        if not (1 <= self.E <= 64 and self.slots >= 1) or moe_workspace_bytes(self.d, self.f, dtype, 1, 1) == 0:
+            raise ValueError(f"invalid expert cache slots={slots} E={E} d={d} f={f}")
+        self.weights = torch.empty((self.slots, 3 * self.d * self.f), dtype=self.dtype, device=self.device)
+        self.slot_of = torch.full((self.E,), -1, dtype=torch.int32, device=self.device)
+        self.flags = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._desc = _lib.ExpertCacheDesc(self.E, self.slots, self.d, self.f, _DTYPES[dtype], self.weights.data_ptr(),
+                                          self.slot_of.data_ptr())
+        self.desc = C.byref(self._desc)
+        self.workspace = None
+
+    def load(self, expert: int, slot: int, gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor) -> None:
+        """Put an expert (gate, up [f][d], down [d][f]) into a slot, on the current stream; an expert that the slot
+        held before is no longer held."""
+        if not (0 <= expert < self.E and 0 <= slot < self.slots):
+            raise ValueError(f"expert {expert} or slot {slot} out of range")
+        n = self.d * self.f
+        for t, name, shape in ((gate, "gate", (self.f, self.d)), (up, "up", (self.f, self.d)),
+                               (down, "down", (self.d, self.f))):
+            if tuple(t.shape) != shape or t.dtype != self.dtype:
+                raise ValueError(f"{name} must be {self.dtype} of shape {list(shape)}")
+        for i, t in enumerate((gate, up, down)):
+            self.weights[slot, i * n:(i + 1) * n].view(t.shape).copy_(t, non_blocking=True)
+        self.slot_of.masked_fill_(self.slot_of == slot, -1)
+        self.slot_of[expert] = slot
+
+    def evict(self, expert: int) -> None:
+        """The expert is no longer held (its slot may be loaded again)."""
+        self.slot_of[expert] = -1
+
+    def check(self) -> int:
+        """Synchronise and return the sticky FM_FLAG_* bits of the calls so far, cleared."""
+        f = int(self.flags.item())
+        self.flags.zero_()
+        return f
+
+    def ensure_workspace(self, T: int, K: int) -> "MoeWorkspace":
+        if self.workspace is None or moe_workspace_bytes(self.d, self.f, self._name(), max(T, 1), K) > self.workspace.nbytes:
+            self.workspace = MoeWorkspace(self, max(T, 1), K)
+        return self.workspace
+
+    def _name(self) -> str:
+        return "bf16" if self.dtype is torch.bfloat16 else "f32"
+
+
+def moe_workspace_bytes(d: int, f: int, dtype: str = "bf16", T_max: int = 256, K: int = 8) -> int:
+    return int(_lib.load().fm_moe_workspace_bytes(d, f, _DTYPES[dtype], T_max, K))
+
+
+class MoeWorkspace:
+    """Device scratch for moe_experts calls of up to T_max tokens of K experts each (every call rewrites what it
+    reads).  Calls sharing one workspace must be ordered."""
+
+    def __init__(self, cache: ExpertCache, T_max: int = 256, K: int = 8):
+        self.nbytes = moe_workspace_bytes(cache.d, cache.f, cache._name(), T_max, K)
+        if self.nbytes == 0:
+            raise ValueError(f"invalid workspace request T_max={T_max} K={K}")
+        self.buf = _aligned_bytes(self.nbytes, cache.device)
+
+
+def moe_experts(cache: ExpertCache, x: torch.Tensor, ids: torch.Tensor, weight: torch.Tensor,
+                residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                workspace: Optional[MoeWorkspace] = None, stream=None) -> torch.Tensor:
+    """residual + the weighted products of each token's experts: x [T][d], ids [T][K] int32, weight [T][K] float32 as
+    moe_route gives them -> [T][d].  Experts that the cache does not hold are left out and flagged (cache.check())."""
+    dev = cache.device
+    _need(x, "x", cache.dtype, (None, cache.d), dev)
+    T = x.shape[0]
+    _need(ids, "ids", torch.int32, (T, None), dev)
+    K = ids.shape[1]
+    _need(weight, "weight", torch.float32, (T, K), dev)
+    if residual is not None:
+        _need(residual, "residual", cache.dtype, (T, cache.d), dev)
+    if out is None:
+        out = torch.empty((T, cache.d), dtype=cache.dtype, device=dev)
+    else:
+        _need(out, "out", cache.dtype, (T, cache.d), dev)
+    ws = workspace if workspace is not None else cache.ensure_workspace(T, K)
+    with _on(dev):
+        _lib.check(_lib.load().fm_moe_experts(cache.desc, x.data_ptr(), ids.data_ptr(), weight.data_ptr(), T, K,
+                                              _ptr(residual), out.data_ptr(), cache.flags.data_ptr(),
+                                              ws.buf.data_ptr(), ws.nbytes, _stream(stream)), "fm_moe_experts")
+    return out
