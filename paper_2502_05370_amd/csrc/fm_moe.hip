@@ -17,6 +17,8 @@
 // and the nearest bf16 of the rest, both multiplied, so that the only rounding
 // to bf16 that shows is the output's own.  The weights' stream bounds the
 // second product, and the extra matrix instructions hide behind it.
+#include <type_traits>
+
 #include "fm_internal.h"
 #include "fm_mma.h"
 
@@ -109,51 +111,63 @@ __device__ __forceinline__ uint16_t to_bf16(float f) { return __builtin_bit_cast
 // ---------------------------------------------------------------- gate and up
 
 // One pass over a block of 16 gate and 16 up rows for up to 16 N of the
-// expert's tokens.
-template <typename T, int N, int PD>
+// expert's tokens.  The wavefronts deal the load groups of a row among
+// themselves, starting at a place that differs from block to block: rows of a
+// power of two bytes would otherwise keep all workgroups on few memory channels
+// at a time (2 GB in rows of 8 KB: 5.9 -> 7.1 TB/s).
+template <typename T, int N, int PA>
 __device__ __forceinline__ void up_pass(const MoeArgs& a, __amdgpu_buffer_rsrc_t rs_w, __amdgpu_buffer_rsrc_t rs_x,
                                         int row0, const int32_t* tok, const float* wt, int n, int place0,
                                         floatx4 (*red)[2][N][kWave]) {
   const int lane = threadIdx.x % kWave;
-  const int wv = threadIdx.x / kWave;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c = lane % 16;
   const int g = lane / 16;
   const uint32_t rb = static_cast<uint32_t>(a.d) * sizeof(T);
-  const bool row_in = row0 + c < a.f;
-  const uint32_t ro_g = row_in ? static_cast<uint32_t>(row0 + c) * rb : kOutside;
-  const uint32_t ro_u = row_in ? static_cast<uint32_t>(a.f + row0 + c) * rb : kOutside;
+  const WeightRows w_gate(row0, a.f, rb, 0u, c, g);
+  const WeightRows w_up(row0, a.f, rb, static_cast<uint32_t>(a.f) * rb, c, g);
   uint32_t ro_x[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) ro_x[j] = 16 * j + c < n ? static_cast<uint32_t>(tok[16 * j + c]) * rb : kOutside;
   floatx4 acc[2][N];
 #pragma unroll
   for (int j = 0; j < N; ++j) acc[0][j] = acc[1][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  uint32x4 fw[PD][2][2], fx[PD][2][N];
-  auto load = [&](int p, uint32_t k) __attribute__((always_inline)) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const uint32_t kk = k + s * kStepBytes + g * 16;
-      fw[p][s][0] = load_step(rs_w, ro_g, kk, rb);
-      fw[p][s][1] = load_step(rs_w, ro_u, kk, rb);
-#pragma unroll
-      for (int j = 0; j < N; ++j) fx[p][s][j] = load_step(rs_x, ro_x[j], kk, rb);
-    }
+  const int groups = static_cast<int>((rb + kGroupBytes - 1) / kGroupBytes);
+  const int mine = groups > wv ? (groups - wv + kUpWaves - 1) / kUpWaves : 0;   // groups of this wavefront
+  const int turn = static_cast<int>(static_cast<uint32_t>(row0 / kUpRows) * 37u % static_cast<uint32_t>(groups));
+  uint32x4 fw[PA][2][2], fx[2][2][N];
+  auto place = [&](int i) __attribute__((always_inline)) {   // byte of group i of this wavefront (past the row: none)
+    const int q = wv + i * kUpWaves + turn;
+    return i < mine ? static_cast<uint32_t>(q < groups ? q : q - groups) * kGroupBytes : rb;
   };
-  const uint32_t stride = kUpWaves * kGroupBytes;
-  const uint32_t k0 = static_cast<uint32_t>(wv) * kGroupBytes;
+  auto load_w = [&](int p, uint32_t k) __attribute__((always_inline)) {
+    w_gate.load(rs_w, k, rb, fw[p][0]);
+    w_up.load(rs_w, k, rb, fw[p][1]);
+  };
+  auto load_x = [&](int p, uint32_t k) __attribute__((always_inline)) {
 #pragma unroll
-  for (int p = 0; p < PD; ++p) load(p, k0 + p * stride);
-  for (uint32_t k = k0; k < rb; k += PD * stride) {
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-    for (int p = 0; p < PD; ++p) {
+      for (int j = 0; j < N; ++j) fx[p][s][j] = load_step(rs_x, ro_x[j], k + s * kStepBytes + g * 16, rb);
+  };
+#pragma unroll
+  for (int p = 0; p < PA; ++p) load_w(p, place(p));
+  load_x(0, place(0));
+  for (int i = 0; i < mine; i += PA) {
+#pragma unroll
+    for (int p = 0; p < PA; ++p) {
+      load_x((p + 1) % 2, place(i + p + 1));
+      uint32x4 sg[2], su[2];
+      WeightRows::steps(fw[p][0], sg);
+      WeightRows::steps(fw[p][1], su);
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          acc[0][j] = mma_step<T>(fw[p][s][0], fx[p][s][j], acc[0][j]);
-          acc[1][j] = mma_step<T>(fw[p][s][1], fx[p][s][j], acc[1][j]);
+          acc[0][j] = mma_step<T>(sg[s], fx[p % 2][s][j], acc[0][j]);
+          acc[1][j] = mma_step<T>(su[s], fx[p % 2][s][j], acc[1][j]);
         }
-      load(p, k + (p + PD) * stride);
+      load_w(p, place(i + p + PA));
     }
   }
 #pragma unroll
@@ -204,7 +218,7 @@ __global__ void __launch_bounds__(kUpWaves * kWave) k_moe_up(MoeArgs a) {
   __shared__ Plan pl;
   __shared__ int32_t tok[kMoeTokens];
   __shared__ float wt[kMoeTokens];
-  __shared__ floatx4 red[kUpWaves][2][N][kWave];
+  __shared__ floatx4 red[kUpWaves * 2 * N * kWave];
   const int blocks = (a.f + kUpRows - 1) / kUpRows;
   // the tickets of the launch after this one
   if (blockIdx.x == 0)
@@ -228,9 +242,16 @@ __global__ void __launch_bounds__(kUpWaves * kWave) k_moe_up(MoeArgs a) {
   const size_t slot_bytes = static_cast<size_t>(3) * a.d * a.f * sizeof(T);
   const __amdgpu_buffer_rsrc_t rs_w = row_buffer(a.slots + pl.slot[e] * slot_bytes, static_cast<uint32_t>(slot_bytes));
   const __amdgpu_buffer_rsrc_t rs_x = row_buffer(a.x, static_cast<uint32_t>(a.T) * a.d * sizeof(T));
+  auto pass = [&](auto cols, int p) __attribute__((always_inline)) {
+    constexpr int C = decltype(cols)::value;
+    up_pass<T, C, C == 1 ? 4 : 2>(a, rs_w, rs_x, row0, tok + p, wt + p, n - p, pl.first[e] + p,
+                                  reinterpret_cast<floatx4(*)[2][C][kWave]>(red));
+  };
   for (int p = 0; p < n; p += 16 * N) {
     if (p > 0) __syncthreads();   // the last pass's sums are read
-    up_pass<T, N, N == 4 ? 2 : 4>(a, rs_w, rs_x, row0, tok + p, wt + p, n - p, pl.first[e] + p, red);
+    if (N == 1 || n - p <= 16) pass(std::integral_constant<int, 1>(), p);
+    else if (N == 2 || n - p <= 32) pass(std::integral_constant<int, N < 2 ? N : 2>(), p);
+    else pass(std::integral_constant<int, N>(), p);
   }
 }
 
@@ -238,10 +259,9 @@ __global__ void __launch_bounds__(kUpWaves * kWave) k_moe_up(MoeArgs a) {
 
 // Load groups [m0, m1) of 16 R rows of one expert's Down for up to 16 N of its
 // tokens, added to the wavefront's sums own[t][16 R].
-template <typename T, int N, int R, int PD>
+template <typename T, int N, int R, int PA>
 __device__ __forceinline__ void down_pass(const MoeArgs& a, __amdgpu_buffer_rsrc_t rs_w, __amdgpu_buffer_rsrc_t rs_h,
-                                          const uint32_t (&ro_w)[R], int m0, int m1, const uint16_t* tok, int n,
-                                          int place0, float* own) {
+                                          int row0, int m0, int m1, const uint16_t* tok, int n, int place0, float* own) {
   constexpr int H = sizeof(T) == 2 ? 2 : 1;   // planes of h
   const int lane = threadIdx.x % kWave;
   const int c = lane % 16;
@@ -256,36 +276,45 @@ __device__ __forceinline__ void down_pass(const MoeArgs& a, __amdgpu_buffer_rsrc
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[r][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  uint32x4 fw[PD][2][R], fh[PD][2][H][N];
+  uint32x4 fw[PA][R][2], fh[2][2][H][N];
   const uint32_t k_end = static_cast<uint32_t>(m1) * kGroupBytes < rb ? static_cast<uint32_t>(m1) * kGroupBytes : rb;
-  auto load = [&](int p, uint32_t k) __attribute__((always_inline)) {
+  auto load_w = [&](int p, uint32_t k) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const uint32_t kk = k + s * kStepBytes + g * 16;
+    for (int r = 0; r < R; ++r) {
+      const WeightRows w(row0 + 16 * r, a.d, rb, 0u, c, g);
+      w.load(rs_w, k, k_end, fw[p][r]);
+    }
+  };
+  auto load_h = [&](int p, uint32_t k) __attribute__((always_inline)) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) fw[p][s][r] = load_step(rs_w, ro_w[r], kk, k_end);
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int j = 0; j < N; ++j)
 #pragma unroll
         for (int q = 0; q < H; ++q)
-          fh[p][s][q][j] = load_step(rs_h, ro_h[j] == kOutside ? kOutside : ro_h[j] + q * plane, kk, k_end);
-    }
+          fh[p][s][q][j] = load_step(rs_h, ro_h[j] == kOutside ? kOutside : ro_h[j] + q * plane,
+                                     k + s * kStepBytes + g * 16, k_end);
   };
   const uint32_t k0 = static_cast<uint32_t>(m0) * kGroupBytes;
 #pragma unroll
-  for (int p = 0; p < PD; ++p) load(p, k0 + p * kGroupBytes);
-  for (uint32_t k = k0; k < k_end; k += PD * kGroupBytes) {
+  for (int p = 0; p < PA; ++p) load_w(p, k0 + p * kGroupBytes);
+  load_h(0, k0);
+  for (uint32_t k = k0; k < k_end; k += PA * kGroupBytes) {
 #pragma unroll
-    for (int p = 0; p < PD; ++p) {
+    for (int p = 0; p < PA; ++p) {
+      load_h((p + 1) % 2, k + (p + 1) * kGroupBytes);
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+      for (int r = 0; r < R; ++r) {
+        uint32x4 sw[2];
+        WeightRows::steps(fw[p][r], sw);
 #pragma unroll
-        for (int j = 0; j < N; ++j)
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int r = 0; r < R; ++r)
+          for (int j = 0; j < N; ++j)
 #pragma unroll
-            for (int q = 0; q < H; ++q) acc[r][j] = mma_step<T>(fw[p][s][r], fh[p][s][q][j], acc[r][j]);
-      load(p, k + (p + PD) * kGroupBytes);
+            for (int q = 0; q < H; ++q) acc[r][j] = mma_step<T>(sw[s], fh[p % 2][s][q][j], acc[r][j]);
+      }
+      load_w(p, k + (p + PA) * kGroupBytes);
     }
   }
 #pragma unroll
@@ -334,12 +363,6 @@ __global__ void __launch_bounds__(NW * kWave) k_moe_down(MoeArgs a) {
   const uint32_t down_bytes = static_cast<uint32_t>(static_cast<size_t>(a.d) * a.f * sizeof(T));
   const uint32_t h_bytes = static_cast<uint32_t>(static_cast<size_t>(a.T) * a.K * a.f * 4);   // two bf16 planes or one float32
   const __amdgpu_buffer_rsrc_t rs_h = row_buffer(a.h, h_bytes);
-  uint32_t ro_w[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int row = row0 + 16 * r + lane % 16;
-    ro_w[r] = row < a.d ? static_cast<uint32_t>(row) * (static_cast<uint32_t>(a.f) * sizeof(T)) : kOutside;
-  }
   while (u < u1) {
     const int i_used = u / groups;
     const int m0 = u - i_used * groups;
@@ -350,8 +373,15 @@ __global__ void __launch_bounds__(NW * kWave) k_moe_down(MoeArgs a) {
     const int slot = __builtin_amdgcn_readfirstlane(pl.slot[e]);
     const __amdgpu_buffer_rsrc_t rs_w = row_buffer(
         a.slots + (slot * slot_elems + static_cast<size_t>(2) * a.d * a.f) * sizeof(T), down_bytes);
-    for (int p = 0; p < n; p += 16 * N)
-      down_pass<T, N, R, N == 4 ? 2 : 4>(a, rs_w, rs_h, ro_w, m0, m1, tok + first + p, n - p, first + p, own);
+    auto pass = [&](auto cols, int p) __attribute__((always_inline)) {
+      constexpr int C = decltype(cols)::value;
+      down_pass<T, C, R, C * R <= 2 ? 4 : 2>(a, rs_w, rs_h, row0, m0, m1, tok + first + p, n - p, first + p, own);
+    };
+    for (int p = 0; p < n; p += 16 * N) {
+      if (N == 1 || n - p <= 16) pass(std::integral_constant<int, 1>(), p);
+      else if (N == 2 || n - p <= 32) pass(std::integral_constant<int, N < 2 ? N : 2>(), p);
+      else pass(std::integral_constant<int, N>(), p);
+    }
     u += m1 - m0;
   }
   __syncthreads();
@@ -366,15 +396,17 @@ __global__ void __launch_bounds__(NW * kWave) k_moe_down(MoeArgs a) {
       floatx4 v = reinterpret_cast<floatx4*>(sums)[i];
 #pragma unroll
       for (int w = 1; w < NW; ++w) v += reinterpret_cast<floatx4*>(sums)[w * quads + i];
-      *reinterpret_cast<floatx4*>(a.partial + (static_cast<int64_t>(split) * a.T + t) * a.d + row) = v;
+      float* o = a.partial + (static_cast<int64_t>(split) * a.T + t) * a.d + row;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) __hip_atomic_store(o + r, v[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    wait_vmcnt<0>();
     __syncthreads();
     if (tid == 0)
-      is_last = __hip_atomic_fetch_add(&a.ticket[rbk], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
+      is_last = __hip_atomic_fetch_add(&a.ticket[rbk], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
                 static_cast<uint32_t>(a.splits) - 1u;
     __syncthreads();
     if (!is_last) return;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   }
   for (int i = tid; i < quads; i += NW * kWave) {
     const int t = i / (4 * R);
@@ -382,8 +414,11 @@ __global__ void __launch_bounds__(NW * kWave) k_moe_down(MoeArgs a) {
     if (row >= a.d) continue;
     floatx4 v = floatx4{0.f, 0.f, 0.f, 0.f};
     if (a.splits > 1) {
-      for (int s = 0; s < a.splits; ++s)
-        v += *reinterpret_cast<const floatx4*>(a.partial + (static_cast<int64_t>(s) * a.T + t) * a.d + row);
+      for (int s = 0; s < a.splits; ++s) {
+        const float* o = a.partial + (static_cast<int64_t>(s) * a.T + t) * a.d + row;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] += __hip_atomic_load(o + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
     } else {
 #pragma unroll
       for (int w = 0; w < NW; ++w) v += reinterpret_cast<floatx4*>(sums)[w * quads + i];
@@ -405,9 +440,21 @@ __global__ void __launch_bounds__(NW * kWave) k_moe_down(MoeArgs a) {
 
 // ---------------------------------------------------------------- host
 
-template <typename T, int N, int NW>
+// Rows and wavefronts of k_moe_down's workgroups for launches of T tokens.
+struct DownShape {
+  int R, NW;
+};
+DownShape down_shape(int32_t T) { return T <= 16 ? DownShape{1, 16} : (T <= 128 ? DownShape{2, 8} : DownShape{2, 4}); }
+int row_blocks_of(int32_t d, int32_t T) { return (d + 16 * down_shape(T).R - 1) / (16 * down_shape(T).R); }
+int splits_of(int32_t d, int32_t T) {
+  const int blocks = row_blocks_of(d, T);
+  const int want = 4096 / down_shape(T).NW;   // workgroups that fill the GPU: 16 wavefronts per CU
+  const int s = (want + blocks - 1) / blocks;
+  return s < kMaxSplits ? s : kMaxSplits;
+}
+
+template <typename T, int N, int R, int NW>
 hipError_t launch(MoeArgs a, hipStream_t st) {
-  constexpr int R = 2;
   const int experts = a.E < a.T * a.K ? a.E : a.T * a.K;   // at most this many are in use
   const unsigned up = static_cast<unsigned>(experts) * static_cast<unsigned>((a.f + kUpRows - 1) / kUpRows);
   k_moe_up<T, N><<<up, kUpWaves * kWave, 0, st>>>(a);
@@ -425,26 +472,21 @@ hipError_t launch(MoeArgs a, hipStream_t st) {
 }
 
 template <typename T>
-hipError_t experts(MoeArgs a, hipStream_t st) {
-  if (a.T <= 16) return launch<T, 1, 8>(a, st);
-  if (a.T <= 32) return launch<T, 2, 8>(a, st);
-  if (a.T <= 128) return launch<T, 4, 8>(a, st);
-  return launch<T, 4, 4>(a, st);
+hipError_t experts(const MoeArgs& a, hipStream_t st) {   // as down_shape
+  if (a.T <= 16) return launch<T, 1, 1, 16>(a, st);
+  if (a.T <= 32) return launch<T, 2, 2, 8>(a, st);
+  if (a.T <= 128) return launch<T, 4, 2, 8>(a, st);
+  return launch<T, 4, 2, 4>(a, st);
 }
 
-int row_blocks_of(int32_t d) { return (d + 31) / 32; }
-int splits_of(int32_t d) {
-  const int s = (512 + row_blocks_of(d) - 1) / row_blocks_of(d);
-  return s < kMaxSplits ? s : kMaxSplits;
-}
-
-// Workspace of one launch: [h][partial sums][tickets], each 256-byte aligned.
+// Workspace of one launch: [h][partial sums][tickets], each 256-byte aligned; a
+// launch of fewer tokens never needs more.
 size_t parts(int32_t d, int32_t f, int32_t T, int32_t K, size_t* partial, size_t* ticket) {
   size_t o = align_up(static_cast<size_t>(T) * K * f * 4, kAlign);
   *partial = o;
-  o += align_up(static_cast<size_t>(splits_of(d)) * T * d * sizeof(float), kAlign);
+  o += align_up(static_cast<size_t>(splits_of(d, T)) * T * d * sizeof(float), kAlign);
   *ticket = o;
-  return o + align_up(static_cast<size_t>(row_blocks_of(d)) * sizeof(uint32_t), kAlign);
+  return o + align_up(static_cast<size_t>((d + 15) / 16) * sizeof(uint32_t), kAlign);   // (the most row blocks of any T)
 }
 
 }  // namespace
@@ -480,8 +522,8 @@ hipError_t launch_moe_experts(const fm_expert_cache& c, const void* x, const int
     a.n_slots = c.n_slots;
     a.d = c.d;
     a.f = c.f;
-    a.splits = splits_of(c.d);
-    a.row_blocks = row_blocks_of(c.d);
+    a.splits = splits_of(c.d, a.T);
+    a.row_blocks = row_blocks_of(c.d, a.T);
     const hipError_t e = c.dtype == FM_BF16 ? experts<uint16_t>(a, st) : experts<float>(a, st);
     if (e != hipSuccess) return e;
   }
