@@ -48,6 +48,7 @@ __device__ __forceinline__ uint32x4 load_step(__amdgpu_buffer_rsrc_t rs, uint32_
 struct WeightRows {
   uint32_t lo, hi;   // byte offsets of rows c % 8 and 8 + c % 8 (or kOutside), with the lane's place in the line
   uint32_t lane_k;   // that place
+  WeightRows() = default;
   __device__ __forceinline__ WeightRows(int row0, int rows, uint32_t row_bytes, uint32_t base, int c, int g) {
     lane_k = static_cast<uint32_t>(c / 8) * kStepBytes + static_cast<uint32_t>(g) * 16u;
     const int r = row0 + c % 8;

@@ -27,9 +27,10 @@ namespace fm {
 namespace {
 
 constexpr int kUpWaves = 8;
-constexpr int kUpRows = 16;        // rows of Gate and of Up per workgroup
+constexpr int kUpRows = 16;        // rows of Gate and of Up per block
 constexpr int kMaxSplits = 16;     // workgroups that share one block of output rows
 constexpr int kGroupBytes = 2 * kStepBytes;   // of every row in one load group
+constexpr int kMaxTiles = 4;       // tiles of 16 tokens in one pass over an expert's weights
 
 struct MoeArgs {
   const char* slots;
@@ -46,137 +47,248 @@ struct MoeArgs {
   int32_t T, K, E, n_slots, d, f, splits, row_blocks;
 };
 
-// Which tokens take which experts, in LDS: for every expert in use its slot,
-// its number of tokens and the first of its places in the concatenated lists.
+// Which tokens take which experts, in LDS, for launches of up to MAXT tokens.
+// An expert's tokens, in order, are its places; the experts' places follow each
+// other.  An entry is one pass over an expert's weights for up to 64 of its
+// places; entries are ordered by their tiles of 16 (1, 2 or 4).
+template <int MAXT>
 struct Plan {
-  uint64_t takes[kMaxE][kMoeTokens / 64];   // tokens that take the expert
+  static constexpr int kWords = (MAXT + 63) / 64;
+  static constexpr int kPairs = MAXT * kMaxK;
+  static constexpr int kEntries = kMaxE + kPairs / 64;
+  uint64_t takes[kMaxE][kWords];   // tokens that take the expert
   int32_t slot[kMaxE];
-  int32_t count[kMaxE];
-  int32_t first[kMaxE];
-  int32_t used[kMaxE];      // the experts in use, in order
-  int32_t n_used;
+  int32_t entry_slot[kEntries];
+  uint16_t entry_place[kEntries];  // the entry's first place
+  uint16_t entry_n[kEntries];      // and its places
+  int32_t classes[3];              // ends of the entries of 1, 2 and 4 tiles
+  uint16_t tok[kPairs];            // token of each place
+  float weight[kPairs];            // and its weight
 };
 
 // Filled by the whole workgroup; ends with a barrier.
-__device__ __forceinline__ void make_plan(const MoeArgs& a, Plan& pl) {
+template <int MAXT, int NT>
+__device__ __forceinline__ void make_plan(const MoeArgs& a, Plan<MAXT>& pl) {
+  using P = Plan<MAXT>;
+  constexpr int kOwn = (P::kPairs + NT - 1) / NT;
   const int tid = threadIdx.x;
-  for (int i = tid; i < kMaxE * (kMoeTokens / 64); i += blockDim.x) pl.takes[i / (kMoeTokens / 64)][i % (kMoeTokens / 64)] = 0;
+  const int lane = tid % kWave;
+  const int pairs = a.T * a.K;
+  // every load before the first barrier
+  int id[kOwn];
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) id[j] = tid + j * NT < pairs ? a.ids[tid + j * NT] : -1;
   if (tid < kMaxE) pl.slot[tid] = tid < a.E ? a.slot_of[tid] : -1;
+  for (int i = tid; i < kMaxE * P::kWords; i += NT) pl.takes[i / P::kWords][i % P::kWords] = 0;
   __syncthreads();
   uint32_t bad = 0;
-  for (int i = tid; i < a.T * a.K; i += blockDim.x) {
-    const int e = a.ids[i];
-    if (e < 0) continue;
-    const int s = e < a.E ? pl.slot[e] : 0;
-    if (e >= a.E || s >= a.n_slots) {
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) {
+    if (id[j] < 0) continue;
+    const int s = id[j] < a.E ? pl.slot[id[j]] : 0;
+    if (id[j] >= a.E || s >= a.n_slots) {
       bad |= FM_FLAG_INDEX_RANGE;
+      id[j] = -1;
     } else if (s < 0) {
       bad |= FM_FLAG_EXPERT_MISSING;
+      id[j] = -1;
     } else {
-      const int t = i / a.K;
-      atomicOr(reinterpret_cast<unsigned long long*>(&pl.takes[e][t / 64]), 1ull << (t % 64));
+      const int t = (tid + j * NT) / a.K;
+      atomicOr(reinterpret_cast<unsigned long long*>(&pl.takes[id[j]][t / 64]), 1ull << (t % 64));
     }
   }
   if (bad != 0 && a.flags != nullptr && blockIdx.x == 0) atomicOr(a.flags, bad);
   __syncthreads();
-  if (tid < kWave) {
-    int n = 0;
+  // each wavefront counts for itself, an expert per lane; the first writes the entries
+  int n = 0;
 #pragma unroll
-    for (int j = 0; j < kMoeTokens / 64; ++j) n += __popcll(pl.takes[tid][j]);
-    int incl = n;
+  for (int j = 0; j < P::kWords; ++j) n += __popcll(pl.takes[lane][j]);
+  auto scan = [&](int v) {   // exclusive, over the lanes
+    int incl = v;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
-      const int v = __shfl_up(incl, o, kWave);
-      if (tid >= o) incl += v;
+      const int u = __shfl_up(incl, o, kWave);
+      if (lane >= o) incl += u;
     }
-    const uint64_t in_use = __ballot(n > 0);
-    pl.count[tid] = n;
-    pl.first[tid] = incl - n;
-    if (n > 0) pl.used[__popcll(in_use & ((1ull << tid) - 1ull))] = tid;
-    if (tid == 0) pl.n_used = __popcll(in_use);
+    return incl - v;
+  };
+  const int first = scan(n);
+  if (tid < kWave) {
+    const int rest = n % 64;
+    const int in1 = rest > 0 && rest <= 16 ? 1 : 0;
+    const int in2 = rest > 16 && rest <= 32 ? 1 : 0;
+    const int in4 = n / 64 + (rest > 32 ? 1 : 0);
+    const int n1 = __popcll(__ballot(in1 != 0));
+    const int n2 = __popcll(__ballot(in2 != 0));
+    const uint64_t below = (1ull << lane) - 1ull;
+    auto put = [&](int i, int place, int count) {
+      pl.entry_slot[i] = pl.slot[lane];
+      pl.entry_place[i] = static_cast<uint16_t>(place);
+      pl.entry_n[i] = static_cast<uint16_t>(count);
+    };
+    const uint64_t m1 = __ballot(in1 != 0), m2 = __ballot(in2 != 0);
+    if (in1) put(__popcll(m1 & below), first + n - rest, rest);
+    if (in2) put(n1 + __popcll(m2 & below), first + n - rest, rest);
+    int n4 = 0;
+    if constexpr (MAXT > 32) {
+      const int p4 = scan(in4);
+      for (int j = 0; j < in4; ++j) put(n1 + n2 + p4 + j, first + 64 * j, n - 64 * j < 64 ? n - 64 * j : 64);
+      n4 = __shfl(p4 + in4, kWave - 1, kWave);
+    }
+    if (lane == 0) {
+      pl.classes[0] = n1;
+      pl.classes[1] = n1 + n2;
+      pl.classes[2] = n1 + n2 + n4;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) {
+    const int e = id[j];
+    const int base = __shfl(first, e < 0 ? 0 : e, kWave);
+    if (e < 0) continue;
+    const int t = (tid + j * NT) / a.K;
+    int p = base + __popcll(pl.takes[e][t / 64] & ((1ull << (t % 64)) - 1ull));
+    for (int q = 0; q < t / 64; ++q) p += __popcll(pl.takes[e][q]);
+    // an expert that the token lists again counts with both weights (every
+    // listing writes the same place and sum)
+    float w = 0.0f;
+    for (int k = 0; k < a.K; ++k)
+      if (a.ids[t * a.K + k] == e) w += a.weight[t * a.K + k];
+    pl.tok[p] = static_cast<uint16_t>(t);
+    pl.weight[p] = w;
   }
   __syncthreads();
 }
 
-// Place of token t among the tokens that take expert e (t takes it).
-__device__ __forceinline__ int place_of(const Plan& pl, int e, int t) {
-  int n = 0;
-  for (int j = 0; j < t / 64; ++j) n += __popcll(pl.takes[e][j]);
-  return n + __popcll(pl.takes[e][t / 64] & ((1ull << (t % 64)) - 1ull));
-}
-__device__ __forceinline__ bool takes(const Plan& pl, int e, int t) { return (pl.takes[e][t / 64] >> (t % 64)) & 1ull; }
-
 __device__ __forceinline__ uint16_t to_bf16(float f) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f)); }
+
+// Load groups of R tiles of 16 weight rows and of C tiles of 16 activation
+// columns in H planes, PA groups in flight.  Loads finish in the order of their
+// issue, so both operands of a group go out together: an activation issued after
+// the weights of later groups would wait for them.
+template <typename T, int C, int R, int H, int PA>
+struct Stream {
+  uint32x4 w[PA][R][2], b[PA][2][H][C];
+  __device__ __forceinline__ void load(int p, __amdgpu_buffer_rsrc_t rs_w, const WeightRows (&rows)[R],
+                                       __amdgpu_buffer_rsrc_t rs_b, const uint32_t (&cols)[C], uint32_t plane,
+                                       uint32_t k, uint32_t k_end) {
+    const uint32_t g16 = (threadIdx.x % kWave) / 16 * 16u;
+#pragma unroll
+    for (int r = 0; r < R; ++r) rows[r].load(rs_w, k, k_end, w[p][r]);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int q = 0; q < H; ++q)
+          b[p][s][q][j] = load_step(rs_b, cols[j] == kOutside ? kOutside : cols[j] + q * plane, k + s * kStepBytes + g16, k_end);
+  }
+  __device__ __forceinline__ void multiply(int p, floatx4 (&acc)[R][C]) const {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      uint32x4 sw[2];
+      WeightRows::steps(w[p][r], sw);
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+#pragma unroll
+          for (int q = 0; q < H; ++q) acc[r][j] = mma_step<T>(sw[s], b[p][s][q][j], acc[r][j]);
+    }
+  }
+};
+
+template <int R, int C>
+__device__ __forceinline__ void clear(floatx4 (&acc)[R][C]) {
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int j = 0; j < C; ++j) acc[r][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+}
 
 // ---------------------------------------------------------------- gate and up
 
-// One pass over a block of 16 gate and 16 up rows for up to 16 N of the
-// expert's tokens.  The wavefronts deal the load groups of a row among
+// The workgroup's units (a block of 16 gate and 16 up rows of one entry) among
+// the entries e0 .. e1 - 1, all of C tiles: every gridDim.x-th unit of the
+// concatenated entries.  The wavefronts deal the load groups of a row among
 // themselves, starting at a place that differs from block to block: rows of a
 // power of two bytes would otherwise keep all workgroups on few memory channels
-// at a time (2 GB in rows of 8 KB: 5.9 -> 7.1 TB/s).
-template <typename T, int N, int PA>
-__device__ __forceinline__ void up_pass(const MoeArgs& a, __amdgpu_buffer_rsrc_t rs_w, __amdgpu_buffer_rsrc_t rs_x,
-                                        int row0, const int32_t* tok, const float* wt, int n, int place0,
-                                        floatx4 (*red)[2][N][kWave]) {
+// at a time (2 GB in rows of 8 KB: 5.9 -> 7.1 TB/s).  The loads of a unit's first
+// groups go out before the last unit's products are done.
+template <typename T, int MAXT, int C, int PA>
+__device__ __forceinline__ void up_units(const MoeArgs& a, const Plan<MAXT>& pl, int e0, int e1,
+                                         floatx4 (*red)[2][C][kWave]) {
   const int lane = threadIdx.x % kWave;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c = lane % 16;
   const int g = lane / 16;
   const uint32_t rb = static_cast<uint32_t>(a.d) * sizeof(T);
-  const WeightRows w_gate(row0, a.f, rb, 0u, c, g);
-  const WeightRows w_up(row0, a.f, rb, static_cast<uint32_t>(a.f) * rb, c, g);
-  uint32_t ro_x[N];
-#pragma unroll
-  for (int j = 0; j < N; ++j) ro_x[j] = 16 * j + c < n ? static_cast<uint32_t>(tok[16 * j + c]) * rb : kOutside;
-  floatx4 acc[2][N];
-#pragma unroll
-  for (int j = 0; j < N; ++j) acc[0][j] = acc[1][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   const int groups = static_cast<int>((rb + kGroupBytes - 1) / kGroupBytes);
   const int mine = groups > wv ? (groups - wv + kUpWaves - 1) / kUpWaves : 0;   // groups of this wavefront
-  const int turn = static_cast<int>(static_cast<uint32_t>(row0 / kUpRows) * 37u % static_cast<uint32_t>(groups));
-  uint32x4 fw[PA][2][2], fx[2][2][N];
-  auto place = [&](int i) __attribute__((always_inline)) {   // byte of group i of this wavefront (past the row: none)
-    const int q = wv + i * kUpWaves + turn;
-    return i < mine ? static_cast<uint32_t>(q < groups ? q : q - groups) * kGroupBytes : rb;
-  };
-  auto load_w = [&](int p, uint32_t k) __attribute__((always_inline)) {
-    w_gate.load(rs_w, k, rb, fw[p][0]);
-    w_up.load(rs_w, k, rb, fw[p][1]);
-  };
-  auto load_x = [&](int p, uint32_t k) __attribute__((always_inline)) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int j = 0; j < N; ++j) fx[p][s][j] = load_step(rs_x, ro_x[j], k + s * kStepBytes + g * 16, rb);
-  };
-#pragma unroll
-  for (int p = 0; p < PA; ++p) load_w(p, place(p));
-  load_x(0, place(0));
-  for (int i = 0; i < mine; i += PA) {
-#pragma unroll
-    for (int p = 0; p < PA; ++p) {
-      load_x((p + 1) % 2, place(i + p + 1));
-      uint32x4 sg[2], su[2];
-      WeightRows::steps(fw[p][0], sg);
-      WeightRows::steps(fw[p][1], su);
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          acc[0][j] = mma_step<T>(sg[s], fx[p % 2][s][j], acc[0][j]);
-          acc[1][j] = mma_step<T>(su[s], fx[p % 2][s][j], acc[1][j]);
-        }
-      load_w(p, place(i + p + PA));
+  const int rounds = ((groups + kUpWaves - 1) / kUpWaves + PA - 1) / PA;        // of PA groups, for every wavefront
+  const int blocks = (a.f + kUpRows - 1) / kUpRows;
+  const int grid = static_cast<int>(gridDim.x);
+  const int u_end = e1 * blocks;
+  int u = e0 * blocks;
+  u += (static_cast<int>(blockIdx.x) - u % grid + grid) % grid;
+  if (u >= u_end) return;
+  const size_t slot_bytes = static_cast<size_t>(3) * a.d * a.f * sizeof(T);
+  const __amdgpu_buffer_rsrc_t rs_x = row_buffer(a.x, static_cast<uint32_t>(a.T) * rb);
+  // the unit that is being loaded
+  __amdgpu_buffer_rsrc_t rs_w = rs_x;
+  WeightRows rows[2] = {WeightRows(0, 0, rb, 0u, c, g), WeightRows(0, 0, rb, 0u, c, g)};
+  uint32_t cols[C];
+  int turn = 0;
+  uint32_t k_end = 0;
+  auto aim = [&](int v) __attribute__((always_inline)) {
+    if (v >= u_end) {
+      k_end = 0;   // nothing more to load
+      return;
     }
-  }
+    k_end = rb;
+    const int e = v / blocks;
+    const int blk = v - e * blocks;
+    rs_w = row_buffer(a.slots + __builtin_amdgcn_readfirstlane(pl.entry_slot[e]) * slot_bytes,
+                      static_cast<uint32_t>(slot_bytes));
+    rows[0] = WeightRows(blk * kUpRows, a.f, rb, 0u, c, g);
+    rows[1] = WeightRows(blk * kUpRows, a.f, rb, static_cast<uint32_t>(a.f) * rb, c, g);
+    const int n = pl.entry_n[e], p0 = pl.entry_place[e];
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    red[wv][0][j][lane] = acc[0][j];
-    red[wv][1][j][lane] = acc[1][j];
-  }
-  __syncthreads();
-  if (wv < N) {
+    for (int j = 0; j < C; ++j)
+      cols[j] = 16 * j + c < n ? static_cast<uint32_t>(pl.tok[p0 + 16 * j + c]) * rb : kOutside;
+    turn = static_cast<int>(static_cast<uint32_t>(blk) * 37u % static_cast<uint32_t>(groups));
+  };
+  Stream<T, C, 2, 1, PA> st;
+  auto load = [&](int p, int i) __attribute__((always_inline)) {   // the wavefront's i-th group
+    const int q = wv + i * kUpWaves + turn;
+    st.load(p, rs_w, rows, rs_x, cols, 0u, static_cast<uint32_t>(q < groups ? q : q - groups) * kGroupBytes,
+            i < mine ? k_end : 0u);
+  };
+  aim(u);
+#pragma unroll
+  for (int p = 0; p < PA; ++p) load(p, p);
+  for (; u < u_end; u += grid) {
+    floatx4 acc[2][C];
+    clear(acc);
+    for (int r = 0; r < rounds; ++r) {
+      const bool next = r + 1 == rounds;
+      if (next) aim(u + grid);
+#pragma unroll
+      for (int p = 0; p < PA; ++p) {
+        st.multiply(p, acc);
+        load(p, next ? p : (r + 1) * PA + p);
+      }
+    }
+    wait_lgkm0();
+    raw_barrier();   // the last unit's sums are read
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      red[wv][0][j][lane] = acc[0][j];
+      red[wv][1][j][lane] = acc[1][j];
+    }
+    wait_lgkm0();
+    raw_barrier();
+    if (wv >= C) continue;
     floatx4 gv = red[0][0][wv][lane], uv = red[0][1][wv][lane];
 #pragma unroll
     for (int w = 1; w < kUpWaves; ++w) {
@@ -185,205 +297,171 @@ __device__ __forceinline__ void up_pass(const MoeArgs& a, __amdgpu_buffer_rsrc_t
     }
     // lane 16 g + c: rows 4 g .. 4 g + 3 of column c (f is a multiple of 8, so
     // the four rows exist or none does)
+    const int e = u / blocks;
     const int col = 16 * wv + c;
-    const int row = row0 + 4 * g;
-    if (col < n && row < a.f) {
-      const float w = wt[col];
-      floatx4 hv;
+    const int row = (u - e * blocks) * kUpRows + 4 * g;
+    if (col >= pl.entry_n[e] || row >= a.f) continue;
+    const int place = pl.entry_place[e] + col;
+    const float w = pl.weight[place];
+    floatx4 hv;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) hv[r] = w * (gv[r] / (1.0f + expf(-gv[r])) * uv[r]);
-      const int64_t o = static_cast<int64_t>(place0 + col) * a.f + row;
-      if constexpr (sizeof(T) == 2) {
-        typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
-        u16x4 hi, lo;
+    for (int r = 0; r < 4; ++r) hv[r] = w * (gv[r] / (1.0f + expf(-gv[r])) * uv[r]);
+    const int64_t o = static_cast<int64_t>(place) * a.f + row;
+    if constexpr (sizeof(T) == 2) {
+      typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+      u16x4 hi, lo;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          hi[r] = to_bf16(hv[r]);
-          // an infinite h has no rest (inf - inf would make it NaN)
-          const float rest = hv[r] - bf16_to_f32(hi[r]);
-          lo[r] = __builtin_fabsf(bf16_to_f32(hi[r])) < __builtin_inff() ? to_bf16(rest) : static_cast<uint16_t>(0);
-        }
-        uint16_t* h = reinterpret_cast<uint16_t*>(a.h);
-        *reinterpret_cast<u16x4*>(h + o) = hi;
-        *reinterpret_cast<u16x4*>(h + static_cast<int64_t>(a.T) * a.K * a.f + o) = lo;
-      } else {
-        *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(a.h) + o) = hv;
+      for (int r = 0; r < 4; ++r) {
+        hi[r] = to_bf16(hv[r]);
+        // an infinite h has no rest (inf - inf would make it NaN)
+        const float rest = hv[r] - bf16_to_f32(hi[r]);
+        lo[r] = __builtin_fabsf(bf16_to_f32(hi[r])) < __builtin_inff() ? to_bf16(rest) : static_cast<uint16_t>(0);
       }
+      uint16_t* h = reinterpret_cast<uint16_t*>(a.h);
+      *reinterpret_cast<u16x4*>(h + o) = hi;
+      *reinterpret_cast<u16x4*>(h + static_cast<int64_t>(a.T) * a.K * a.f + o) = lo;
+    } else {
+      *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(a.h) + o) = hv;
     }
   }
+  wait_lgkm0();
 }
 
+// Tokens of a launch of N tiles: up to 16 N, or any number for N = 4.
+constexpr int max_tokens(int N) { return N < kMaxTiles ? 16 * N : kMoeTokens; }
+
 template <typename T, int N>
-__global__ void __launch_bounds__(kUpWaves * kWave) k_moe_up(MoeArgs a) {
-  __shared__ Plan pl;
-  __shared__ int32_t tok[kMoeTokens];
-  __shared__ float wt[kMoeTokens];
+__global__ void __launch_bounds__(kUpWaves * kWave, N == 4 ? 2 : 4) k_moe_up(MoeArgs a) {
+  constexpr int MAXT = max_tokens(N);
+  __shared__ Plan<MAXT> pl;
   __shared__ floatx4 red[kUpWaves * 2 * N * kWave];
-  const int blocks = (a.f + kUpRows - 1) / kUpRows;
   // the tickets of the launch after this one
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i < a.row_blocks; i += kUpWaves * kWave) a.ticket[i] = 0;
-  make_plan(a, pl);
-  const int i_used = static_cast<int>(blockIdx.x) / blocks;
-  if (i_used >= pl.n_used) return;
-  const int row0 = (static_cast<int>(blockIdx.x) % blocks) * kUpRows;
-  const int e = pl.used[i_used];
-  const int n = pl.count[e];
-  for (int t = threadIdx.x; t < a.T; t += kUpWaves * kWave) {
-    if (!takes(pl, e, t)) continue;
-    float w = 0.0f;
-    for (int k = 0; k < a.K; ++k)
-      if (a.ids[t * a.K + k] == e) w += a.weight[t * a.K + k];
-    const int p = place_of(pl, e, t);
-    tok[p] = t;
-    wt[p] = w;
-  }
-  __syncthreads();
-  const size_t slot_bytes = static_cast<size_t>(3) * a.d * a.f * sizeof(T);
-  const __amdgpu_buffer_rsrc_t rs_w = row_buffer(a.slots + pl.slot[e] * slot_bytes, static_cast<uint32_t>(slot_bytes));
-  const __amdgpu_buffer_rsrc_t rs_x = row_buffer(a.x, static_cast<uint32_t>(a.T) * a.d * sizeof(T));
-  auto pass = [&](auto cols, int p) __attribute__((always_inline)) {
-    constexpr int C = decltype(cols)::value;
-    up_pass<T, C, C == 1 ? 4 : 2>(a, rs_w, rs_x, row0, tok + p, wt + p, n - p, pl.first[e] + p,
-                                  reinterpret_cast<floatx4(*)[2][C][kWave]>(red));
+  make_plan<MAXT, kUpWaves * kWave>(a, pl);
+  auto run = [&](auto tiles, auto depth, int e0, int e1) __attribute__((always_inline)) {
+    constexpr int C = decltype(tiles)::value;
+    if (e0 < e1)
+      up_units<T, MAXT, C, decltype(depth)::value>(a, pl, e0, e1, reinterpret_cast<floatx4(*)[2][C][kWave]>(red));
   };
-  for (int p = 0; p < n; p += 16 * N) {
-    if (p > 0) __syncthreads();   // the last pass's sums are read
-    if (N == 1 || n - p <= 16) pass(std::integral_constant<int, 1>(), p);
-    else if (N == 2 || n - p <= 32) pass(std::integral_constant<int, N < 2 ? N : 2>(), p);
-    else pass(std::integral_constant<int, N>(), p);
-  }
+  run(std::integral_constant<int, 1>(), std::integral_constant<int, N == 4 ? 4 : 2>(), 0, pl.classes[0]);
+  if constexpr (N >= 2)
+    run(std::integral_constant<int, 2>(), std::integral_constant<int, N == 4 ? 4 : 2>(), pl.classes[0], pl.classes[1]);
+  if constexpr (N == 4) run(std::integral_constant<int, 4>(), std::integral_constant<int, 2>(), pl.classes[1], pl.classes[2]);
 }
 
 // ---------------------------------------------------------------- down
 
-// Load groups [m0, m1) of 16 R rows of one expert's Down for up to 16 N of its
-// tokens, added to the wavefront's sums own[t][16 R].
-template <typename T, int N, int R, int PA>
-__device__ __forceinline__ void down_pass(const MoeArgs& a, __amdgpu_buffer_rsrc_t rs_w, __amdgpu_buffer_rsrc_t rs_h,
-                                          int row0, int m0, int m1, const uint16_t* tok, int n, int place0, float* own) {
+// Load groups [u, u1) of the concatenated entries, those among entries e0 .. e1 - 1
+// (all of C tiles), for 16 R output rows; an entry's products are added to the
+// wavefront's sums own[t][16 R].
+template <typename T, int MAXT, int C, int R, int PA>
+__device__ __forceinline__ void down_groups(const MoeArgs& a, const Plan<MAXT>& pl, int e0, int e1, int row0, int groups,
+                                            int64_t share_u0, int64_t share_u1, float* own) {
   constexpr int H = sizeof(T) == 2 ? 2 : 1;   // planes of h
   const int lane = threadIdx.x % kWave;
   const int c = lane % 16;
   const int g = lane / 16;
   const uint32_t rb = static_cast<uint32_t>(a.f) * sizeof(T);
   const uint32_t plane = static_cast<uint32_t>(a.T) * a.K * rb;
-  uint32_t ro_h[N];
+  int u = static_cast<int>(share_u0 > static_cast<int64_t>(e0) * groups ? share_u0 : static_cast<int64_t>(e0) * groups);
+  const int u1 = static_cast<int>(share_u1 < static_cast<int64_t>(e1) * groups ? share_u1 : static_cast<int64_t>(e1) * groups);
+  if (u >= u1) return;
+  const size_t slot_elems = static_cast<size_t>(3) * a.d * a.f;
+  const uint32_t down_bytes = static_cast<uint32_t>(static_cast<size_t>(a.d) * a.f * sizeof(T));
+  const __amdgpu_buffer_rsrc_t rs_h =
+      row_buffer(a.h, static_cast<uint32_t>(static_cast<size_t>(a.T) * a.K * a.f * 4));   // two bf16 planes or one float32
+  WeightRows rows[R];
 #pragma unroll
-  for (int j = 0; j < N; ++j) ro_h[j] = 16 * j + c < n ? static_cast<uint32_t>(place0 + 16 * j + c) * rb : kOutside;
-  floatx4 acc[R][N];
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-#pragma unroll
-    for (int j = 0; j < N; ++j) acc[r][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  uint32x4 fw[PA][R][2], fh[2][2][H][N];
-  const uint32_t k_end = static_cast<uint32_t>(m1) * kGroupBytes < rb ? static_cast<uint32_t>(m1) * kGroupBytes : rb;
-  auto load_w = [&](int p, uint32_t k) __attribute__((always_inline)) {
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const WeightRows w(row0 + 16 * r, a.d, rb, 0u, c, g);
-      w.load(rs_w, k, k_end, fw[p][r]);
+  for (int r = 0; r < R; ++r) rows[r] = WeightRows(row0 + 16 * r, a.d, rb, 0u, c, g);
+  // the entry that is being loaded, and its groups from l on
+  __amdgpu_buffer_rsrc_t rs_w = rs_h;
+  uint32_t cols[C];
+  uint32_t k = 0, k_end = 0;
+  int l = u;
+  auto aim = [&]() __attribute__((always_inline)) {
+    if (l >= u1) {
+      k = k_end = 0;
+      return;
     }
+    const int e = l / groups;
+    const int m0 = l - e * groups;
+    const int m1 = groups - m0 < u1 - l ? groups : m0 + (u1 - l);
+    rs_w = row_buffer(a.slots + (__builtin_amdgcn_readfirstlane(pl.entry_slot[e]) * slot_elems +
+                                 static_cast<size_t>(2) * a.d * a.f) * sizeof(T), down_bytes);
+    const int n = pl.entry_n[e], p0 = pl.entry_place[e];
+#pragma unroll
+    for (int j = 0; j < C; ++j) cols[j] = 16 * j + c < n ? static_cast<uint32_t>(p0 + 16 * j + c) * rb : kOutside;
+    k = static_cast<uint32_t>(m0) * kGroupBytes;
+    k_end = static_cast<uint32_t>(m1) * kGroupBytes < rb ? static_cast<uint32_t>(m1) * kGroupBytes : rb;
+    l += m1 - m0;
   };
-  auto load_h = [&](int p, uint32_t k) __attribute__((always_inline)) {
+  Stream<T, C, R, H, PA> st;
+  aim();
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+  for (int p = 0; p < PA; ++p) st.load(p, rs_w, rows, rs_h, cols, plane, k + p * kGroupBytes, k_end);
+  while (u < u1) {
+    const int e = u / groups;
+    const int m0 = u - e * groups;
+    const int m = groups - m0 < u1 - u ? groups - m0 : u1 - u;   // groups of this entry
+    floatx4 acc[R][C];
+    clear(acc);
+    for (int i = 0; i < m; i += PA) {
+      k += PA * kGroupBytes;
+      if (i + PA >= m) aim();
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-#pragma unroll
-        for (int q = 0; q < H; ++q)
-          fh[p][s][q][j] = load_step(rs_h, ro_h[j] == kOutside ? kOutside : ro_h[j] + q * plane,
-                                     k + s * kStepBytes + g * 16, k_end);
-  };
-  const uint32_t k0 = static_cast<uint32_t>(m0) * kGroupBytes;
-#pragma unroll
-  for (int p = 0; p < PA; ++p) load_w(p, k0 + p * kGroupBytes);
-  load_h(0, k0);
-  for (uint32_t k = k0; k < k_end; k += PA * kGroupBytes) {
-#pragma unroll
-    for (int p = 0; p < PA; ++p) {
-      load_h((p + 1) % 2, k + (p + 1) * kGroupBytes);
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        uint32x4 sw[2];
-        WeightRows::steps(fw[p][r], sw);
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int j = 0; j < N; ++j)
-#pragma unroll
-            for (int q = 0; q < H; ++q) acc[r][j] = mma_step<T>(sw[s], fh[p % 2][s][q][j], acc[r][j]);
+      for (int p = 0; p < PA; ++p) {
+        st.multiply(p, acc);
+        st.load(p, rs_w, rows, rs_h, cols, plane, k + p * kGroupBytes, k_end);
       }
-      load_w(p, k + (p + PA) * kGroupBytes);
     }
-  }
+    const int n = pl.entry_n[e], p0 = pl.entry_place[e];
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    if (16 * j + c >= n) continue;
-    float* o = own + tok[16 * j + c] * (16 * R) + 4 * g;
+    for (int j = 0; j < C; ++j) {
+      if (16 * j + c >= n) continue;
+      float* o = own + pl.tok[p0 + 16 * j + c] * (16 * R) + 4 * g;
 #pragma unroll
-    for (int r = 0; r < R; ++r) *reinterpret_cast<floatx4*>(o + 16 * r) += acc[r][j];
+      for (int r = 0; r < R; ++r) *reinterpret_cast<floatx4*>(o + 16 * r) += acc[r][j];
+    }
+    u += m;
   }
 }
 
 // A workgroup owns 16 R output rows and, with splits, one share of the experts'
-// products for them: the load groups of all experts in use, one expert after
-// the other, are dealt to the splits and to their wavefronts as contiguous
-// ranges.  Each wavefront adds its products by token in its own LDS rows; the
-// workgroup joins them, and the last of the splits to finish joins theirs.
+// products for them: the load groups of all entries, one entry after the other,
+// are dealt to the splits and to their wavefronts as contiguous ranges.  Each
+// wavefront adds its products by token in its own LDS rows; the workgroup joins
+// them, and the last of the splits to finish joins theirs.
 template <typename T, int N, int R, int NW>
-__global__ void __launch_bounds__(NW * kWave) k_moe_down(MoeArgs a) {
-  __shared__ Plan pl;
-  __shared__ uint16_t tok[kMoeTokens * kMaxK];
+__global__ void __launch_bounds__(NW * kWave, N == 4 ? 2 : 4) k_moe_down(MoeArgs a) {
+  constexpr int MAXT = max_tokens(N);
+  __shared__ Plan<MAXT> pl;
   __shared__ int32_t is_last;
   extern __shared__ __align__(16) unsigned char smem[];   // [NW][T][16 R] float32
   float* sums = reinterpret_cast<float*>(smem);
   const int tid = threadIdx.x;
   const int lane = tid % kWave;
-  const int wv = tid / kWave;
+  const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int rbk = static_cast<int>(blockIdx.x) / a.splits;
   const int split = static_cast<int>(blockIdx.x) % a.splits;
   const int row0 = rbk * 16 * R;
   float* own = sums + static_cast<size_t>(wv) * a.T * (16 * R);
   for (int i = lane; i < a.T * 4 * R; i += kWave) reinterpret_cast<floatx4*>(own)[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-  make_plan(a, pl);
-  for (int i = tid; i < a.T * a.K; i += NW * kWave) {
-    const int e = a.ids[i];
-    const int t = i / a.K;
-    if (e >= 0 && e < a.E && takes(pl, e, t)) tok[pl.first[e] + place_of(pl, e, t)] = static_cast<uint16_t>(t);
-  }
-  __syncthreads();
+  make_plan<MAXT, NW * kWave>(a, pl);
   const int groups = (a.f * static_cast<int>(sizeof(T)) + kGroupBytes - 1) / kGroupBytes;   // load groups of a row
-  const int64_t total = static_cast<int64_t>(pl.n_used) * groups;
-  const int share = split * NW + __builtin_amdgcn_readfirstlane(wv);
+  const int64_t total = static_cast<int64_t>(pl.classes[2]) * groups;
+  const int share = split * NW + wv;
   const int shares = a.splits * NW;
-  int u = static_cast<int>(total * share / shares);
-  const int u1 = static_cast<int>(total * (share + 1) / shares);
-  const size_t slot_elems = static_cast<size_t>(3) * a.d * a.f;
-  const uint32_t down_bytes = static_cast<uint32_t>(static_cast<size_t>(a.d) * a.f * sizeof(T));
-  const uint32_t h_bytes = static_cast<uint32_t>(static_cast<size_t>(a.T) * a.K * a.f * 4);   // two bf16 planes or one float32
-  const __amdgpu_buffer_rsrc_t rs_h = row_buffer(a.h, h_bytes);
-  while (u < u1) {
-    const int i_used = u / groups;
-    const int m0 = u - i_used * groups;
-    const int m1 = groups - m0 < u1 - u ? groups : m0 + (u1 - u);
-    const int e = __builtin_amdgcn_readfirstlane(pl.used[i_used]);
-    const int n = __builtin_amdgcn_readfirstlane(pl.count[e]);
-    const int first = __builtin_amdgcn_readfirstlane(pl.first[e]);
-    const int slot = __builtin_amdgcn_readfirstlane(pl.slot[e]);
-    const __amdgpu_buffer_rsrc_t rs_w = row_buffer(
-        a.slots + (slot * slot_elems + static_cast<size_t>(2) * a.d * a.f) * sizeof(T), down_bytes);
-    auto pass = [&](auto cols, int p) __attribute__((always_inline)) {
-      constexpr int C = decltype(cols)::value;
-      down_pass<T, C, R, C * R <= 2 ? 4 : 2>(a, rs_w, rs_h, row0, m0, m1, tok + first + p, n - p, first + p, own);
-    };
-    for (int p = 0; p < n; p += 16 * N) {
-      if (N == 1 || n - p <= 16) pass(std::integral_constant<int, 1>(), p);
-      else if (N == 2 || n - p <= 32) pass(std::integral_constant<int, N < 2 ? N : 2>(), p);
-      else pass(std::integral_constant<int, N>(), p);
-    }
-    u += m1 - m0;
-  }
+  const int64_t u0 = total * share / shares;
+  const int64_t u1 = total * (share + 1) / shares;
+  auto run = [&](auto tiles, auto depth, int e0, int e1) __attribute__((always_inline)) {
+    if (e0 < e1)
+      down_groups<T, MAXT, decltype(tiles)::value, R, decltype(depth)::value>(a, pl, e0, e1, row0, groups, u0, u1, own);
+  };
+  run(std::integral_constant<int, 1>(), std::integral_constant<int, N == 4 ? 4 : R == 1 ? 3 : 2>(), 0, pl.classes[0]);
+  if constexpr (N >= 2)
+    run(std::integral_constant<int, 2>(), std::integral_constant<int, N == 4 ? 3 : 2>(), pl.classes[0], pl.classes[1]);
+  if constexpr (N == 4) run(std::integral_constant<int, 4>(), std::integral_constant<int, 2>(), pl.classes[1], pl.classes[2]);
   __syncthreads();
 
   // the wavefronts' sums, then the splits', both in order; four rows per thread
@@ -453,11 +531,15 @@ int splits_of(int32_t d, int32_t T) {
   return s < kMaxSplits ? s : kMaxSplits;
 }
 
+constexpr int kCus = 256;
+
 template <typename T, int N, int R, int NW>
 hipError_t launch(MoeArgs a, hipStream_t st) {
-  const int experts = a.E < a.T * a.K ? a.E : a.T * a.K;   // at most this many are in use
-  const unsigned up = static_cast<unsigned>(experts) * static_cast<unsigned>((a.f + kUpRows - 1) / kUpRows);
-  k_moe_up<T, N><<<up, kUpWaves * kWave, 0, st>>>(a);
+  // at most this many units; each workgroup takes its turn at them
+  const int experts = a.E + a.T * a.K / 64 < a.T * a.K ? a.E + a.T * a.K / 64 : a.T * a.K;
+  const int units = experts * ((a.f + kUpRows - 1) / kUpRows);
+  const int fill = N == 4 ? kCus : 2 * kCus;
+  k_moe_up<T, N><<<static_cast<unsigned>(units < fill ? units : fill), kUpWaves * kWave, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   auto kern = k_moe_down<T, N, R, NW>;
