@@ -355,9 +355,9 @@ __global__ void __launch_bounds__(kUpWaves * kWave, N == 4 ? 2 : 4) k_moe_up(Moe
 // Load groups [u, u1) of the concatenated entries, those among entries e0 .. e1 - 1
 // (all of C tiles), for 16 R output rows; an entry's products are added to the
 // wavefront's sums own[t][16 R].
-template <typename T, int MAXT, int C, int R, int PA>
+template <typename T, int MAXT, int C, int R, int NW, int PA>
 __device__ __forceinline__ void down_groups(const MoeArgs& a, const Plan<MAXT>& pl, int e0, int e1, int row0, int groups,
-                                            int64_t share_u0, int64_t share_u1, float* own) {
+                                            int64_t share_u0, int64_t share_u1, int wv, float* own) {
   constexpr int H = sizeof(T) == 2 ? 2 : 1;   // planes of h
   const int lane = threadIdx.x % kWave;
   const int c = lane % 16;
@@ -374,11 +374,12 @@ __device__ __forceinline__ void down_groups(const MoeArgs& a, const Plan<MAXT>& 
   WeightRows rows[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) rows[r] = WeightRows(row0 + 16 * r, a.d, rb, 0u, c, g);
-  // the entry that is being loaded, and its groups from l on
+  // the entry that is being loaded: this wavefront's groups k, k + NW, ... of it
   __amdgpu_buffer_rsrc_t rs_w = rs_h;
   uint32_t cols[C];
   uint32_t k = 0, k_end = 0;
   int l = u;
+  const int u_first = u;
   auto aim = [&]() __attribute__((always_inline)) {
     if (l >= u1) {
       k = k_end = 0;
@@ -392,27 +393,28 @@ __device__ __forceinline__ void down_groups(const MoeArgs& a, const Plan<MAXT>& 
     const int n = pl.entry_n[e], p0 = pl.entry_place[e];
 #pragma unroll
     for (int j = 0; j < C; ++j) cols[j] = 16 * j + c < n ? static_cast<uint32_t>(p0 + 16 * j + c) * rb : kOutside;
-    k = static_cast<uint32_t>(m0) * kGroupBytes;
+    // (dealt on from where the last entry's groups ended)
+    k = static_cast<uint32_t>(m0 + (wv + NW - (l - u_first) % NW) % NW) * kGroupBytes;
     k_end = static_cast<uint32_t>(m1) * kGroupBytes < rb ? static_cast<uint32_t>(m1) * kGroupBytes : rb;
     l += m1 - m0;
   };
   Stream<T, C, R, H, PA> st;
   aim();
 #pragma unroll
-  for (int p = 0; p < PA; ++p) st.load(p, rs_w, rows, rs_h, cols, plane, k + p * kGroupBytes, k_end);
+  for (int p = 0; p < PA; ++p) st.load(p, rs_w, rows, rs_h, cols, plane, k + p * NW * kGroupBytes, k_end);
   while (u < u1) {
     const int e = u / groups;
     const int m0 = u - e * groups;
     const int m = groups - m0 < u1 - u ? groups - m0 : u1 - u;   // groups of this entry
     floatx4 acc[R][C];
     clear(acc);
-    for (int i = 0; i < m; i += PA) {
-      k += PA * kGroupBytes;
-      if (i + PA >= m) aim();
+    for (int i = 0; i < m; i += PA * NW) {
+      k += PA * NW * kGroupBytes;
+      if (i + PA * NW >= m) aim();
 #pragma unroll
       for (int p = 0; p < PA; ++p) {
         st.multiply(p, acc);
-        st.load(p, rs_w, rows, rs_h, cols, plane, k + p * kGroupBytes, k_end);
+        st.load(p, rs_w, rows, rs_h, cols, plane, k + p * NW * kGroupBytes, k_end);
       }
     }
     const int n = pl.entry_n[e], p0 = pl.entry_place[e];
@@ -450,15 +452,13 @@ __global__ void __launch_bounds__(NW * kWave, N == 4 ? 2 : 4) k_moe_down(MoeArgs
   make_plan<MAXT, NW * kWave>(a, pl);
   const int groups = (a.f * static_cast<int>(sizeof(T)) + kGroupBytes - 1) / kGroupBytes;   // load groups of a row
   const int64_t total = static_cast<int64_t>(pl.classes[2]) * groups;
-  const int share = split * NW + wv;
-  const int shares = a.splits * NW;
-  const int64_t u0 = total * share / shares;
-  const int64_t u1 = total * (share + 1) / shares;
+  const int64_t u0 = total * split / a.splits;
+  const int64_t u1 = total * (split + 1) / a.splits;
   auto run = [&](auto tiles, auto depth, int e0, int e1) __attribute__((always_inline)) {
     if (e0 < e1)
-      down_groups<T, MAXT, decltype(tiles)::value, R, decltype(depth)::value>(a, pl, e0, e1, row0, groups, u0, u1, own);
+      down_groups<T, MAXT, decltype(tiles)::value, R, NW, decltype(depth)::value>(a, pl, e0, e1, row0, groups, u0, u1, wv, own);
   };
-  run(std::integral_constant<int, 1>(), std::integral_constant<int, N == 4 ? 4 : R == 1 ? 3 : 2>(), 0, pl.classes[0]);
+  run(std::integral_constant<int, 1>(), std::integral_constant<int, N == 4 ? 4 : 2>(), 0, pl.classes[0]);
   if constexpr (N >= 2)
     run(std::integral_constant<int, 2>(), std::integral_constant<int, N == 4 ? 3 : 2>(), pl.classes[0], pl.classes[1]);
   if constexpr (N == 4) run(std::integral_constant<int, 4>(), std::integral_constant<int, 2>(), pl.classes[1], pl.classes[2]);
@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(NW * kWave, N == 4 ? 2 : 4) k_moe_down(MoeArgs
 struct DownShape {
   int R, NW;
 };
-DownShape down_shape(int32_t T) { return T <= 16 ? DownShape{1, 16} : (T <= 128 ? DownShape{2, 8} : DownShape{2, 4}); }
+DownShape down_shape(int32_t T) { return T <= 128 ? DownShape{2, 8} : DownShape{2, 4}; }
 int row_blocks_of(int32_t d, int32_t T) { return (d + 16 * down_shape(T).R - 1) / (16 * down_shape(T).R); }
 int splits_of(int32_t d, int32_t T) {
   const int blocks = row_blocks_of(d, T);
@@ -555,7 +555,7 @@ hipError_t launch(MoeArgs a, hipStream_t st) {
 
 template <typename T>
 hipError_t experts(const MoeArgs& a, hipStream_t st) {   // as down_shape
-  if (a.T <= 16) return launch<T, 1, 1, 16>(a, st);
+  if (a.T <= 16) return launch<T, 1, 2, 8>(a, st);
   if (a.T <= 32) return launch<T, 2, 2, 8>(a, st);
   if (a.T <= 128) return launch<T, 4, 2, 8>(a, st);
   return launch<T, 4, 2, 4>(a, st);
