@@ -217,7 +217,7 @@ __device__ __forceinline__ void clear(floatx4 (&acc)[R][C]) {
 // groups go out before the last unit's products are done.
 template <typename T, int MAXT, int C, int PA>
 __device__ __forceinline__ void up_units(const MoeArgs& a, const Plan<MAXT>& pl, int e0, int e1,
-                                         floatx4 (*red)[2][C][kWave]) {
+                                         floatx4 (*red)[C][kWave]) {
   const int lane = threadIdx.x % kWave;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c = lane % 16;
@@ -279,22 +279,24 @@ __device__ __forceinline__ void up_units(const MoeArgs& a, const Plan<MAXT>& pl,
         load(p, next ? p : (r + 1) * PA + p);
       }
     }
-    wait_lgkm0();
-    raw_barrier();   // the last unit's sums are read
+    // the wavefronts' sums meet in LDS, gate's and then up's
+    floatx4 sum[2];
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-      red[wv][0][j][lane] = acc[0][j];
-      red[wv][1][j][lane] = acc[1][j];
+    for (int m = 0; m < 2; ++m) {
+      wait_lgkm0();
+      raw_barrier();   // the sums before are read
+#pragma unroll
+      for (int j = 0; j < C; ++j) red[wv][j][lane] = acc[m][j];
+      wait_lgkm0();
+      raw_barrier();
+      if (wv < C) {
+        sum[m] = red[0][wv][lane];
+#pragma unroll
+        for (int w = 1; w < kUpWaves; ++w) sum[m] += red[w][wv][lane];
+      }
     }
-    wait_lgkm0();
-    raw_barrier();
     if (wv >= C) continue;
-    floatx4 gv = red[0][0][wv][lane], uv = red[0][1][wv][lane];
-#pragma unroll
-    for (int w = 1; w < kUpWaves; ++w) {
-      gv += red[w][0][wv][lane];
-      uv += red[w][1][wv][lane];
-    }
+    const floatx4 gv = sum[0], uv = sum[1];
     // lane 16 g + c: rows 4 g .. 4 g + 3 of column c (f is a multiple of 8, so
     // the four rows exist or none does)
     const int e = u / blocks;
@@ -331,10 +333,10 @@ __device__ __forceinline__ void up_units(const MoeArgs& a, const Plan<MAXT>& pl,
 constexpr int max_tokens(int N) { return N < kMaxTiles ? 16 * N : kMoeTokens; }
 
 template <typename T, int N>
-__global__ void __launch_bounds__(kUpWaves * kWave, N == 4 ? 2 : 4) k_moe_up(MoeArgs a) {
+__global__ void __launch_bounds__(kUpWaves * kWave, 4) k_moe_up(MoeArgs a) {
   constexpr int MAXT = max_tokens(N);
   __shared__ Plan<MAXT> pl;
-  __shared__ floatx4 red[kUpWaves * 2 * N * kWave];
+  __shared__ floatx4 red[kUpWaves * N * kWave];
   // the tickets of the launch after this one
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i < a.row_blocks; i += kUpWaves * kWave) a.ticket[i] = 0;
@@ -342,12 +344,11 @@ __global__ void __launch_bounds__(kUpWaves * kWave, N == 4 ? 2 : 4) k_moe_up(Moe
   auto run = [&](auto tiles, auto depth, int e0, int e1) __attribute__((always_inline)) {
     constexpr int C = decltype(tiles)::value;
     if (e0 < e1)
-      up_units<T, MAXT, C, decltype(depth)::value>(a, pl, e0, e1, reinterpret_cast<floatx4(*)[2][C][kWave]>(red));
+      up_units<T, MAXT, C, decltype(depth)::value>(a, pl, e0, e1, reinterpret_cast<floatx4(*)[C][kWave]>(red));
   };
-  run(std::integral_constant<int, 1>(), std::integral_constant<int, N == 4 ? 4 : 2>(), 0, pl.classes[0]);
-  if constexpr (N >= 2)
-    run(std::integral_constant<int, 2>(), std::integral_constant<int, N == 4 ? 4 : 2>(), pl.classes[0], pl.classes[1]);
-  if constexpr (N == 4) run(std::integral_constant<int, 4>(), std::integral_constant<int, 2>(), pl.classes[1], pl.classes[2]);
+  run(std::integral_constant<int, 1>(), std::integral_constant<int, 2>(), 0, pl.classes[0]);
+  if constexpr (N >= 2) run(std::integral_constant<int, 2>(), std::integral_constant<int, 2>(), pl.classes[0], pl.classes[1]);
+  if constexpr (N == 4) run(std::integral_constant<int, 4>(), std::integral_constant<int, 1>(), pl.classes[1], pl.classes[2]);
 }
 
 // ---------------------------------------------------------------- down
@@ -538,7 +539,7 @@ hipError_t launch(MoeArgs a, hipStream_t st) {
   // at most this many units; each workgroup takes its turn at them
   const int experts = a.E + a.T * a.K / 64 < a.T * a.K ? a.E + a.T * a.K / 64 : a.T * a.K;
   const int units = experts * ((a.f + kUpRows - 1) / kUpRows);
-  const int fill = N == 4 ? kCus : 2 * kCus;
+  const int fill = 2 * kCus;
   k_moe_up<T, N><<<static_cast<unsigned>(units < fill ? units : fill), kUpWaves * kWave, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
