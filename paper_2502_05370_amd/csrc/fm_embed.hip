@@ -13,19 +13,12 @@ namespace fm {
 
 namespace {
 
-template <typename T>
-struct Vec;   // 16 bytes of a row, aligned to an element only
-template <>
-struct Vec<uint16_t> {
-  static constexpr int N = 8;
-  typedef uint16_t raw __attribute__((ext_vector_type(8)));
-  typedef raw mem __attribute__((aligned(2)));
-};
-template <>
-struct Vec<float> {
-  static constexpr int N = 4;
-  typedef float raw __attribute__((ext_vector_type(4)));
-  typedef raw mem __attribute__((aligned(4)));
+// N elements of a row, aligned to one element only; by default 16 bytes.
+template <typename T, int n = 16 / sizeof(T)>
+struct Vec {
+  static constexpr int N = n;
+  typedef T raw __attribute__((ext_vector_type(n)));
+  typedef raw mem __attribute__((aligned(sizeof(T))));
 };
 
 __device__ __forceinline__ float widen(uint16_t h) { return bf16_to_f32(h); }
@@ -38,25 +31,28 @@ __device__ __forceinline__ T narrow(float f) {
 
 // The n <= N elements of a row at p (n < N only at the end of a row), zeros past
 // them.
-template <typename T>
-__device__ __forceinline__ typename Vec<T>::raw load_part(const T* p, int n) {
-  typename Vec<T>::raw v = {};
-  if (n >= Vec<T>::N) {
-    v = *reinterpret_cast<const typename Vec<T>::mem*>(p);
+template <typename T, int N = Vec<T>::N>
+__device__ __forceinline__ typename Vec<T, N>::raw load_part(const T* p, int n) {
+  typename Vec<T, N>::raw v = {};
+  if (n >= N) {
+    v = *reinterpret_cast<const typename Vec<T, N>::mem*>(p);
   } else {
 #pragma unroll
-    for (int i = 0; i < Vec<T>::N - 1; ++i)
+    for (int i = 0; i < N - 1; ++i)
       if (i < n) v[i] = p[i];
   }
   return v;
 }
-template <typename T>
-__device__ __forceinline__ void store_part(T* p, typename Vec<T>::raw v, int n) {
-  if (n >= Vec<T>::N) {
-    *reinterpret_cast<typename Vec<T>::mem*>(p) = v;
+// STREAM: the row is not read again soon (a hint to the caches).
+template <bool STREAM, typename T, int N = Vec<T>::N>
+__device__ __forceinline__ void store_part(T* p, typename Vec<T, N>::raw v, int n) {
+  if (n >= N) {
+    typename Vec<T, N>::mem* q = reinterpret_cast<typename Vec<T, N>::mem*>(p);
+    if constexpr (STREAM) __builtin_nontemporal_store(v, q);
+    else *q = v;
   } else {
 #pragma unroll
-    for (int i = 0; i < Vec<T>::N - 1; ++i)
+    for (int i = 0; i < N - 1; ++i)
       if (i < n) p[i] = v[i];
   }
 }
@@ -99,7 +95,7 @@ __global__ void __launch_bounds__(kLookThreads) k_embed_lookup(const T* __restri
     if (c >= d) break;
 #pragma unroll
     for (int i = 0; i < N; ++i) v[u][i] = narrow<T>(widen(v[u][i]) * scale);
-    store_part(dst + c, v[u], d - c);
+    store_part<true>(dst + c, v[u], d - c);
   }
 }
 
@@ -201,7 +197,7 @@ __global__ void __launch_bounds__(NW * kWave) k_embed_pool(const T* __restrict__
     Vec<uint16_t>::raw v;
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = r[i];
-    store_part(dst, v, have);
+    store_part<false>(dst, v, have);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -230,136 +226,153 @@ void pool(const void* table, int32_t V, int32_t d, const int32_t* tokens, int32_
 
 // ---------------------------------------------------------------- gradient
 
-// A frequent token's row (more than kFrequent tokens select it) is summed by
-// whole workgroups, every other row by one wavefront.
+// Three launches: the rows' lists are cleared, the batch's tokens are listed by
+// row, and the rows are written.  A frequent token's row (more than kFrequent
+// tokens select it) is summed by whole workgroups, every other row by one
+// wavefront.
 constexpr int kFrequent = 32;
-constexpr int kGradThreads = 256;
-constexpr int kFreqThreads = 512;
+constexpr int kListTokens = 1024;   // tokens that a workgroup lists
+constexpr int kListSlots = 2048;    // slots of its table of distinct tokens
+constexpr int kRowThreads = 256;
+constexpr int kWaveRows = 8;        // rows of one wavefront
 constexpr int kFreqLanes = 32;      // lanes over the columns of a frequent row's block
 constexpr int kFreqGroups = 512;    // workgroups that share the frequent rows
-constexpr int kFreqList = 512;      // positions a wavefront lists at a time
+constexpr int kFreqList = 256;      // positions a wavefront lists at a time
+
+// What the batch holds of a row: the last token listed (-1: none) and how many.
+struct RowList {
+  int32_t head, count;
+};
 
 struct GradScratch {
-  int32_t* head;     // [V] last token listed for the row (-1: none)
-  int32_t* count;    // [V] tokens of the row
+  RowList* rows;     // [V]
   int32_t* next;     // [T] the token listed before it in its row
   int32_t* freq;     // [T / kFrequent] the frequent rows
   int32_t* n_freq;
 };
 
 size_t scratch_parts(int32_t T, int32_t V, GradScratch* s, char* base) {
-  size_t o = 0;
-  auto part = [&](size_t n, int32_t** p) {
-    if (s != nullptr) *p = reinterpret_cast<int32_t*>(base + o);
-    o += align_up(n * sizeof(int32_t), kAlign);
-  };
-  GradScratch dummy;
-  GradScratch* g = s != nullptr ? s : &dummy;
-  part(1, &g->n_freq);
-  part(static_cast<size_t>(V), &g->head);
-  part(static_cast<size_t>(V), &g->count);
-  part(static_cast<size_t>(T), &g->next);
-  part(static_cast<size_t>(T) / kFrequent + 1, &g->freq);
-  return o;
+  const size_t rows = align_up(sizeof(int32_t), kAlign);
+  const size_t next = rows + align_up(static_cast<size_t>(V) * sizeof(RowList), kAlign);
+  const size_t freq = next + align_up(static_cast<size_t>(T) * sizeof(int32_t), kAlign);
+  if (s != nullptr) {
+    s->n_freq = reinterpret_cast<int32_t*>(base);
+    s->rows = reinterpret_cast<RowList*>(base + rows);
+    s->next = reinterpret_cast<int32_t*>(base + next);
+    s->freq = reinterpret_cast<int32_t*>(base + freq);
+  }
+  return freq + align_up((static_cast<size_t>(T) / kFrequent + 1) * sizeof(int32_t), kAlign);
 }
 
 __global__ void __launch_bounds__(256) k_grad_clear(GradScratch s, int32_t V) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (i == 0) *s.n_freq = 0;
-  if (i < V) {
-    s.head[i] = -1;
-    s.count[i] = 0;
-  }
+  if (i < V) s.rows[i] = RowList{-1, 0};
 }
 
 // Each row's tokens become a list in an order that depends on timing; the sums
-// below put the positions back in order.
-__global__ void __launch_bounds__(256) k_grad_list(GradScratch s, const int32_t* __restrict__ tokens, int32_t n_tok,
-                                                   int32_t V, uint32_t* __restrict__ flags) {
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (t >= n_tok) return;
-  const int row = row_of(tokens[t], V, flags);
-  if (row < 0) return;
-  s.next[t] = atomicExch(&s.head[row], static_cast<int32_t>(t));
-  if (atomicAdd(&s.count[row], 1) == kFrequent) s.freq[atomicAdd(s.n_freq, 1)] = row;
+// below put the positions back in order.  A workgroup first lists its own tokens
+// in a table in LDS and then joins each distinct token's list to the row's: an
+// atomic per occurrence costs 18 ns on the rows of frequent tokens (65,536
+// tokens of text frequencies: 40.6 us for this launch).
+__global__ void __launch_bounds__(kListTokens) k_grad_list(GradScratch s, const int32_t* __restrict__ tokens,
+                                                           int32_t n_tok, int32_t V, uint32_t* __restrict__ flags) {
+  __shared__ int32_t key[kListSlots], head[kListSlots], tail[kListSlots], count[kListSlots];
+  const int tid = threadIdx.x;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * kListTokens + tid;
+  const int row = t < n_tok ? row_of(tokens[t], V, flags) : -1;
+  for (int i = tid; i < kListSlots; i += kListTokens) {
+    key[i] = head[i] = -1;
+    count[i] = 0;
+  }
+  __syncthreads();
+  if (row >= 0) {
+    // at most kListTokens of the slots are taken, so that a free one is met
+    uint32_t i = static_cast<uint32_t>(row) * 2654435761u >> 21;
+    for (;;) {
+      const int32_t k = atomicCAS(&key[i], -1, row);
+      if (k == -1 || k == row) break;
+      i = (i + 1) % kListSlots;
+    }
+    const int32_t before = atomicExch(&head[i], static_cast<int32_t>(t));
+    if (before < 0) tail[i] = static_cast<int32_t>(t);
+    else s.next[t] = before;
+    atomicAdd(&count[i], 1);
+  }
+  __syncthreads();
+  for (int i = tid; i < kListSlots; i += kListTokens) {
+    const int32_t r = key[i];
+    if (r < 0) continue;
+    s.next[tail[i]] = atomicExch(&s.rows[r].head, head[i]);
+    const int32_t n = atomicAdd(&s.rows[r].count, count[i]);
+    if (n <= kFrequent && n + count[i] > kFrequent) s.freq[atomicAdd(s.n_freq, 1)] = r;
+  }
 }
 
-template <typename G>
+// N sums into a row of the gradient.
+template <typename G, int N>
 __device__ __forceinline__ void put_row(G* dst, const float* acc, int n, float scale, bool accumulate, bool any) {
-  constexpr int N = Vec<G>::N;
-  typename Vec<G>::raw v = {};
-  if (accumulate) v = load_part(dst, n);
+  typename Vec<G, N>::raw v = {};
+  if (accumulate) v = load_part<G, N>(dst, n);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const float s = any ? acc[i] * scale : 0.0f;
     v[i] = narrow<G>(accumulate ? widen(v[i]) + s : s);
   }
-  store_part(dst, v, n);
+  store_part<true, G, N>(dst, v, n);
 }
 
-// acc[N of T] (one 16-byte vector of dout) into dtable, whose vectors may be
-// half or twice as long.
+struct GradArgs {
+  GradScratch s;
+  const int32_t* tokens;
+  int32_t n_tok, V, d;
+  float scale;
+  bool accumulate;
+  int freq_groups;   // workgroups of the frequent rows, before those of the others
+};
+
+// Vectors of a row: 16 bytes of the wider type.
 template <typename T, typename G>
-__device__ __forceinline__ void put_vec(G* dst, const float* acc, int n, float scale, bool accumulate, bool any) {
-  if constexpr (Vec<T>::N <= Vec<G>::N) {
-    if constexpr (Vec<T>::N == Vec<G>::N) {
-      put_row(dst, acc, n, scale, accumulate, any);
-    } else {   // float rows into a bf16 table: half a vector
-#pragma unroll
-      for (int i = 0; i < Vec<T>::N; ++i) {
-        if (i >= n) break;
-        const float s = any ? acc[i] * scale : 0.0f;
-        dst[i] = narrow<G>(accumulate ? widen(dst[i]) + s : s);
-      }
-    }
-  } else {
-    put_row(dst, acc, n, scale, accumulate, any);
-    if (n > Vec<G>::N) put_row(dst + Vec<G>::N, acc + Vec<G>::N, n - Vec<G>::N, scale, accumulate, any);
-  }
+constexpr int vec_elems() {
+  return 16 / (sizeof(T) > sizeof(G) ? sizeof(T) : sizeof(G));
 }
 
-// Rows of at most kFrequent tokens, one wavefront each: the row's positions are
+// A row of at most kFrequent tokens by one wavefront: the row's positions are
 // read off its list, put in order by rank (each lane holds one), and the rows of
-// dout added in that order.  Rows without a token are written as zeros, or left
+// dout added in that order.  A row without a token is written as zeros, or left
 // alone when accumulating.
 template <typename T, typename G>
-__device__ __forceinline__ void rare_row(const GradScratch& s, const T* __restrict__ dout, int32_t d, int64_t row,
-                                         float scale, bool accumulate, G* __restrict__ dtable, int32_t* ord) {
-  constexpr int N = Vec<T>::N;
+__device__ __forceinline__ void rare_row(const GradArgs& a, const T* __restrict__ dout, int64_t row, int head, int n,
+                                         G* __restrict__ dtable, int32_t* ord) {
+  constexpr int N = vec_elems<T, G>();
   constexpr int U = 4;
   const int lane = threadIdx.x % kWave;
-  const int n = s.count[row];
-  if (n > kFrequent || (accumulate && n == 0)) return;
-  if (n > 0) {
-    int mine = s.head[row];
-    if (n > 1) {
-      int p = mine;
-      for (int i = 1; i < n; ++i) {
-        p = s.next[p];
-        if (lane == i) mine = p;
-      }
-      int rank = 0;
-      for (int i = 0; i < n; ++i) rank += __shfl(mine, i, kWave) < mine ? 1 : 0;
-      if (lane < n) ord[rank] = mine;
-    } else if (lane == 0) {
-      ord[0] = mine;
+  if (n > 1) {
+    int mine = head;
+    int p = head;
+    for (int i = 1; i < n; ++i) {
+      p = a.s.next[p];
+      if (lane == i) mine = p;
     }
+    int rank = 0;
+    for (int i = 0; i < n; ++i) rank += __builtin_amdgcn_readlane(mine, i) < mine ? 1 : 0;
+    if (lane < n) ord[rank] = mine;
+    wait_lgkm0();
   }
-  wait_lgkm0();
-  G* dst = dtable + row * d;
-  for (int c0 = lane * N; c0 < d; c0 += U * kWave * N) {
+  G* dst = dtable + row * a.d;
+  for (int c0 = lane * N; c0 < a.d; c0 += U * kWave * N) {
     float acc[U][N];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int i = 0; i < N; ++i) acc[u][i] = 0.0f;
     for (int j = 0; j < n; ++j) {
-      const T* src = dout + static_cast<int64_t>(ord[j]) * d;
-      typename Vec<T>::raw v[U];
+      const T* src = dout + static_cast<int64_t>(n > 1 ? ord[j] : head) * a.d;
+      typename Vec<T, N>::raw v[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int c = c0 + u * kWave * N;
-        v[u] = load_part(src + c, d - c);
+        v[u] = load_part<T, N>(src + c, a.d - c);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -369,47 +382,37 @@ __device__ __forceinline__ void rare_row(const GradScratch& s, const T* __restri
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + u * kWave * N;
-      if (c < d) put_vec<T, G>(dst + c, acc[u], d - c, scale, accumulate, n > 0);
+      if (c < a.d) put_row<G, N>(dst + c, acc[u], a.d - c, a.scale, a.accumulate, n > 0);
     }
   }
 }
 
-template <typename T, typename G>
-__global__ void __launch_bounds__(kGradThreads) k_grad_rare(GradScratch s, const T* __restrict__ dout, int32_t V,
-                                                            int32_t d, float scale, bool accumulate,
-                                                            G* __restrict__ dtable) {
-  __shared__ int32_t ord[kGradThreads / kWave][kFrequent];
-  const int wv = threadIdx.x / kWave;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * (kGradThreads / kWave) + wv;
-  if (row < V) rare_row<T, G>(s, dout, d, row, scale, accumulate, dtable, ord[wv]);
-}
-
 // Frequent rows: a workgroup takes (row, block of columns) units in turn.  Its
-// wavefronts share the batch in equal ranges, list their tokens of the row in
-// order, and each lane group adds every second listed row; the groups' and
-// wavefronts' sums are joined in a fixed order.
+// wavefronts share the batch in equal ranges, list their tokens of the row in an
+// order that the tokens alone decide, and the lane groups add the listed rows in
+// turn; the groups' and wavefronts' sums are joined in a fixed order.
 template <typename T, typename G>
-__global__ void __launch_bounds__(kFreqThreads) k_grad_frequent(GradScratch s, const T* __restrict__ dout,
-                                                                const int32_t* __restrict__ tokens, int32_t n_tok,
-                                                                int32_t d, float scale, bool accumulate,
-                                                                G* __restrict__ dtable) {
-  constexpr int N = Vec<T>::N;
-  constexpr int NW = kFreqThreads / kWave;
+__device__ __forceinline__ void frequent_rows(const GradArgs& a, const T* __restrict__ dout, G* __restrict__ dtable,
+                                              int32_t (*list)[kFreqList + 4 * kWave], float* part) {
+  constexpr int N = vec_elems<T, G>();
+  constexpr int NW = kRowThreads / kWave;
   constexpr int GR = kWave / kFreqLanes;
-  constexpr int U = 8;
-  __shared__ int32_t list[NW][kFreqList + kWave];
-  __shared__ float part[NW][kFreqLanes * N + 4];
+  constexpr int U = 8;      // rows in flight per lane
+  constexpr int TB = 4;     // loads of four tokens in flight
+  constexpr int kLd = kFreqLanes * N + 4;
+  typedef int32_t int4v __attribute__((ext_vector_type(4)));
+  typedef int4v int4m __attribute__((aligned(4)));
   const int lane = threadIdx.x % kWave;
   const int wv = threadIdx.x / kWave;
-  const int n_blk = (d + kFreqLanes * N - 1) / (kFreqLanes * N);
-  const int64_t units = static_cast<int64_t>(*s.n_freq) * n_blk;
-  const int share = (n_tok + NW * kWave - 1) / (NW * kWave) * kWave;   // tokens per wavefront
-  const int first = wv * share;   // (n_tok + NW * kWave fits: the host bounds T)
-  const int last = first + share < n_tok ? first + share : n_tok;
-  for (int64_t u0 = blockIdx.x; u0 < units; u0 += gridDim.x) {
-    const int32_t row = s.freq[u0 / n_blk];
+  const int n_blk = (a.d + kFreqLanes * N - 1) / (kFreqLanes * N);
+  const int64_t units = static_cast<int64_t>(*a.s.n_freq) * n_blk;
+  const int share = (a.n_tok + NW * 4 - 1) / (NW * 4) * 4;   // tokens per wavefront
+  const int first = wv * share;
+  const int last = first + share < a.n_tok ? first + share : a.n_tok;
+  for (int64_t u0 = blockIdx.x; u0 < units; u0 += a.freq_groups) {
+    const int32_t row = a.s.freq[u0 / n_blk];
     const int col = (static_cast<int>(u0 % n_blk) * kFreqLanes + lane % kFreqLanes) * N;
-    const int have = d - col;
+    const int have = a.d - col;
     float acc[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[i] = 0.0f;
@@ -417,11 +420,11 @@ __global__ void __launch_bounds__(kFreqThreads) k_grad_frequent(GradScratch s, c
     auto drain = [&]() __attribute__((always_inline)) {
       wait_lgkm0();
       for (int i0 = lane / kFreqLanes; i0 < n; i0 += U * GR) {
-        typename Vec<T>::raw v[U];
+        typename Vec<T, N>::raw v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int i = i0 + u * GR;
-          v[u] = load_part(dout + static_cast<int64_t>(i < n ? list[wv][i] : 0) * d + col, i < n ? have : 0);
+          v[u] = load_part<T, N>(dout + static_cast<int64_t>(i < n ? list[wv][i] : 0) * a.d + col, i < n ? have : 0);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -430,13 +433,35 @@ __global__ void __launch_bounds__(kFreqThreads) k_grad_frequent(GradScratch s, c
       }
       n = 0;
     };
-    for (int t = first; t < last; t += kWave) {
-      const bool hit = t + lane < last && tokens[t + lane] == row;
-      const uint64_t m = __ballot(hit);
-      if (m == 0) continue;
-      if (hit) list[wv][n + __popcll(m & ((1ull << lane) - 1ull))] = t + lane;
-      n += __popcll(m);
-      if (n >= kFreqList) drain();
+    for (int t0 = first; t0 < last; t0 += TB * 4 * kWave) {
+      int4v tok[TB];
+#pragma unroll
+      for (int b = 0; b < TB; ++b) {
+        const int t = t0 + (b * kWave + lane) * 4;
+        if (t + 3 < last) {
+          tok[b] = *reinterpret_cast<const int4m*>(a.tokens + t);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tok[b][i] = t + i < last ? a.tokens[t + i] : -1;
+        }
+      }
+      bool any = false;
+#pragma unroll
+      for (int b = 0; b < TB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) any = any || tok[b][i] == row;
+      if (__ballot(any) == 0) continue;
+#pragma unroll
+      for (int b = 0; b < TB; ++b) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool hit = tok[b][i] == row;
+          const uint64_t m = __ballot(hit);
+          if (hit) list[wv][n + __popcll(m & ((1ull << lane) - 1ull))] = t0 + (b * kWave + lane) * 4 + i;
+          n += __popcll(m);
+        }
+        if (n >= kFreqList) drain();
+      }
     }
     drain();
 #pragma unroll
@@ -445,32 +470,56 @@ __global__ void __launch_bounds__(kFreqThreads) k_grad_frequent(GradScratch s, c
       for (int i = 0; i < N; ++i) acc[i] += __shfl_xor(acc[i], m, kWave);
     if (lane < kFreqLanes)
 #pragma unroll
-      for (int i = 0; i < N; ++i) part[wv][lane * N + i] = acc[i];
+      for (int i = 0; i < N; ++i) part[wv * kLd + lane * N + i] = acc[i];
     __syncthreads();
     if (wv == 0 && lane < kFreqLanes && have > 0) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         acc[i] = 0.0f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) acc[i] += part[w][lane * N + i];
+        for (int w = 0; w < NW; ++w) acc[i] += part[w * kLd + lane * N + i];
       }
-      put_vec<T, G>(dtable + static_cast<int64_t>(row) * d + col, acc, have, scale, accumulate, true);
+      put_row<G, N>(dtable + static_cast<int64_t>(row) * a.d + col, acc, have, a.scale, a.accumulate, true);
     }
     __syncthreads();
   }
 }
 
+// The frequent rows' workgroups come first in the grid, so that their longer
+// work overlaps the other rows' stores, which bound the dense form.
 template <typename T, typename G>
-void grad(const void* dout, const int32_t* tokens, int32_t n_tok, int32_t V, int32_t d, float scale, bool accumulate,
-          void* dtable, const GradScratch& s, uint32_t* flags, hipStream_t st) {
-  k_grad_clear<<<(static_cast<unsigned>(V) + 255) / 256, 256, 0, st>>>(s, V);
-  if (n_tok > 0) k_grad_list<<<(static_cast<unsigned>(n_tok) + 255) / 256, 256, 0, st>>>(s, tokens, n_tok, V, flags);
-  if (n_tok > kFrequent)
-    k_grad_frequent<T, G><<<kFreqGroups, kFreqThreads, 0, st>>>(s, static_cast<const T*>(dout), tokens, n_tok, d, scale,
-                                                                accumulate, static_cast<G*>(dtable));
-  constexpr int kRows = kGradThreads / kWave;
-  k_grad_rare<T, G><<<(static_cast<unsigned>(V) + kRows - 1) / kRows, kGradThreads, 0, st>>>(
-      s, static_cast<const T*>(dout), V, d, scale, accumulate, static_cast<G*>(dtable));
+__global__ void __launch_bounds__(kRowThreads) k_grad_rows(GradArgs a, const T* __restrict__ dout,
+                                                           G* __restrict__ dtable) {
+  constexpr int NW = kRowThreads / kWave;
+  __shared__ int32_t list[NW][kFreqList + 4 * kWave];
+  __shared__ float part[NW * (kFreqLanes * vec_elems<T, G>() + 4)];
+  if (static_cast<int>(blockIdx.x) < a.freq_groups) {
+    frequent_rows<T, G>(a, dout, dtable, list, part);
+    return;
+  }
+  const int lane = threadIdx.x % kWave;
+  const int wv = threadIdx.x / kWave;
+  const int64_t row0 = (static_cast<int64_t>(blockIdx.x - a.freq_groups) * NW + wv) * kWaveRows;
+  RowList mine = {-1, 0};
+  if (lane < kWaveRows && row0 + lane < a.V) mine = a.s.rows[row0 + lane];
+#pragma unroll 1
+  for (int j = 0; j < kWaveRows && row0 + j < a.V; ++j) {
+    const int n = __builtin_amdgcn_readlane(mine.count, j);
+    if (n > kFrequent || (a.accumulate && n == 0)) continue;
+    rare_row<T, G>(a, dout, row0 + j, __builtin_amdgcn_readlane(mine.head, j), n, dtable, list[wv]);
+  }
+}
+
+template <typename T, typename G>
+void grad(GradArgs a, const void* dout, void* dtable, uint32_t* flags, hipStream_t st) {
+  constexpr int kRows = kRowThreads / kWave * kWaveRows;
+  k_grad_clear<<<(static_cast<unsigned>(a.V) + 255) / 256, 256, 0, st>>>(a.s, a.V);
+  if (a.n_tok > 0)
+    k_grad_list<<<(static_cast<unsigned>(a.n_tok) + kListTokens - 1) / kListTokens, kListTokens, 0, st>>>(
+        a.s, a.tokens, a.n_tok, a.V, flags);
+  a.freq_groups = a.n_tok > kFrequent ? kFreqGroups : 0;
+  const unsigned blocks = static_cast<unsigned>(a.freq_groups) + (static_cast<unsigned>(a.V) + kRows - 1) / kRows;
+  k_grad_rows<T, G><<<blocks, kRowThreads, 0, st>>>(a, static_cast<const T*>(dout), static_cast<G*>(dtable));
 }
 
 }  // namespace
@@ -495,12 +544,18 @@ size_t embed_grad_scratch_bytes(int32_t T, int32_t V) { return scratch_parts(T, 
 hipError_t launch_embed_grad(const void* dout, fm_dtype dt, const int32_t* tokens, int32_t T, int32_t V, int32_t d,
                              float scale, bool accumulate, void* dtable, fm_dtype gdt, void* scratch, uint32_t* flags,
                              hipStream_t st) {
-  GradScratch s;
-  scratch_parts(T, V, &s, static_cast<char*>(scratch));
-  if (dt == FM_BF16 && gdt == FM_BF16) grad<uint16_t, uint16_t>(dout, tokens, T, V, d, scale, accumulate, dtable, s, flags, st);
-  else if (dt == FM_BF16) grad<uint16_t, float>(dout, tokens, T, V, d, scale, accumulate, dtable, s, flags, st);
-  else if (gdt == FM_BF16) grad<float, uint16_t>(dout, tokens, T, V, d, scale, accumulate, dtable, s, flags, st);
-  else grad<float, float>(dout, tokens, T, V, d, scale, accumulate, dtable, s, flags, st);
+  GradArgs a;
+  scratch_parts(T, V, &a.s, static_cast<char*>(scratch));
+  a.tokens = tokens;
+  a.n_tok = T;
+  a.V = V;
+  a.d = d;
+  a.scale = scale;
+  a.accumulate = accumulate;
+  if (dt == FM_BF16 && gdt == FM_BF16) grad<uint16_t, uint16_t>(a, dout, dtable, flags, st);
+  else if (dt == FM_BF16) grad<uint16_t, float>(a, dout, dtable, flags, st);
+  else if (gdt == FM_BF16) grad<float, uint16_t>(a, dout, dtable, flags, st);
+  else grad<float, float>(a, dout, dtable, flags, st);
   return hipGetLastError();
 }
 
