@@ -234,10 +234,11 @@ constexpr int kFrequent = 32;
 constexpr int kListTokens = 1024;   // tokens that a workgroup lists
 constexpr int kListSlots = 2048;    // slots of its table of distinct tokens
 constexpr int kRowThreads = 256;
-constexpr int kWaveRows = 8;        // rows of one wavefront
+constexpr int kWaveRows = 4;        // rows of one wavefront
 constexpr int kFreqLanes = 32;      // lanes over the columns of a frequent row's block
 constexpr int kFreqGroups = 512;    // workgroups that share the frequent rows
-constexpr int kFreqList = 256;      // positions a wavefront lists at a time
+constexpr int kFreqList = 256;      // positions from which a wavefront adds the rows it has listed
+constexpr int kFreqSpace = kFreqList + 1024;
 
 // What the batch holds of a row: the last token listed (-1: none) and how many.
 struct RowList {
@@ -337,52 +338,106 @@ constexpr int vec_elems() {
   return 16 / (sizeof(T) > sizeof(G) ? sizeof(T) : sizeof(G));
 }
 
-// A row of at most kFrequent tokens by one wavefront: the row's positions are
-// read off its list, put in order by rank (each lane holds one), and the rows of
-// dout added in that order.  A row without a token is written as zeros, or left
-// alone when accumulating.
+// kWaveRows rows of at most kFrequent tokens by one wavefront.  The lanes read
+// the rows' positions off their lists side by side and put them in order by
+// rank; then the rows of dout are added in that order, the first of the next row
+// on its way while this one is written.  A row without a token is written as
+// zeros, or left alone when accumulating.
 template <typename T, typename G>
-__device__ __forceinline__ void rare_row(const GradArgs& a, const T* __restrict__ dout, int64_t row, int head, int n,
-                                         G* __restrict__ dtable, int32_t* ord) {
+__device__ __forceinline__ void rare_rows(const GradArgs& a, const T* __restrict__ dout, int64_t row0,
+                                          G* __restrict__ dtable, int32_t (*ord)[kFrequent], int32_t* unordered) {
   constexpr int N = vec_elems<T, G>();
   constexpr int U = 4;
+  constexpr int kSpan = U * kWave * N;   // columns of one pass
   const int lane = threadIdx.x % kWave;
-  if (n > 1) {
-    int mine = head;
-    int p = head;
-    for (int i = 1; i < n; ++i) {
-      p = a.s.next[p];
-      if (lane == i) mine = p;
+  RowList mine = {-1, 0};
+  if (lane < kWaveRows && row0 + lane < a.V) mine = a.s.rows[row0 + lane];
+  if (mine.count > kFrequent) mine.count = -1;
+  const int longest = [&] {
+    int m = 0;
+#pragma unroll
+    for (int j = 0; j < kWaveRows; ++j) {
+      const int n = __builtin_amdgcn_readlane(mine.count, j);
+      m = n > m ? n : m;
     }
-    int rank = 0;
-    for (int i = 0; i < n; ++i) rank += __builtin_amdgcn_readlane(mine, i) < mine ? 1 : 0;
-    if (lane < n) ord[rank] = mine;
+    return m;
+  }();
+  {
+    int p = mine.head;
+    for (int i = 0; i < longest; ++i) {
+      if (i < mine.count) {
+        unordered[lane * kFrequent + i] = p;
+        if (i + 1 < mine.count) p = a.s.next[p];
+      }
+    }
     wait_lgkm0();
   }
-  G* dst = dtable + row * a.d;
-  for (int c0 = lane * N; c0 < a.d; c0 += U * kWave * N) {
-    float acc[U][N];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+  for (int j = 0; j < kWaveRows; ++j) {
+    const int n = __builtin_amdgcn_readlane(mine.count, j);
+    if (n < 1) continue;
+    const int pos = lane < n ? unordered[j * kFrequent + lane] : 0;
+    int rank = 0;
+    for (int i = 0; i < n; ++i) rank += __builtin_amdgcn_readlane(pos, i) < pos ? 1 : 0;
+    if (lane < n) ord[j][rank] = pos;
+  }
+  wait_lgkm0();
+  const int passes = (a.d + kSpan - 1) / kSpan;
+  auto fetch = [&](typename Vec<T, N>::raw (&v)[U], int j, int i, int pass) __attribute__((always_inline)) {
+    const T* src = dout + static_cast<int64_t>(ord[j][i]) * a.d;
 #pragma unroll
-      for (int i = 0; i < N; ++i) acc[u][i] = 0.0f;
-    for (int j = 0; j < n; ++j) {
-      const T* src = dout + static_cast<int64_t>(n > 1 ? ord[j] : head) * a.d;
-      typename Vec<T, N>::raw v[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * kWave * N;
-        v[u] = load_part<T, N>(src + c, a.d - c);
-      }
+    for (int u = 0; u < U; ++u) {
+      const int c = pass * kSpan + (u * kWave + lane) * N;
+      v[u] = load_part<T, N>(src + c, a.d - c);
+    }
+  };
+  // rows with tokens first, so that their loads start at once
+  for (int pass = 0; pass < passes; ++pass) {
+    typename Vec<T, N>::raw ahead[U];
+    int j = 0;
+    int n = 0;
+    auto next_row = [&](int from) __attribute__((always_inline)) {
+      for (int q = from; q < kWaveRows; ++q)
+        if (__builtin_amdgcn_readlane(mine.count, q) > 0) return q;
+      return kWaveRows;
+    };
+    j = next_row(0);
+    if (j < kWaveRows) fetch(ahead, j, 0, pass);
+    while (j < kWaveRows) {
+      n = __builtin_amdgcn_readlane(mine.count, j);
+      float acc[U][N];
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < N; ++i) acc[u][i] += widen(v[u][i]);
-    }
+        for (int i = 0; i < N; ++i) acc[u][i] = widen(ahead[u][i]);
+      for (int i = 1; i < n; ++i) {
+        typename Vec<T, N>::raw v[U];
+        fetch(v, j, i, pass);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int c = c0 + u * kWave * N;
-      if (c < a.d) put_row<G, N>(dst + c, acc[u], a.d - c, a.scale, a.accumulate, n > 0);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < N; ++e) acc[u][e] += widen(v[u][e]);
+      }
+      const int after = next_row(j + 1);
+      if (after < kWaveRows) fetch(ahead, after, 0, pass);
+      G* dst = dtable + (row0 + j) * a.d;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = pass * kSpan + (u * kWave + lane) * N;
+        if (c < a.d) put_row<G, N>(dst + c, acc[u], a.d - c, a.scale, a.accumulate, true);
+      }
+      j = after;
+    }
+    if (a.accumulate) continue;
+    for (int q = 0; q < kWaveRows && row0 + q < a.V; ++q) {
+      if (__builtin_amdgcn_readlane(mine.count, q) != 0) continue;
+      G* dst = dtable + (row0 + q) * a.d;
+      const float none[N] = {};
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = pass * kSpan + (u * kWave + lane) * N;
+        if (c < a.d) put_row<G, N>(dst + c, none, a.d - c, a.scale, false, false);
+      }
     }
   }
 }
@@ -393,7 +448,7 @@ __device__ __forceinline__ void rare_row(const GradArgs& a, const T* __restrict_
 // turn; the groups' and wavefronts' sums are joined in a fixed order.
 template <typename T, typename G>
 __device__ __forceinline__ void frequent_rows(const GradArgs& a, const T* __restrict__ dout, G* __restrict__ dtable,
-                                              int32_t (*list)[kFreqList + 4 * kWave], float* part) {
+                                              int32_t (*list)[kFreqSpace], float* part) {
   constexpr int N = vec_elems<T, G>();
   constexpr int NW = kRowThreads / kWave;
   constexpr int GR = kWave / kFreqLanes;
@@ -402,6 +457,7 @@ __device__ __forceinline__ void frequent_rows(const GradArgs& a, const T* __rest
   constexpr int kLd = kFreqLanes * N + 4;
   typedef int32_t int4v __attribute__((ext_vector_type(4)));
   typedef int4v int4m __attribute__((aligned(4)));
+  static_assert(kFreqSpace >= kFreqList + TB * 4 * kWave, "a batch of loads fits the list");
   const int lane = threadIdx.x % kWave;
   const int wv = threadIdx.x / kWave;
   const int n_blk = (a.d + kFreqLanes * N - 1) / (kFreqLanes * N);
@@ -417,8 +473,35 @@ __device__ __forceinline__ void frequent_rows(const GradArgs& a, const T* __rest
 #pragma unroll
     for (int i = 0; i < N; ++i) acc[i] = 0.0f;
     int n = 0;   // listed positions
-    auto drain = [&]() __attribute__((always_inline)) {
+#pragma unroll 1
+    for (int t0 = first; t0 < last; t0 += TB * 4 * kWave) {
+      int4v tok[TB];
+#pragma unroll
+      for (int b = 0; b < TB; ++b) {
+        const int t = t0 + (b * kWave + lane) * 4;
+        if (t + 3 < last) {
+          tok[b] = *reinterpret_cast<const int4m*>(a.tokens + t);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tok[b][i] = t + i < last ? a.tokens[t + i] : -1;
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < TB; ++b) {
+        uint64_t m[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = __ballot(tok[b][i] == row);
+        if ((m[0] | m[1] | m[2] | m[3]) == 0) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if ((m[i] >> lane) & 1ull)
+            list[wv][n + __popcll(m[i] & ((1ull << lane) - 1ull))] = t0 + (b * kWave + lane) * 4 + i;
+          n += __popcll(m[i]);
+        }
+      }
+      if (n < kFreqList && t0 + TB * 4 * kWave < last) continue;
       wait_lgkm0();
+#pragma unroll 1
       for (int i0 = lane / kFreqLanes; i0 < n; i0 += U * GR) {
         typename Vec<T, N>::raw v[U];
 #pragma unroll
@@ -432,38 +515,7 @@ __device__ __forceinline__ void frequent_rows(const GradArgs& a, const T* __rest
           for (int i = 0; i < N; ++i) acc[i] += widen(v[u][i]);
       }
       n = 0;
-    };
-    for (int t0 = first; t0 < last; t0 += TB * 4 * kWave) {
-      int4v tok[TB];
-#pragma unroll
-      for (int b = 0; b < TB; ++b) {
-        const int t = t0 + (b * kWave + lane) * 4;
-        if (t + 3 < last) {
-          tok[b] = *reinterpret_cast<const int4m*>(a.tokens + t);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) tok[b][i] = t + i < last ? a.tokens[t + i] : -1;
-        }
-      }
-      bool any = false;
-#pragma unroll
-      for (int b = 0; b < TB; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) any = any || tok[b][i] == row;
-      if (__ballot(any) == 0) continue;
-#pragma unroll
-      for (int b = 0; b < TB; ++b) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bool hit = tok[b][i] == row;
-          const uint64_t m = __ballot(hit);
-          if (hit) list[wv][n + __popcll(m & ((1ull << lane) - 1ull))] = t0 + (b * kWave + lane) * 4 + i;
-          n += __popcll(m);
-        }
-        if (n >= kFreqList) drain();
-      }
     }
-    drain();
 #pragma unroll
     for (int m = kFreqLanes; m < kWave; m <<= 1)
 #pragma unroll
@@ -486,28 +538,21 @@ __device__ __forceinline__ void frequent_rows(const GradArgs& a, const T* __rest
 }
 
 // The frequent rows' workgroups come first in the grid, so that their longer
-// work overlaps the other rows' stores, which bound the dense form.
+// work overlaps the other rows', which memory bounds.
 template <typename T, typename G>
-__global__ void __launch_bounds__(kRowThreads) k_grad_rows(GradArgs a, const T* __restrict__ dout,
-                                                           G* __restrict__ dtable) {
+__global__ void __launch_bounds__(kRowThreads, 5) k_grad_rows(GradArgs a, const T* __restrict__ dout,
+                                                              G* __restrict__ dtable) {
   constexpr int NW = kRowThreads / kWave;
-  __shared__ int32_t list[NW][kFreqList + 4 * kWave];
+  __shared__ int32_t list[NW][kFreqSpace];
   __shared__ float part[NW * (kFreqLanes * vec_elems<T, G>() + 4)];
   if (static_cast<int>(blockIdx.x) < a.freq_groups) {
     frequent_rows<T, G>(a, dout, dtable, list, part);
     return;
   }
-  const int lane = threadIdx.x % kWave;
   const int wv = threadIdx.x / kWave;
-  const int64_t row0 = (static_cast<int64_t>(blockIdx.x - a.freq_groups) * NW + wv) * kWaveRows;
-  RowList mine = {-1, 0};
-  if (lane < kWaveRows && row0 + lane < a.V) mine = a.s.rows[row0 + lane];
-#pragma unroll 1
-  for (int j = 0; j < kWaveRows && row0 + j < a.V; ++j) {
-    const int n = __builtin_amdgcn_readlane(mine.count, j);
-    if (n > kFrequent || (a.accumulate && n == 0)) continue;
-    rare_row<T, G>(a, dout, row0 + j, __builtin_amdgcn_readlane(mine.head, j), n, dtable, list[wv]);
-  }
+  static_assert(2 * kWaveRows * kFrequent <= kFreqSpace, "the rows' positions, listed and in order");
+  rare_rows<T, G>(a, dout, (static_cast<int64_t>(blockIdx.x - a.freq_groups) * NW + wv) * kWaveRows, dtable,
+                  reinterpret_cast<int32_t(*)[kFrequent]>(list[wv]), list[wv] + kWaveRows * kFrequent);
 }
 
 template <typename T, typename G>
