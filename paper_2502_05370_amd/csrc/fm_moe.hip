@@ -168,33 +168,39 @@ __device__ __forceinline__ uint16_t to_bf16(float f) { return __builtin_bit_cast
 // the weights of later groups would wait for them.
 template <typename T, int C, int R, int H, int PA>
 struct Stream {
-  uint32x4 w[PA][R][2], b[PA][2][H][C];
-  __device__ __forceinline__ void load(int p, __amdgpu_buffer_rsrc_t rs_w, const WeightRows (&rows)[R],
-                                       __amdgpu_buffer_rsrc_t rs_b, const uint32_t (&cols)[C], uint32_t plane,
+  uint32x4 w[PA][R][2], b[PA][H][C][2];
+  __device__ __forceinline__ void load(int p, __amdgpu_buffer_rsrc_t rs_w, const RowPairs (&rows)[R],
+                                       __amdgpu_buffer_rsrc_t rs_b, const RowPairs (&cols)[C], uint32_t plane,
                                        uint32_t k, uint32_t k_end) {
-    const uint32_t g16 = (threadIdx.x % kWave) / 16 * 16u;
 #pragma unroll
-    for (int r = 0; r < R; ++r) rows[r].load(rs_w, k, k_end, w[p][r]);
+    for (int r = 0; r < R; ++r) rows[r].template load<kStream>(rs_w, k, k_end, w[p][r]);
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int j = 0; j < C; ++j)
 #pragma unroll
-      for (int j = 0; j < C; ++j)
-#pragma unroll
-        for (int q = 0; q < H; ++q)
-          b[p][s][q][j] = load_step(rs_b, cols[j] == kOutside ? kOutside : cols[j] + q * plane, k + s * kStepBytes + g16, k_end);
+      for (int q = 0; q < H; ++q) {
+        RowPairs c = cols[j];
+        if (q > 0) {
+          if (c.even != kOutside) c.even += plane;
+          if (c.odd != kOutside) c.odd += plane;
+        }
+        c.template load<kKeep>(rs_b, k, k_end, b[p][q][j]);
+      }
   }
   __device__ __forceinline__ void multiply(int p, floatx4 (&acc)[R][C]) const {
+    uint32x4 sw[R][2];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      uint32x4 sw[2];
-      WeightRows::steps(w[p][r], sw);
+    for (int r = 0; r < R; ++r) RowPairs::steps(w[p][r], sw[r]);
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+    for (int j = 0; j < C; ++j)
 #pragma unroll
-        for (int j = 0; j < C; ++j)
+      for (int q = 0; q < H; ++q) {
+        uint32x4 sb[2];
+        RowPairs::steps(b[p][q][j], sb);
 #pragma unroll
-          for (int q = 0; q < H; ++q) acc[r][j] = mma_step<T>(sw[s], b[p][s][q][j], acc[r][j]);
-    }
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int r = 0; r < R; ++r) acc[r][j] = mma_step<T>(sw[r][s], sb[s], acc[r][j]);
+      }
   }
 };
 
@@ -236,8 +242,7 @@ __device__ __forceinline__ void up_units(const MoeArgs& a, const Plan<MAXT>& pl,
   const __amdgpu_buffer_rsrc_t rs_x = row_buffer(a.x, static_cast<uint32_t>(a.T) * rb);
   // the unit that is being loaded
   __amdgpu_buffer_rsrc_t rs_w = rs_x;
-  WeightRows rows[2] = {WeightRows(0, 0, rb, 0u, c, g), WeightRows(0, 0, rb, 0u, c, g)};
-  uint32_t cols[C];
+  RowPairs rows[2] = {}, cols[C] = {};
   int turn = 0;
   uint32_t k_end = 0;
   auto aim = [&](int v) __attribute__((always_inline)) {
@@ -250,12 +255,15 @@ __device__ __forceinline__ void up_units(const MoeArgs& a, const Plan<MAXT>& pl,
     const int blk = v - e * blocks;
     rs_w = row_buffer(a.slots + __builtin_amdgcn_readfirstlane(pl.entry_slot[e]) * slot_bytes,
                       static_cast<uint32_t>(slot_bytes));
-    rows[0] = WeightRows(blk * kUpRows, a.f, rb, 0u, c, g);
-    rows[1] = WeightRows(blk * kUpRows, a.f, rb, static_cast<uint32_t>(a.f) * rb, c, g);
+    rows[0] = RowPairs(blk * kUpRows, a.f, rb, 0u);
+    rows[1] = RowPairs(blk * kUpRows, a.f, rb, static_cast<uint32_t>(a.f) * rb);
     const int n = pl.entry_n[e], p0 = pl.entry_place[e];
 #pragma unroll
-    for (int j = 0; j < C; ++j)
-      cols[j] = 16 * j + c < n ? static_cast<uint32_t>(pl.tok[p0 + 16 * j + c]) * rb : kOutside;
+    for (int j = 0; j < C; ++j) {
+      const int q = 16 * j + c / 2 * 2;
+      cols[j].even = q < n ? static_cast<uint32_t>(pl.tok[p0 + q]) * rb + RowPairs::place() : kOutside;
+      cols[j].odd = q + 1 < n ? static_cast<uint32_t>(pl.tok[p0 + q + 1]) * rb + RowPairs::place() : kOutside;
+    }
     turn = static_cast<int>(static_cast<uint32_t>(blk) * 37u % static_cast<uint32_t>(groups));
   };
   Stream<T, C, 2, 1, PA> st;
@@ -372,12 +380,11 @@ __device__ __forceinline__ void down_groups(const MoeArgs& a, const Plan<MAXT>& 
   const uint32_t down_bytes = static_cast<uint32_t>(static_cast<size_t>(a.d) * a.f * sizeof(T));
   const __amdgpu_buffer_rsrc_t rs_h =
       row_buffer(a.h, static_cast<uint32_t>(static_cast<size_t>(a.T) * a.K * a.f * 4));   // two bf16 planes or one float32
-  WeightRows rows[R];
+  RowPairs rows[R], cols[C] = {};
 #pragma unroll
-  for (int r = 0; r < R; ++r) rows[r] = WeightRows(row0 + 16 * r, a.d, rb, 0u, c, g);
+  for (int r = 0; r < R; ++r) rows[r] = RowPairs(row0 + 16 * r, a.d, rb, 0u);
   // the entry that is being loaded: this wavefront's groups k, k + NW, ... of it
   __amdgpu_buffer_rsrc_t rs_w = rs_h;
-  uint32_t cols[C];
   uint32_t k = 0, k_end = 0;
   int l = u;
   const int u_first = u;
@@ -393,7 +400,7 @@ __device__ __forceinline__ void down_groups(const MoeArgs& a, const Plan<MAXT>& 
                                  static_cast<size_t>(2) * a.d * a.f) * sizeof(T), down_bytes);
     const int n = pl.entry_n[e], p0 = pl.entry_place[e];
 #pragma unroll
-    for (int j = 0; j < C; ++j) cols[j] = 16 * j + c < n ? static_cast<uint32_t>(p0 + 16 * j + c) * rb : kOutside;
+    for (int j = 0; j < C; ++j) cols[j] = RowPairs(16 * j, n, rb, static_cast<uint32_t>(p0) * rb);
     // (dealt on from where the last entry's groups ended)
     k = static_cast<uint32_t>(m0 + (wv + NW - (l - u_first) % NW) % NW) * kGroupBytes;
     k_end = static_cast<uint32_t>(m1) * kGroupBytes < rb ? static_cast<uint32_t>(m1) * kGroupBytes : rb;

@@ -22,12 +22,12 @@ __device__ __forceinline__ uint32_t logit_key(float l) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-template <typename T, int TT, int NE, int NW>
+template <typename T, int TT, int NE, int NW, int PD>
 __global__ void __launch_bounds__(NW * kWave) k_route(RouteArgs a, bool probs_bf16) {
   constexpr int kLd = NE * 16 + 1;   // (an odd row length keeps the tile's rows apart)
   __shared__ float red[NW][16 * TT][kLd];
   const int lane = threadIdx.x % kWave;
-  const int wv = threadIdx.x / kWave;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c = lane % 16;
   const int g = lane / 16;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * (16 * TT);
@@ -37,39 +37,49 @@ __global__ void __launch_bounds__(NW * kWave) k_route(RouteArgs a, bool probs_bf
   const __amdgpu_buffer_rsrc_t rs_x =
       row_buffer(static_cast<const char*>(a.x) + t0 * rb, static_cast<uint32_t>(n_tok) * rb);
   const __amdgpu_buffer_rsrc_t rs_g = row_buffer(a.gate, static_cast<uint32_t>(a.E) * rb);
+  // which of this workgroup's tokens have a request, a token per lane (loaded
+  // now, looked at after the products)
+  uint32_t live = 1;
+  if (a.active != nullptr && lane < n_tok) live = a.active[t0 + lane];
   floatx4 acc[TT][NE];
 #pragma unroll
   for (int i = 0; i < TT; ++i)
 #pragma unroll
     for (int j = 0; j < NE; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  constexpr int S = 2;    // k-steps of a load group: one 128-byte line of every row
-  constexpr int PD = 2;   // load groups in flight
-  uint32x4 fx[PD][S][TT], fg[PD][S][NE];
+  RowPairs tokens[TT], experts[NE];
+#pragma unroll
+  for (int i = 0; i < TT; ++i) tokens[i] = RowPairs(16 * i, n_tok, rb, 0u);
+#pragma unroll
+  for (int j = 0; j < NE; ++j) experts[j] = RowPairs(16 * j, a.E, rb, 0u);
+  uint32x4 fx[PD][TT][2], fg[PD][NE][2];
   auto load = [&](int p, uint32_t k) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const uint32_t kk = k + s * kStepBytes + g * 16;
+    for (int i = 0; i < TT; ++i) tokens[i].template load<kStream>(rs_x, k, rb, fx[p][i]);
 #pragma unroll
-      for (int i = 0; i < TT; ++i) fx[p][s][i] = load_step(rs_x, (16u * i + c) * rb, kk, rb);
-#pragma unroll
-      for (int j = 0; j < NE; ++j) fg[p][s][j] = load_step(rs_g, (16u * j + c) * rb, kk, rb);
-    }
+    for (int j = 0; j < NE; ++j) experts[j].template load<kKeep>(rs_g, k, rb, fg[p][j]);
   };
-  const uint32_t stride = NW * S * kStepBytes;
-  const uint32_t k0 = static_cast<uint32_t>(wv) * (S * kStepBytes);
+  // the wavefronts deal the rows' lines among themselves
+  constexpr uint32_t kStride = NW * RowPairs::kBytes;
+  const uint32_t k0 = static_cast<uint32_t>(wv) * RowPairs::kBytes;
 #pragma unroll
-  for (int p = 0; p < PD; ++p) load(p, k0 + p * stride);
-  for (uint32_t k = k0; k < rb; k += PD * stride) {
+  for (int p = 0; p < PD; ++p) load(p, k0 + p * kStride);
+  for (uint32_t k = k0; k < rb; k += PD * kStride) {
 #pragma unroll
     for (int p = 0; p < PD; ++p) {
+      uint32x4 sx[TT][2];
 #pragma unroll
-      for (int s = 0; s < S; ++s)
+      for (int i = 0; i < TT; ++i) RowPairs::steps(fx[p][i], sx[i]);
 #pragma unroll
-        for (int i = 0; i < TT; ++i)
+      for (int j = 0; j < NE; ++j) {
+        uint32x4 sg[2];
+        RowPairs::steps(fg[p][j], sg);
 #pragma unroll
-          for (int j = 0; j < NE; ++j) acc[i][j] = mma_step<T>(fx[p][s][i], fg[p][s][j], acc[i][j]);
-      load(p, k + (p + PD) * stride);
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int i = 0; i < TT; ++i) acc[i][j] = mma_step<T>(sx[i][s], sg[s], acc[i][j]);
+      }
+      load(p, k + (p + PD) * kStride);
     }
   }
   // lane 16 g + c of a tile holds tokens 4 g .. 4 g + 3 of expert c
@@ -80,6 +90,7 @@ __global__ void __launch_bounds__(NW * kWave) k_route(RouteArgs a, bool probs_bf
 #pragma unroll
       for (int r = 0; r < 4; ++r) red[wv][16 * i + 4 * g + r][16 * j + c] = acc[i][j][r];
   __syncthreads();
+  const uint64_t on_mask = __ballot(live != 0);
 
   for (int i = wv; i < n_tok; i += NW) {
     const int64_t t = t0 + i;
@@ -89,7 +100,7 @@ __global__ void __launch_bounds__(NW * kWave) k_route(RouteArgs a, bool probs_bf
 #pragma unroll
       for (int w = 0; w < NW; ++w) l += red[w][i][lane];
     }
-    const bool on = a.active == nullptr || a.active[t] != 0;
+    const bool on = (on_mask >> i) & 1ull;
     float top = expert ? l : -__builtin_inff();
 #pragma unroll
     for (int m = kWave / 2; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, kWave));
@@ -98,12 +109,14 @@ __global__ void __launch_bounds__(NW * kWave) k_route(RouteArgs a, bool probs_bf
 #pragma unroll
     for (int m = kWave / 2; m >= 1; m >>= 1) sum += __shfl_xor(sum, m, kWave);
     const float p = e / sum;
-    // place in the order by logit: the experts before this one
-    const uint32_t key = logit_key(l);
+    // place in the order by logit: the experts before this one (an equal logit
+    // comes before where its index is lower; keys stay below 2^32 - 1)
+    const uint32_t key = expert ? logit_key(l) : 0u;
     int rank = expert ? 0 : kMaxE;
-    for (int j = 0; j < a.E; ++j) {
-      const uint32_t o = __builtin_amdgcn_readlane(key, j);
-      rank += o > key || (o == key && j < lane) ? 1 : 0;
+#pragma unroll
+    for (int j = 0; j < NE * 16; ++j) {
+      const uint32_t o = __builtin_amdgcn_readlane(key, j) + (j < lane ? 1u : 0u);
+      rank += o > key && j < a.E ? 1 : 0;
     }
     const bool chosen = rank < a.K;
     float w = chosen ? p : 0.0f;
@@ -131,13 +144,15 @@ __global__ void __launch_bounds__(NW * kWave) k_route(RouteArgs a, bool probs_bf
 
 template <typename T, int NE>
 void route(const RouteArgs& a, bool probs_bf16, hipStream_t st) {
+  // Few tokens: every load of the gate in flight at once.  Many: as many
+  // wavefronts per CU on 16 tokens each, or 32 where the gate's tiles outweigh
+  // the tokens' (its lines come from the L2 once per workgroup).
+  constexpr int TT = NE == 4 ? 2 : 1;
   if (a.T <= 2048) {
-    const unsigned grid = static_cast<unsigned>((a.T + 15) / 16);
-    constexpr int NW = NE == 4 ? 8 : 16;   // (the sums of 16 wavefronts of 64 experts would not fit 64 KB)
-    k_route<T, 1, NE, NW><<<grid, NW * kWave, 0, st>>>(a, probs_bf16);
+    k_route<T, 1, NE, 16, 2><<<static_cast<unsigned>((a.T + 15) / 16), 16 * kWave, 0, st>>>(a, probs_bf16);
   } else {
-    const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.T) + 31) / 32);
-    k_route<T, 2, NE, 4><<<grid, 4 * kWave, 0, st>>>(a, probs_bf16);
+    const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.T) + 16 * TT - 1) / (16 * TT));
+    k_route<T, TT, NE, 8, NE == 1 ? 4 : 2><<<grid, 8 * kWave, 0, st>>>(a, probs_bf16);
   }
 }
 
