@@ -64,6 +64,7 @@ struct Plan {
   int32_t classes[3];              // ends of the entries of 1, 2 and 4 tiles
   uint16_t tok[kPairs];            // token of each place
   float weight[kPairs];            // and its weight
+  int32_t again;                   // some token lists an expert twice
 };
 
 // Filled by the whole workgroup; ends with a barrier.
@@ -76,8 +77,13 @@ __device__ __forceinline__ void make_plan(const MoeArgs& a, Plan<MAXT>& pl) {
   const int pairs = a.T * a.K;
   // every load before the first barrier
   int id[kOwn];
+  float wt[kOwn];
 #pragma unroll
-  for (int j = 0; j < kOwn; ++j) id[j] = tid + j * NT < pairs ? a.ids[tid + j * NT] : -1;
+  for (int j = 0; j < kOwn; ++j) {
+    id[j] = tid + j * NT < pairs ? a.ids[tid + j * NT] : -1;
+    wt[j] = tid + j * NT < pairs ? a.weight[tid + j * NT] : 0.0f;
+  }
+  if (tid == 0) pl.again = 0;
   if (tid < kMaxE) pl.slot[tid] = tid < a.E ? a.slot_of[tid] : -1;
   for (int i = tid; i < kMaxE * P::kWords; i += NT) pl.takes[i / P::kWords][i % P::kWords] = 0;
   __syncthreads();
@@ -94,7 +100,8 @@ __device__ __forceinline__ void make_plan(const MoeArgs& a, Plan<MAXT>& pl) {
       id[j] = -1;
     } else {
       const int t = (tid + j * NT) / a.K;
-      atomicOr(reinterpret_cast<unsigned long long*>(&pl.takes[id[j]][t / 64]), 1ull << (t % 64));
+      const uint64_t bit = 1ull << (t % 64);
+      if ((atomicOr(reinterpret_cast<unsigned long long*>(&pl.takes[id[j]][t / 64]), bit) & bit) != 0) pl.again = 1;
     }
   }
   if (bad != 0 && a.flags != nullptr && blockIdx.x == 0) atomicOr(a.flags, bad);
@@ -151,9 +158,12 @@ __device__ __forceinline__ void make_plan(const MoeArgs& a, Plan<MAXT>& pl) {
     for (int q = 0; q < t / 64; ++q) p += __popcll(pl.takes[e][q]);
     // an expert that the token lists again counts with both weights (every
     // listing writes the same place and sum)
-    float w = 0.0f;
-    for (int k = 0; k < a.K; ++k)
-      if (a.ids[t * a.K + k] == e) w += a.weight[t * a.K + k];
+    float w = wt[j];
+    if (pl.again != 0) {
+      w = 0.0f;
+      for (int k = 0; k < a.K; ++k)
+        if (a.ids[t * a.K + k] == e) w += a.weight[t * a.K + k];
+    }
     pl.tok[p] = static_cast<uint16_t>(t);
     pl.weight[p] = w;
   }
@@ -341,7 +351,7 @@ __device__ __forceinline__ void up_units(const MoeArgs& a, const Plan<MAXT>& pl,
 constexpr int max_tokens(int N) { return N < kMaxTiles ? 16 * N : kMoeTokens; }
 
 template <typename T, int N>
-__global__ void __launch_bounds__(kUpWaves * kWave, 4) k_moe_up(MoeArgs a) {
+__global__ void __launch_bounds__(kUpWaves * kWave, N == 1 ? 4 : 2) k_moe_up(MoeArgs a) {
   constexpr int MAXT = max_tokens(N);
   __shared__ Plan<MAXT> pl;
   __shared__ floatx4 red[kUpWaves * N * kWave];
@@ -354,9 +364,9 @@ __global__ void __launch_bounds__(kUpWaves * kWave, 4) k_moe_up(MoeArgs a) {
     if (e0 < e1)
       up_units<T, MAXT, C, decltype(depth)::value>(a, pl, e0, e1, reinterpret_cast<floatx4(*)[C][kWave]>(red));
   };
-  run(std::integral_constant<int, 1>(), std::integral_constant<int, 2>(), 0, pl.classes[0]);
-  if constexpr (N >= 2) run(std::integral_constant<int, 2>(), std::integral_constant<int, 2>(), pl.classes[0], pl.classes[1]);
-  if constexpr (N == 4) run(std::integral_constant<int, 4>(), std::integral_constant<int, 1>(), pl.classes[1], pl.classes[2]);
+  run(std::integral_constant<int, 1>(), std::integral_constant<int, N == 1 ? 2 : 4>(), 0, pl.classes[0]);
+  if constexpr (N >= 2) run(std::integral_constant<int, 2>(), std::integral_constant<int, 4>(), pl.classes[0], pl.classes[1]);
+  if constexpr (N == 4) run(std::integral_constant<int, 4>(), std::integral_constant<int, 2>(), pl.classes[1], pl.classes[2]);
 }
 
 // ---------------------------------------------------------------- down
@@ -546,7 +556,7 @@ hipError_t launch(MoeArgs a, hipStream_t st) {
   // at most this many units; each workgroup takes its turn at them
   const int experts = a.E + a.T * a.K / 64 < a.T * a.K ? a.E + a.T * a.K / 64 : a.T * a.K;
   const int units = experts * ((a.f + kUpRows - 1) / kUpRows);
-  const int fill = 2 * kCus;
+  const int fill = N == 1 ? 2 * kCus : kCus;
   k_moe_up<T, N><<<static_cast<unsigned>(units < fill ? units : fill), kUpWaves * kWave, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
