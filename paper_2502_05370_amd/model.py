@@ -9,7 +9,6 @@ stream, or to ``stream``.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 from typing import Optional, Tuple
 
@@ -18,23 +17,39 @@ import torch
 from . import _DTYPES, _TORCH, _aligned_bytes, _lib, _need, _ptr, _stream
 
 _CODE = {torch.float32: _lib.FM_F32, torch.bfloat16: _lib.FM_BF16}
-_NO_GUARD = contextlib.nullcontext()
+_LIBRARY = _lib.load()
 
 
-def _on(device: torch.device):
-    """The calls enqueue on the current device: make it the tensors'."""
+def _call(name: str, device: torch.device, stream, *args) -> None:
+    """Call the library, which enqueues on the current device, with the tensors' device current."""
     if device.type != "cuda":
         raise ValueError(f"tensors are on {device}, not on a GPU")
-    return _NO_GUARD if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    if device.index == torch.cuda.current_device():
+        status = getattr(_LIBRARY, name)(*args, _stream(stream))
+    else:
+        with torch.cuda.device(device):
+            status = getattr(_LIBRARY, name)(*args, _stream(stream))
+    if status != _lib.FM_OK:
+        _lib.check(status, name)
 
 
-def _float_rows(t, name: str, shape) -> torch.Tensor:
-    """A float32 or bfloat16 tensor; later tensors are checked against its device."""
+def _float_rows(t, name: str) -> torch.Tensor:
+    """A float32 or bfloat16 matrix; later tensors are checked against its device."""
+    if type(t) is torch.Tensor and t.dtype in _CODE and t.dim() == 2 and t.is_contiguous():
+        return t   # the usual case
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
     if t.dtype not in _CODE:
         raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
-    return _need(t, name, t.dtype, shape, t.device)
+    return _need(t, name, t.dtype, (None, None), t.device)
+
+
+def _vector(t, name: str, device: torch.device) -> int:
+    """The length of an int32 vector."""
+    if not (type(t) is torch.Tensor and t.dtype is torch.int32 and t.dim() == 1 and t.device == device
+            and t.is_contiguous()):
+        _need(t, name, torch.int32, (None,), device)
+    return t.shape[0]
 
 
 def _flags(flags, dev):
@@ -44,19 +59,16 @@ def _flags(flags, dev):
 def embed_lookup(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
                  flags: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """scale * table[tokens]: table [V][d], tokens [T] int32 (negative: padding, a row of zeros) -> [T][d]."""
-    _float_rows(table, "table", (None, None))
+    _float_rows(table, "table")
     V, d = table.shape
     dev = table.device
-    _need(tokens, "tokens", torch.int32, (None,), dev)
-    T = tokens.shape[0]
+    T = _vector(tokens, "tokens", dev)
     if out is None:
         out = torch.empty((T, d), dtype=table.dtype, device=dev)
     else:
         _need(out, "out", table.dtype, (T, d), dev)
-    fl = _flags(flags, dev)
-    with _on(dev):
-        _lib.check(_lib.load().fm_embed_lookup(table.data_ptr(), V, d, _CODE[table.dtype], tokens.data_ptr(), T, scale,
-                                               out.data_ptr(), fl, _stream(stream)), "fm_embed_lookup")
+    _call("fm_embed_lookup", dev, stream, table.data_ptr(), V, d, _CODE[table.dtype], tokens.data_ptr(), T, scale,
+          out.data_ptr(), _flags(flags, dev))
     return out
 
 
@@ -64,23 +76,19 @@ def embed_pool(table: torch.Tensor, tokens: torch.Tensor, offsets: torch.Tensor,
                out: Optional[torch.Tensor] = None, flags: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Mean embedding of each request, times scale: offsets [B + 1] int32 into tokens -> [B][d] bfloat16, the
     queries of match_semantic."""
-    _float_rows(table, "table", (None, None))
+    _float_rows(table, "table")
     V, d = table.shape
     dev = table.device
-    _need(tokens, "tokens", torch.int32, (None,), dev)
-    _need(offsets, "offsets", torch.int32, (None,), dev)
-    B = offsets.shape[0] - 1
+    T = _vector(tokens, "tokens", dev)
+    B = _vector(offsets, "offsets", dev) - 1
     if B < 0:
         raise ValueError("offsets must hold at least one element")
     if out is None:
         out = torch.empty((B, d), dtype=torch.bfloat16, device=dev)
     else:
         _need(out, "out", torch.bfloat16, (B, d), dev)
-    fl = _flags(flags, dev)
-    with _on(dev):
-        _lib.check(_lib.load().fm_embed_pool(table.data_ptr(), V, d, _CODE[table.dtype], tokens.data_ptr(),
-                                             tokens.shape[0], offsets.data_ptr(), B, scale, out.data_ptr(),
-                                             fl, _stream(stream)), "fm_embed_pool")
+    _call("fm_embed_pool", dev, stream, table.data_ptr(), V, d, _CODE[table.dtype], tokens.data_ptr(), T,
+          offsets.data_ptr(), B, scale, out.data_ptr(), _flags(flags, dev))
     return out
 
 
@@ -105,7 +113,7 @@ def embed_grad(dout: torch.Tensor, tokens: torch.Tensor, V: int, scale: float = 
                stream=None) -> torch.Tensor:
     """Gradient of embed_lookup with respect to the table: dout [T][d], tokens [T] int32 -> [V][d] of grad_dtype
     (float32 by default, or out's).  accumulate adds to the rows of ``out`` that tokens select."""
-    _float_rows(dout, "dout", (None, None))
+    _float_rows(dout, "dout")
     T, d = dout.shape
     dev = dout.device
     _need(tokens, "tokens", torch.int32, (T,), dev)
@@ -115,17 +123,14 @@ def embed_grad(dout: torch.Tensor, tokens: torch.Tensor, V: int, scale: float = 
         out = torch.empty((V, d), dtype=torch.float32 if grad_dtype is None else grad_dtype, device=dev)
     if grad_dtype is not None and out.dtype != grad_dtype:
         raise ValueError(f"out must be {grad_dtype}, got {out.dtype}")
-    _float_rows(out, "out", (V, d))
+    _float_rows(out, "out")
     _need(out, "out", out.dtype, (V, d), dev)
-    fl = _flags(flags, dev)
-    with _on(dev):
-        if scratch is None:
-            scratch = EmbedGradScratch(T, V, dev)
-        _need(scratch.buf, "scratch", torch.uint8, (scratch.nbytes,), dev)
-        _lib.check(_lib.load().fm_embed_grad(dout.data_ptr(), _CODE[dout.dtype], tokens.data_ptr(), T, V, d, scale,
-                                             1 if accumulate else 0, out.data_ptr(), _CODE[out.dtype],
-                                             scratch.buf.data_ptr(), scratch.nbytes, fl,
-                                             _stream(stream)), "fm_embed_grad")
+    if scratch is None:
+        scratch = EmbedGradScratch(T, V, dev)
+    _need(scratch.buf, "scratch", torch.uint8, (scratch.nbytes,), dev)
+    _call("fm_embed_grad", dev, stream, dout.data_ptr(), _CODE[dout.dtype], tokens.data_ptr(), T, V, d, scale,
+          1 if accumulate else 0, out.data_ptr(), _CODE[out.dtype], scratch.buf.data_ptr(), scratch.nbytes,
+          _flags(flags, dev))
     return out
 
 
@@ -136,11 +141,12 @@ def moe_route(x: torch.Tensor, gate: torch.Tensor, k: int, renorm: bool = False,
     """The gate of one MoE layer: x [T][d], gate [E][d], active [T] uint8 or None -> (probs [T][E], ids [T][k] int32,
     weight [T][k] float32, mask [T] int64 holding uint64 bits).  ``out`` may give probs as a layer's rows of a batch of
     maps or trajectory queries (q[:, layer]): its rows need not follow each other; mask may be None there."""
-    _float_rows(x, "x", (None, None))
+    _float_rows(x, "x")
     T, d = x.shape
     dev = x.device
-    _need(gate, "gate", x.dtype, (None, d), dev)
+    _float_rows(gate, "gate")
     E = gate.shape[0]
+    _need(gate, "gate", x.dtype, (E, d), dev)
     if active is not None:
         _need(active, "active", torch.uint8, (T,), dev)
     if out is None:
@@ -154,11 +160,9 @@ def moe_route(x: torch.Tensor, gate: torch.Tensor, k: int, renorm: bool = False,
     _need(weight, "out[2] (weight)", torch.float32, (T, k), dev)
     if mask is not None:
         _need(mask, "out[3] (mask)", torch.int64, (T,), dev)
-    with _on(dev):
-        _lib.check(_lib.load().fm_moe_route(x.data_ptr(), gate.data_ptr(), _CODE[x.dtype], T, d, E, k,
-                                            1 if renorm else 0, _ptr(active), probs.data_ptr(), _CODE[probs.dtype],
-                                            probs.stride(0) if T > 1 else E, ids.data_ptr(), weight.data_ptr(),
-                                            _ptr(mask), _stream(stream)), "fm_moe_route")
+    _call("fm_moe_route", dev, stream, x.data_ptr(), gate.data_ptr(), _CODE[x.dtype], T, d, E, k, 1 if renorm else 0,
+          _ptr(active), probs.data_ptr(), _CODE[probs.dtype], probs.stride(0) if T > 1 else E, ids.data_ptr(),
+          weight.data_ptr(), _ptr(mask))
     return out
 
 
@@ -238,10 +242,13 @@ def moe_experts(cache: ExpertCache, x: torch.Tensor, ids: torch.Tensor, weight: 
     """residual + the weighted products of each token's experts: x [T][d], ids [T][K] int32, weight [T][K] float32 as
     moe_route gives them -> [T][d].  Experts that the cache does not hold are left out and flagged (cache.check())."""
     dev = cache.device
-    _need(x, "x", cache.dtype, (None, cache.d), dev)
+    _float_rows(x, "x")
     T = x.shape[0]
-    _need(ids, "ids", torch.int32, (T, None), dev)
+    _need(x, "x", cache.dtype, (T, cache.d), dev)
+    if not (isinstance(ids, torch.Tensor) and ids.dim() == 2):
+        _need(ids, "ids", torch.int32, (T, None), dev)
     K = ids.shape[1]
+    _need(ids, "ids", torch.int32, (T, K), dev)
     _need(weight, "weight", torch.float32, (T, K), dev)
     if residual is not None:
         _need(residual, "residual", cache.dtype, (T, cache.d), dev)
@@ -250,8 +257,6 @@ def moe_experts(cache: ExpertCache, x: torch.Tensor, ids: torch.Tensor, weight: 
     else:
         _need(out, "out", cache.dtype, (T, cache.d), dev)
     ws = workspace if workspace is not None else cache.ensure_workspace(T, K)
-    with _on(dev):
-        _lib.check(_lib.load().fm_moe_experts(cache.desc, x.data_ptr(), ids.data_ptr(), weight.data_ptr(), T, K,
-                                              _ptr(residual), out.data_ptr(), cache.flags.data_ptr(),
-                                              ws.buf.data_ptr(), ws.nbytes, _stream(stream)), "fm_moe_experts")
+    _call("fm_moe_experts", dev, stream, cache.desc, x.data_ptr(), ids.data_ptr(), weight.data_ptr(), T, K,
+          _ptr(residual), out.data_ptr(), cache.flags.data_ptr(), ws.buf.data_ptr(), ws.nbytes)
     return out
