@@ -17,8 +17,6 @@
 // and the nearest bf16 of the rest, both multiplied, so that the only rounding
 // to bf16 that shows is the output's own.  The weights' stream bounds the
 // second product, and the extra matrix instructions hide behind it.
-#include <type_traits>
-
 #include "fm_internal.h"
 #include "fm_mma.h"
 
@@ -28,9 +26,8 @@ namespace {
 
 constexpr int kUpWaves = 8;
 constexpr int kUpRows = 16;        // rows of Gate and of Up per block
-constexpr int kMaxSplits = 16;     // workgroups that share one block of output rows
+constexpr int kDownWaves = 8;
 constexpr int kGroupBytes = 2 * kStepBytes;   // of every row in one load group
-constexpr int kMaxTiles = 4;       // tiles of 16 tokens in one pass over an expert's weights
 
 struct MoeArgs {
   const char* slots;
@@ -222,6 +219,44 @@ __device__ __forceinline__ void clear(floatx4 (&acc)[R][C]) {
     for (int j = 0; j < C; ++j) acc[r][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 }
 
+// Four rows of h of one place.
+template <typename T>
+__device__ __forceinline__ void store_h(const MoeArgs& a, int place, int row, floatx4 hv) {
+  const int64_t o = static_cast<int64_t>(place) * a.f + row;
+  if constexpr (sizeof(T) == 2) {
+    typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+    u16x4 hi, lo;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      hi[r] = to_bf16(hv[r]);
+      // an infinite h has no rest (inf - inf would make it NaN)
+      const float rest = hv[r] - bf16_to_f32(hi[r]);
+      lo[r] = __builtin_fabsf(bf16_to_f32(hi[r])) < __builtin_inff() ? to_bf16(rest) : static_cast<uint16_t>(0);
+    }
+    uint16_t* h = reinterpret_cast<uint16_t*>(a.h);
+    *reinterpret_cast<u16x4*>(h + o) = hi;
+    *reinterpret_cast<u16x4*>(h + static_cast<int64_t>(a.T) * a.K * a.f + o) = lo;
+  } else {
+    *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(a.h) + o) = hv;
+  }
+}
+
+// Four outputs: the residual and the sums.
+template <typename T>
+__device__ __forceinline__ void store_out(const MoeArgs& a, int64_t o, floatx4 v) {
+  if constexpr (sizeof(T) == 2) {
+    typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+    u16x4 q = {};
+    if (a.residual != nullptr) q = *reinterpret_cast<const u16x4*>(a.residual + o * 2);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) q[r] = to_bf16(bf16_to_f32(q[r]) + v[r]);
+    *reinterpret_cast<u16x4*>(a.out + o * 2) = q;
+  } else {
+    if (a.residual != nullptr) v = *reinterpret_cast<const floatx4*>(a.residual + o * 4) + v;
+    *reinterpret_cast<floatx4*>(a.out + o * 4) = v;
+  }
+}
+
 // ---------------------------------------------------------------- gate and up
 
 // The workgroup's units (a block of 16 gate and 16 up rows of one entry) among
@@ -326,47 +361,20 @@ __device__ __forceinline__ void up_units(const MoeArgs& a, const Plan<MAXT>& pl,
     floatx4 hv;
 #pragma unroll
     for (int r = 0; r < 4; ++r) hv[r] = w * (gv[r] / (1.0f + expf(-gv[r])) * uv[r]);
-    const int64_t o = static_cast<int64_t>(place) * a.f + row;
-    if constexpr (sizeof(T) == 2) {
-      typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
-      u16x4 hi, lo;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        hi[r] = to_bf16(hv[r]);
-        // an infinite h has no rest (inf - inf would make it NaN)
-        const float rest = hv[r] - bf16_to_f32(hi[r]);
-        lo[r] = __builtin_fabsf(bf16_to_f32(hi[r])) < __builtin_inff() ? to_bf16(rest) : static_cast<uint16_t>(0);
-      }
-      uint16_t* h = reinterpret_cast<uint16_t*>(a.h);
-      *reinterpret_cast<u16x4*>(h + o) = hi;
-      *reinterpret_cast<u16x4*>(h + static_cast<int64_t>(a.T) * a.K * a.f + o) = lo;
-    } else {
-      *reinterpret_cast<floatx4*>(reinterpret_cast<float*>(a.h) + o) = hv;
-    }
+    store_h<T>(a, place, row, hv);
   }
   wait_lgkm0();
 }
 
-// Tokens of a launch of N tiles: up to 16 N, or any number for N = 4.
-constexpr int max_tokens(int N) { return N < kMaxTiles ? 16 * N : kMoeTokens; }
-
-template <typename T, int N>
-__global__ void __launch_bounds__(kUpWaves * kWave, N == 1 ? 4 : 2) k_moe_up(MoeArgs a) {
-  constexpr int MAXT = max_tokens(N);
-  __shared__ Plan<MAXT> pl;
-  __shared__ floatx4 red[kUpWaves * N * kWave];
+template <typename T>
+__global__ void __launch_bounds__(kUpWaves * kWave, 4) k_moe_up(MoeArgs a) {
+  __shared__ Plan<16> pl;
+  __shared__ floatx4 red[kUpWaves][1][kWave];
   // the tickets of the launch after this one
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i < a.row_blocks; i += kUpWaves * kWave) a.ticket[i] = 0;
-  make_plan<MAXT, kUpWaves * kWave>(a, pl);
-  auto run = [&](auto tiles, auto depth, int e0, int e1) __attribute__((always_inline)) {
-    constexpr int C = decltype(tiles)::value;
-    if (e0 < e1)
-      up_units<T, MAXT, C, decltype(depth)::value>(a, pl, e0, e1, reinterpret_cast<floatx4(*)[C][kWave]>(red));
-  };
-  run(std::integral_constant<int, 1>(), std::integral_constant<int, N == 1 ? 2 : 4>(), 0, pl.classes[0]);
-  if constexpr (N >= 2) run(std::integral_constant<int, 2>(), std::integral_constant<int, 4>(), pl.classes[0], pl.classes[1]);
-  if constexpr (N == 4) run(std::integral_constant<int, 4>(), std::integral_constant<int, 2>(), pl.classes[1], pl.classes[2]);
+  make_plan<16, kUpWaves * kWave>(a, pl);
+  up_units<T, 16, 1, 2>(a, pl, 0, pl.classes[2], red);
 }
 
 // ---------------------------------------------------------------- down
@@ -452,12 +460,12 @@ __device__ __forceinline__ void down_groups(const MoeArgs& a, const Plan<MAXT>& 
 // are dealt to the splits and to their wavefronts as contiguous ranges.  Each
 // wavefront adds its products by token in its own LDS rows; the workgroup joins
 // them, and the last of the splits to finish joins theirs.
-template <typename T, int N, int R, int NW>
-__global__ void __launch_bounds__(NW * kWave, N == 4 ? 2 : 4) k_moe_down(MoeArgs a) {
-  constexpr int MAXT = max_tokens(N);
-  __shared__ Plan<MAXT> pl;
+template <typename T>
+__global__ void __launch_bounds__(kDownWaves * kWave, 4) k_moe_down(MoeArgs a) {
+  constexpr int R = 2, NW = kDownWaves;
+  __shared__ Plan<16> pl;
   __shared__ int32_t is_last;
-  extern __shared__ __align__(16) unsigned char smem[];   // [NW][T][16 R] float32
+  __shared__ floatx4 smem[NW * 16 * 4 * R];   // [NW][T][16 R] float32
   float* sums = reinterpret_cast<float*>(smem);
   const int tid = threadIdx.x;
   const int lane = tid % kWave;
@@ -467,19 +475,12 @@ __global__ void __launch_bounds__(NW * kWave, N == 4 ? 2 : 4) k_moe_down(MoeArgs
   const int row0 = rbk * 16 * R;
   float* own = sums + static_cast<size_t>(wv) * a.T * (16 * R);
   for (int i = lane; i < a.T * 4 * R; i += kWave) reinterpret_cast<floatx4*>(own)[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-  make_plan<MAXT, NW * kWave>(a, pl);
+  make_plan<16, NW * kWave>(a, pl);
   const int groups = (a.f * static_cast<int>(sizeof(T)) + kGroupBytes - 1) / kGroupBytes;   // load groups of a row
   const int64_t total = static_cast<int64_t>(pl.classes[2]) * groups;
   const int64_t u0 = total * split / a.splits;
   const int64_t u1 = total * (split + 1) / a.splits;
-  auto run = [&](auto tiles, auto depth, int e0, int e1) __attribute__((always_inline)) {
-    if (e0 < e1)
-      down_groups<T, MAXT, decltype(tiles)::value, R, NW, decltype(depth)::value>(a, pl, e0, e1, row0, groups, u0, u1, wv, own);
-  };
-  run(std::integral_constant<int, 1>(), std::integral_constant<int, N == 4 ? 4 : 2>(), 0, pl.classes[0]);
-  if constexpr (N >= 2)
-    run(std::integral_constant<int, 2>(), std::integral_constant<int, N == 4 ? 3 : 2>(), pl.classes[0], pl.classes[1]);
-  if constexpr (N == 4) run(std::integral_constant<int, 4>(), std::integral_constant<int, 2>(), pl.classes[1], pl.classes[2]);
+  down_groups<T, 16, 1, R, NW, 2>(a, pl, 0, pl.classes[2], row0, groups, u0, u1, wv, own);
   __syncthreads();
 
   // the wavefronts' sums, then the splits', both in order; four rows per thread
@@ -519,81 +520,385 @@ __global__ void __launch_bounds__(NW * kWave, N == 4 ? 2 : 4) k_moe_down(MoeArgs
 #pragma unroll
       for (int w = 0; w < NW; ++w) v += reinterpret_cast<floatx4*>(sums)[w * quads + i];
     }
-    const int64_t o = static_cast<int64_t>(t) * a.d + row;
-    if constexpr (sizeof(T) == 2) {
-      typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
-      u16x4 q = {};
-      if (a.residual != nullptr) q = *reinterpret_cast<const u16x4*>(a.residual + o * 2);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) q[r] = to_bf16(bf16_to_f32(q[r]) + v[r]);
-      *reinterpret_cast<u16x4*>(a.out + o * 2) = q;
-    } else {
-      if (a.residual != nullptr) v = *reinterpret_cast<const floatx4*>(a.residual + o * 4) + v;
-      *reinterpret_cast<floatx4*>(a.out + o * 4) = v;
-    }
+    store_out<T>(a, static_cast<int64_t>(t) * a.d + row, v);
   }
+}
+
+// ---------------------------------------------------------------- more tokens
+
+// From 17 tokens on a workgroup's eight wavefronts own different weight rows and
+// share the activations: with up to 64 columns those would otherwise be read from
+// the L2 as often as the weights from HBM, and a CU's loads cannot serve both
+// (64 tokens through 8 experts of 4,096 x 14,336: 543 us that way, ROWS_US this).
+// They pass through LDS a slab of SG load groups at a time, two slabs deep; the
+// weights keep going straight to registers, a slab ahead.
+constexpr int kRowWaves = 8;
+
+// One slab of the sequence that a workgroup streams.
+template <int C, int H, int R>
+struct Slab {
+  __amdgpu_buffer_rsrc_t w;
+  RowPairs rows[R];
+  uint32_t col[H][C];     // where the columns that this thread copies start
+  uint32_t k, k_end;      // bytes of the rows; zeros from k_end on
+  bool last;              // of its unit or entry
+};
+
+// next(slab) sets the slab after the one it set last (false: none left);
+// done(acc) takes the sums after a slab that is the last.  Called by the whole
+// workgroup; buf holds two slabs of columns.
+template <typename T, int C, int H, int R, int SG, typename Next, typename Done>
+__device__ __forceinline__ void stream_slabs(__amdgpu_buffer_rsrc_t rs_b, unsigned char* buf, Next next, Done done) {
+  constexpr int kChunks = SG * 8;                       // 16-byte pieces of a column in a slab
+  constexpr int kCol = SG * RowPairs::kBytes + 16;      // (the odd piece keeps the columns' banks apart)
+  constexpr int kSlab = H * C * 16 * kCol;
+  static_assert(kRowWaves * kWave == 16 * kChunks || kRowWaves * kWave == 32 * kChunks, "threads per column piece");
+  constexpr int kCols = kRowWaves * kWave / kChunks;    // columns per pass of the threads
+  constexpr int NB = H * C * 16 / kCols;                // pieces of each thread
+  const int tid = threadIdx.x;
+  const int lane = tid % kWave;
+  const int c = lane % 16;
+  const int g = lane / 16;
+  uint32x4 piece[NB];
+  uint32x4 fw[SG][R][2];
+  floatx4 acc[R][C];
+  Slab<C, H, R> cur, nx;
+  auto load_b = [&](const Slab<C, H, R>& s) __attribute__((always_inline)) {
+    const uint32_t at = static_cast<uint32_t>(tid % kChunks) * 16u;
+    const bool in = s.k + at < s.k_end;
+    const int ks = static_cast<int>(s.k < s.k_end ? s.k : 0u);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const uint32_t col = s.col[i / (NB / H)][i % (NB / H)];
+      piece[i] = __builtin_amdgcn_raw_buffer_load_b128(
+          rs_b, static_cast<int>(in && col != kOutside ? col + at : kOutside), ks, kKeep);
+    }
+  };
+  auto store_b = [&](unsigned char* to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+      *reinterpret_cast<uint32x4*>(to + (i * kCols + tid / kChunks) * kCol + tid % kChunks * 16) = piece[i];
+  };
+  auto load_w = [&](const Slab<C, H, R>& s, int p) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) s.rows[r].template load<kStream>(s.w, s.k + p * RowPairs::kBytes, s.k_end, fw[p][r]);
+  };
+  raw_barrier();   // the buffers are free
+  if (!next(cur)) return;
+  nx = cur;        // (its buffer stands also where nothing comes next)
+  load_b(cur);
+#pragma unroll
+  for (int p = 0; p < SG; ++p) load_w(cur, p);
+  store_b(buf);
+  wait_lgkm0();
+  raw_barrier();
+  clear(acc);
+  for (int turn = 0;; turn ^= 1) {
+    const bool more = next(nx);
+    if (!more) nx.k = nx.k_end = 0;
+    load_b(nx);
+    const unsigned char* from = buf + turn * kSlab;
+#pragma unroll
+    for (int p = 0; p < SG; ++p) {
+      uint32x4 sw[R][2];
+#pragma unroll
+      for (int r = 0; r < R; ++r) RowPairs::steps(fw[p][r], sw[r]);
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int q = 0; q < H; ++q)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            const uint32x4 b = *reinterpret_cast<const uint32x4*>(
+                from + (q * C * 16 + 16 * j + c) * kCol + p * RowPairs::kBytes + 32 * g + 16 * s);
+#pragma unroll
+            for (int r = 0; r < R; ++r) acc[r][j] = mma_step<T>(sw[r][s], b, acc[r][j]);
+          }
+      load_w(nx, p);
+    }
+    if (cur.last) {
+      done(acc);
+      clear(acc);
+    }
+    if (!more) break;
+    store_b(buf + (turn ^ 1) * kSlab);
+    wait_lgkm0();
+    raw_barrier();
+    cur = nx;
+  }
+}
+
+// This thread's columns of an entry: `row(place)` is the byte offset of a place's
+// activations; places past the entry's are kOutside.
+template <int SG, int C, int H, typename Row>
+__device__ __forceinline__ void aim_columns(uint32_t (&col)[H][C], int n, int p0, uint32_t plane, Row row) {
+  constexpr int kCols = kRowWaves * kWave / (SG * 8);
+  constexpr int kPer = C * 16 / kCols;   // of each plane
+  static_assert(kPer <= C, "a thread's columns");
+#pragma unroll
+  for (int q = 0; q < H; ++q)
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int j = i * kCols + static_cast<int>(threadIdx.x) / (SG * 8);
+      col[q][i] = i < kPer && j < n ? row(p0 + j) + q * plane : kOutside;
+    }
+}
+
+// Units of 128 gate and 128 up rows of one entry, 16 and 16 per wavefront.
+template <typename T, int C, int SG>
+__device__ __forceinline__ void up_rows(const MoeArgs& a, const Plan<kMoeTokens>& pl, int e0, int e1, unsigned char* buf) {
+  constexpr int kRows = 16 * kRowWaves;
+  const int lane = threadIdx.x % kWave;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const uint32_t rb = static_cast<uint32_t>(a.d) * sizeof(T);
+  const int blocks = (a.f + kRows - 1) / kRows;
+  const int slabs = static_cast<int>((rb + SG * RowPairs::kBytes - 1) / (SG * RowPairs::kBytes));
+  const int grid = static_cast<int>(gridDim.x);
+  const int u_end = e1 * blocks;
+  int u = e0 * blocks;
+  u += (static_cast<int>(blockIdx.x) - u % grid + grid) % grid;
+  const size_t slot_bytes = static_cast<size_t>(3) * a.d * a.f * sizeof(T);
+  int at = u;      // the unit of the slab set last,
+  int i = -1;      // and that slab among the unit's
+  int turn = 0;    // (rows of a power of two bytes: blocks start at different places)
+  int unit = u;    // of the sums
+  auto next = [&](Slab<C, 1, 2>& s) __attribute__((always_inline)) {
+    if (++i == slabs) {
+      i = 0;
+      at += grid;
+    }
+    if (at >= u_end) return false;
+    const int e = at / blocks;
+    const int blk = at - e * blocks;
+    s.w = row_buffer(a.slots + __builtin_amdgcn_readfirstlane(pl.entry_slot[e]) * slot_bytes,
+                     static_cast<uint32_t>(slot_bytes));
+    s.rows[0] = RowPairs(blk * kRows + 16 * wv, a.f, rb, 0u);
+    s.rows[1] = RowPairs(blk * kRows + 16 * wv, a.f, rb, static_cast<uint32_t>(a.f) * rb);
+    aim_columns<SG>(s.col, pl.entry_n[e], pl.entry_place[e], 0u,
+                    [&](int p) { return static_cast<uint32_t>(pl.tok[p]) * rb; });
+    turn = static_cast<int>(static_cast<uint32_t>(blk) * 5u % static_cast<uint32_t>(slabs));
+    const int q = i + turn < slabs ? i + turn : i + turn - slabs;
+    s.k = static_cast<uint32_t>(q) * (SG * RowPairs::kBytes);
+    s.k_end = rb;
+    s.last = i + 1 == slabs;
+    return true;
+  };
+  auto done = [&](floatx4 (&acc)[2][C]) __attribute__((always_inline)) {
+    const int e = unit / blocks;
+    const int row = (unit - e * blocks) * kRows + 16 * wv + 4 * (lane / 16);
+    unit += grid;
+    if (row >= a.f) return;   // (f is a multiple of 8: four rows exist or none does)
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int col = 16 * j + lane % 16;
+      if (col >= pl.entry_n[e]) continue;
+      const int place = pl.entry_place[e] + col;
+      const float w = pl.weight[place];
+      floatx4 hv;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float gv = acc[0][j][r];
+        hv[r] = w * (gv / (1.0f + expf(-gv)) * acc[1][j][r]);
+      }
+      store_h<T>(a, place, row, hv);
+    }
+  };
+  stream_slabs<T, C, 1, 2, SG>(row_buffer(a.x, static_cast<uint32_t>(a.T) * rb), buf, next, done);
+}
+
+constexpr int slab_bytes(int C, int H, int SG) { return 2 * H * C * 16 * (SG * 128 + 16); }
+
+template <typename T>
+__global__ void __launch_bounds__(kRowWaves * kWave, 4) k_moe_up_rows(MoeArgs a) {
+  __shared__ Plan<kMoeTokens> pl;
+  __shared__ __align__(16) unsigned char buf[slab_bytes(4, 1, 2) > slab_bytes(2, 1, 4) ? slab_bytes(4, 1, 2) : slab_bytes(2, 1, 4)];
+  make_plan<kMoeTokens, kRowWaves * kWave>(a, pl);
+  up_rows<T, 1, 4>(a, pl, 0, pl.classes[0], buf);
+  up_rows<T, 2, 4>(a, pl, pl.classes[0], pl.classes[1], buf);
+  up_rows<T, 4, 2>(a, pl, pl.classes[1], pl.classes[2], buf);
+}
+
+// Load groups [u, u1) of the concatenated entries, those among entries e0 .. e1 - 1
+// (all of C tiles), for the workgroup's 128 R output rows, added to sums[t][128 R].
+template <typename T, int C, int R, int SG>
+__device__ __forceinline__ void down_rows(const MoeArgs& a, const Plan<kMoeTokens>& pl, int e0, int e1, int row0,
+                                          int groups, int64_t share_u0, int64_t share_u1, float* sums,
+                                          unsigned char* buf) {
+  constexpr int H = sizeof(T) == 2 ? 2 : 1;   // planes of h
+  constexpr int kRows = 16 * R * kRowWaves;
+  const int lane = threadIdx.x % kWave;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const uint32_t rb = static_cast<uint32_t>(a.f) * sizeof(T);
+  const uint32_t plane = static_cast<uint32_t>(a.T) * a.K * rb;
+  const int64_t lo = static_cast<int64_t>(e0) * groups, hi = static_cast<int64_t>(e1) * groups;
+  int u = static_cast<int>(share_u0 > lo ? share_u0 : lo);
+  const int u1 = static_cast<int>(share_u1 < hi ? share_u1 : hi);
+  const size_t slot_elems = static_cast<size_t>(3) * a.d * a.f;
+  const uint32_t down_bytes = static_cast<uint32_t>(static_cast<size_t>(a.d) * a.f * sizeof(T));
+  RowPairs rows[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) rows[r] = RowPairs(row0 + 16 * (wv * R + r), a.d, rb, 0u);
+  int at = u;          // first group of the next slab
+  int entry = u / groups;   // of the sums
+  auto next = [&](Slab<C, H, R>& s) __attribute__((always_inline)) {
+    if (at >= u1) return false;
+    const int e = at / groups;
+    const int m0 = at - e * groups;
+    const int end = (e + 1) * groups < u1 ? (e + 1) * groups : u1;   // of the entry's groups
+    s.w = row_buffer(a.slots + (__builtin_amdgcn_readfirstlane(pl.entry_slot[e]) * slot_elems +
+                                static_cast<size_t>(2) * a.d * a.f) * sizeof(T), down_bytes);
+#pragma unroll
+    for (int r = 0; r < R; ++r) s.rows[r] = rows[r];
+    aim_columns<SG>(s.col, pl.entry_n[e], pl.entry_place[e], plane,
+                    [&](int p) { return static_cast<uint32_t>(p) * rb; });
+    s.k = static_cast<uint32_t>(m0) * RowPairs::kBytes;
+    const uint32_t k_end = static_cast<uint32_t>(m0 + end - at) * RowPairs::kBytes;
+    s.k_end = k_end < rb ? k_end : rb;
+    at = at + SG < end ? at + SG : end;
+    s.last = at == end;
+    return true;
+  };
+  auto done = [&](floatx4 (&acc)[R][C]) __attribute__((always_inline)) {
+    const int n = pl.entry_n[entry], p0 = pl.entry_place[entry];
+    ++entry;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int col = 16 * j + lane % 16;
+      if (col >= n) continue;
+      float* o = sums + pl.tok[p0 + col] * kRows + 16 * R * wv + 4 * (lane / 16);
+#pragma unroll
+      for (int r = 0; r < R; ++r) *reinterpret_cast<floatx4*>(o + 16 * r) += acc[r][j];
+    }
+  };
+  const uint32_t h_bytes = static_cast<uint32_t>(static_cast<size_t>(a.T) * a.K * a.f * 4);
+  stream_slabs<T, C, H, R, SG>(row_buffer(a.h, h_bytes), buf, next, done);
+}
+
+// A workgroup owns 128 R output rows and one of the splits' shares of the load
+// groups of all entries; its sums by token go to the split's partial sums.
+template <typename T, int R>
+__global__ void __launch_bounds__(kRowWaves * kWave, 2) k_moe_down_rows(MoeArgs a) {
+  constexpr int H = sizeof(T) == 2 ? 2 : 1;
+  constexpr int kRows = 16 * R * kRowWaves;
+  constexpr int S2 = slab_bytes(2, H, 4), S4 = slab_bytes(4, H, 2);
+  __shared__ Plan<kMoeTokens> pl;
+  __shared__ __align__(16) unsigned char buf[S2 > S4 ? S2 : S4];
+  extern __shared__ __align__(16) unsigned char smem[];   // [T][kRows] float32
+  float* sums = reinterpret_cast<float*>(smem);
+  const int tid = threadIdx.x;
+  const int rbk = static_cast<int>(blockIdx.x) / a.splits;
+  const int split = static_cast<int>(blockIdx.x) % a.splits;
+  const int row0 = rbk * kRows;
+  for (int i = tid; i < a.T * kRows / 4; i += kRowWaves * kWave)
+    reinterpret_cast<floatx4*>(sums)[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+  make_plan<kMoeTokens, kRowWaves * kWave>(a, pl);
+  const int groups = (a.f * static_cast<int>(sizeof(T)) + kGroupBytes - 1) / kGroupBytes;
+  const int64_t total = static_cast<int64_t>(pl.classes[2]) * groups;
+  const int64_t u0 = total * split / a.splits;
+  const int64_t u1 = total * (split + 1) / a.splits;
+  down_rows<T, 1, R, 4>(a, pl, 0, pl.classes[0], row0, groups, u0, u1, sums, buf);
+  down_rows<T, 2, R, 4>(a, pl, pl.classes[0], pl.classes[1], row0, groups, u0, u1, sums, buf);
+  down_rows<T, 4, R, 2>(a, pl, pl.classes[1], pl.classes[2], row0, groups, u0, u1, sums, buf);
+  __syncthreads();
+  for (int i = tid; i < a.T * kRows / 4; i += kRowWaves * kWave) {
+    const int t = i / (kRows / 4);
+    const int row = row0 + 4 * (i % (kRows / 4));
+    if (row < a.d)
+      *reinterpret_cast<floatx4*>(a.partial + (static_cast<int64_t>(split) * a.T + t) * a.d + row) =
+          reinterpret_cast<floatx4*>(sums)[i];
+  }
+}
+
+// The splits' partial sums, in order, and the residual.
+template <typename T>
+__global__ void __launch_bounds__(256) k_moe_join(MoeArgs a) {
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+  const int64_t n = static_cast<int64_t>(a.T) * a.d;
+  if (i >= n) return;
+  floatx4 v = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const floatx4*>(a.partial + s * n + i);
+  store_out<T>(a, i, v);
 }
 
 // ---------------------------------------------------------------- host
 
-// Rows and wavefronts of k_moe_down's workgroups for launches of T tokens.
+constexpr int kCus = 256;
+constexpr int kFewTokens = 16;   // up to here the wavefronts of a workgroup split the long axis
+
+// How k_moe_down (few tokens) or k_moe_down_rows cuts the output.
 struct DownShape {
-  int R, NW;
+  int rows;     // per workgroup
+  int blocks;   // of rows
+  int splits;   // shares of the experts' products, so that the workgroups fill the GPU
 };
-DownShape down_shape(int32_t T) { return T <= 128 ? DownShape{2, 8} : DownShape{2, 4}; }
-int row_blocks_of(int32_t d, int32_t T) { return (d + 16 * down_shape(T).R - 1) / (16 * down_shape(T).R); }
-int splits_of(int32_t d, int32_t T) {
-  const int blocks = row_blocks_of(d, T);
-  const int want = 4096 / down_shape(T).NW;   // workgroups that fill the GPU: 16 wavefronts per CU
-  const int s = (want + blocks - 1) / blocks;
-  return s < kMaxSplits ? s : kMaxSplits;
+DownShape down_shape(int32_t d, int32_t T) {
+  DownShape s;
+  s.rows = T <= kFewTokens ? 32 : (T <= 64 ? 256 : 128);   // (sums by token of up to 64 KB)
+  s.blocks = (d + s.rows - 1) / s.rows;
+  const int want = T <= kFewTokens ? 2 * kCus : kCus;
+  s.splits = (want + s.blocks - 1) / s.blocks;
+  const int most = T <= kFewTokens ? 16 : 64;
+  if (s.splits > most) s.splits = most;
+  return s;
 }
 
-constexpr int kCus = 256;
-
-template <typename T, int N, int R, int NW>
-hipError_t launch(MoeArgs a, hipStream_t st) {
+template <typename T>
+hipError_t few_tokens(const MoeArgs& a, hipStream_t st) {
   // at most this many units; each workgroup takes its turn at them
-  const int experts = a.E + a.T * a.K / 64 < a.T * a.K ? a.E + a.T * a.K / 64 : a.T * a.K;
+  const int experts = a.E < a.T * a.K ? a.E : a.T * a.K;
   const int units = experts * ((a.f + kUpRows - 1) / kUpRows);
-  const int fill = N == 1 ? 2 * kCus : kCus;
-  k_moe_up<T, N><<<static_cast<unsigned>(units < fill ? units : fill), kUpWaves * kWave, 0, st>>>(a);
+  k_moe_up<T><<<static_cast<unsigned>(units < 2 * kCus ? units : 2 * kCus), kUpWaves * kWave, 0, st>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  k_moe_down<T><<<static_cast<unsigned>(a.row_blocks) * static_cast<unsigned>(a.splits), kDownWaves * kWave, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int R>
+hipError_t more_tokens(const MoeArgs& a, hipStream_t st) {
+  const int experts = a.E + a.T * a.K / 64 < a.T * a.K ? a.E + a.T * a.K / 64 : a.T * a.K;   // entries, at most
+  const int units = experts * ((a.f + 16 * kRowWaves - 1) / (16 * kRowWaves));
+  k_moe_up_rows<T><<<static_cast<unsigned>(units < 2 * kCus ? units : 2 * kCus), kRowWaves * kWave, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  auto kern = k_moe_down<T, N, R, NW>;
-  const size_t lds = static_cast<size_t>(NW) * a.T * 16 * R * sizeof(float);
-  if (lds + 16384 > 65536) {
-    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
-                            static_cast<int>(lds));
-    if (e != hipSuccess) return e;
-  }
-  kern<<<static_cast<unsigned>(a.row_blocks) * static_cast<unsigned>(a.splits), NW * kWave, lds, st>>>(a);
+  auto kern = k_moe_down_rows<T, R>;
+  const size_t lds = static_cast<size_t>(a.T) * 16 * R * kRowWaves * sizeof(float);
+  e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
+                          static_cast<int>(lds));
+  if (e != hipSuccess) return e;
+  kern<<<static_cast<unsigned>(a.row_blocks) * static_cast<unsigned>(a.splits), kRowWaves * kWave, lds, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t quads = static_cast<int64_t>(a.T) * a.d / 4;
+  k_moe_join<T><<<static_cast<unsigned>((quads + 255) / 256), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t experts(const MoeArgs& a, hipStream_t st) {   // as down_shape
-  if (a.T <= 16) return launch<T, 1, 2, 8>(a, st);
-  if (a.T <= 32) return launch<T, 2, 2, 8>(a, st);
-  if (a.T <= 128) return launch<T, 4, 2, 8>(a, st);
-  return launch<T, 4, 2, 4>(a, st);
+hipError_t experts(const MoeArgs& a, hipStream_t st) {
+  if (a.T <= kFewTokens) return few_tokens<T>(a, st);
+  return a.T <= 64 ? more_tokens<T, 2>(a, st) : more_tokens<T, 1>(a, st);
 }
 
-// Workspace of one launch: [h][partial sums][tickets], each 256-byte aligned; a
-// launch of fewer tokens never needs more.
-size_t parts(int32_t d, int32_t f, int32_t T, int32_t K, size_t* partial, size_t* ticket) {
-  size_t o = align_up(static_cast<size_t>(T) * K * f * 4, kAlign);
-  *partial = o;
-  o += align_up(static_cast<size_t>(splits_of(d, T)) * T * d * sizeof(float), kAlign);
-  *ticket = o;
-  return o + align_up(static_cast<size_t>((d + 15) / 16) * sizeof(uint32_t), kAlign);   // (the most row blocks of any T)
+// Workspace of one launch: [h][tickets][partial sums], each 256-byte aligned.
+size_t parts(int32_t d, int32_t f, int32_t T, int32_t K, size_t* ticket, size_t* partial) {
+  const size_t h = align_up(static_cast<size_t>(T) * K * f * 4, kAlign);
+  *ticket = h;
+  *partial = h + align_up(static_cast<size_t>((d + 31) / 32) * sizeof(uint32_t), kAlign);
+  return *partial + align_up(static_cast<size_t>(down_shape(d, T).splits) * T * d * sizeof(float), kAlign);
 }
 
 }  // namespace
 
 size_t moe_workspace_bytes(int32_t d, int32_t f, fm_dtype, int32_t T, int32_t K) {
-  size_t p, k;
-  return parts(d, f, T < kMoeTokens ? T : kMoeTokens, K, &p, &k);
+  // what the largest launch needs, and any smaller one
+  size_t most = 0, p, k;
+  for (int32_t t : {kFewTokens, 64, kMoeTokens}) {
+    const size_t n = parts(d, f, T < t ? T : t, K, &p, &k);
+    most = n > most ? n : most;
+  }
+  return most;
 }
 
 hipError_t launch_moe_experts(const fm_expert_cache& c, const void* x, const int32_t* ids, const float* weight,
@@ -604,8 +909,9 @@ hipError_t launch_moe_experts(const fm_expert_cache& c, const void* x, const int
   for (int32_t t0 = 0; t0 < T; t0 += kMoeTokens) {
     MoeArgs a;
     a.T = T - t0 < kMoeTokens ? T - t0 : kMoeTokens;
-    size_t partial, ticket;
-    parts(c.d, c.f, a.T, K, &partial, &ticket);
+    size_t ticket, partial;
+    parts(c.d, c.f, a.T, K, &ticket, &partial);
+    const DownShape s = down_shape(c.d, a.T);
     a.slots = static_cast<const char*>(c.slots);
     a.slot_of = c.slot_of;
     a.x = static_cast<const char*>(x) + t0 * row;
@@ -622,8 +928,8 @@ hipError_t launch_moe_experts(const fm_expert_cache& c, const void* x, const int
     a.n_slots = c.n_slots;
     a.d = c.d;
     a.f = c.f;
-    a.splits = splits_of(c.d, a.T);
-    a.row_blocks = row_blocks_of(c.d, a.T);
+    a.splits = s.splits;
+    a.row_blocks = s.blocks;
     const hipError_t e = c.dtype == FM_BF16 ? experts<uint16_t>(a, st) : experts<float>(a, st);
     if (e != hipSuccess) return e;
   }
