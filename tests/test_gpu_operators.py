@@ -141,7 +141,8 @@ def _some_tokens(rng, T, V, law):
 @pytest.mark.parametrize("T,V,d,law", [(1, 1, 1, "uniform"), (1, 300, 64, "uniform"), (50, 7, 1001, "uniform"),
                                        (777, 2000, 136, "zipf"), (33, 5, 8, "same"), (32, 5, 8, "same"),
                                        (9000, 3, 40, "same"), (5000, 900, 260, "zipf"), (400, 60, 2051, "zipf"),
-                                       (64, 1000, 4096, "uniform")])
+                                       (64, 1000, 4096, "uniform"), (1024, 5000, 40, "zipf"),
+                                       (1025, 5000, 40, "zipf"), (700, 4000, 72, "same"), (900, 3500, 33, "uniform")])
 def test_grad(T, V, d, law, dtype, grad):
     print(f"grad T={T} V={V} d={d} {law} {dtype}->{grad}", flush=True)
     fm = _fm()
@@ -179,6 +180,7 @@ def test_grad_special():
     # no tokens: zeros, or nothing touched; a zero scale gives zeros
     none = torch.empty(0, 5, device="cuda")
     assert (fm.embed_grad(none, tok[:0], 4) == 0).all()
+    assert (fm.embed_grad(none, tok[:0], 4000) == 0).all()
     keep = torch.full((4, 5), 3.0, device="cuda")
     assert (fm.embed_grad(none, tok[:0], 4, accumulate=True, out=keep) == 3).all()
 
