@@ -17,6 +17,9 @@ It is a plain, slow, obviously correct restatement of what the paper defines:
 * ``brute``    pure-Python brute force with correctly rounded sums
   (``math.fsum``) and full subset enumeration, used to pin ``finemoe`` on
   tiny inputs.
+* ``operators`` the model operators around the search (embedding lookup, pooling
+  and gradient, an MoE layer's gate and experts), with bounds on what a float32
+  computation may be off by.
 
 Every function is pinned by the ``-m "not gpu"`` tests against closed forms,
 invariants and brute force, including the similarity-weighted blend with

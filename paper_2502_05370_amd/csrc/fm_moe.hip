@@ -6,12 +6,20 @@
 //
 // With few tokens each weight meets a handful of columns, so reading every
 // expert in use once from HBM bounds both products (6 T K d f operations on
-// 6 d f bytes per expert in bf16).  Two launches: k_moe_up (Gate and Up, joined
-// to h) and k_moe_down.  Weights go straight from memory to the registers of
-// the matrix instructions, 16 rows by 128 contiguous bytes per load group;
-// activations, the other operand, come from the caches.  The wavefronts of a
-// workgroup split the long axis, which keeps many loads in flight for any
-// number of experts, and their sums meet in LDS in a fixed order.
+// 6 d f bytes per expert in bf16).  Weights go straight from memory to the
+// registers of the matrix instructions, 16 rows by 128 contiguous bytes per load
+// group.  Up to 16 tokens two launches, k_moe_up (Gate and Up, joined to h) and
+// k_moe_down: the wavefronts of a workgroup split the long axis, which keeps many
+// loads in flight for any number of experts, their sums meet in LDS in a fixed
+// order, and the activations come from the caches.  More tokens take three
+// (k_moe_up_rows, k_moe_down_rows, k_moe_join): the wavefronts own weight rows and
+// share the activations through LDS.
+//
+// Measured, one MI355X, bf16: 8 tokens through 16 experts of 4,096 x 6,400 (1.65
+// GB of weights in use) 162 + 89 us, 6.6 TB/s; 64 tokens through 8 of 4,096 x
+// 14,336 (2.82 GB) 330 + 146 + 5 us, 5.9 TB/s; one token through 4 of 60 of
+// 2,048 x 1,408 (69 MB) 15 + 13 us, of which reading takes 10: the plan, the first
+// loads' latency and the joins of two dependent launches are the rest.
 //
 // h keeps 16 bits of mantissa in bf16 models: it is stored as the nearest bf16
 // and the nearest bf16 of the rest, both multiplied, so that the only rounding
@@ -170,7 +178,8 @@ __device__ __forceinline__ void make_plan(const MoeArgs& a, Plan<MAXT>& pl) {
 __device__ __forceinline__ uint16_t to_bf16(float f) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f)); }
 
 // Load groups of R tiles of 16 weight rows and of C tiles of 16 activation
-// columns in H planes, PA groups in flight.  Loads finish in the order of their
+// columns in H planes, PA groups in flight (a third one, on more registers, costs
+// as much as it hides).  Loads finish in the order of their
 // issue, so both operands of a group go out together: an activation issued after
 // the weights of later groups would wait for them.
 template <typename T, int C, int R, int H, int PA>
@@ -529,7 +538,7 @@ __global__ void __launch_bounds__(kDownWaves * kWave, 4) k_moe_down(MoeArgs a) {
 // From 17 tokens on a workgroup's eight wavefronts own different weight rows and
 // share the activations: with up to 64 columns those would otherwise be read from
 // the L2 as often as the weights from HBM, and a CU's loads cannot serve both
-// (64 tokens through 8 experts of 4,096 x 14,336: 543 us that way, ROWS_US this).
+// (64 tokens through 8 experts of 4,096 x 14,336: 535 us that way, 480 this).
 // They pass through LDS a slab of SG load groups at a time, two slabs deep; the
 // weights keep going straight to registers, a slab ahead.
 constexpr int kRowWaves = 8;

@@ -4,7 +4,9 @@
 // there.
 //
 // A batch of decode tokens is bound by latency (one workgroup reads E d values,
-// 246 KB for 60 experts of 2,048), a prefill by reading x.  A workgroup takes 16
+// 246 KB for 60 experts of 2,048: 11 us, 5 of them without the gate), a prefill by
+// reading x (8,192 x 4,096 bf16, 16 experts: 18 us, 3.8 TB/s of x and the gate's
+// 64 MB from the L2).  A workgroup takes 16
 // tokens per tile; its wavefronts split d, so that every load of a decode call
 // is in flight at once, and join their sums in LDS in a fixed order.  One
 // wavefront then holds one token's logits, an expert per lane.
