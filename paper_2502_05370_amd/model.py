@@ -5,10 +5,12 @@ that a cache holds (fm_embed_*, fm_moe_* of include/finemoe_map.h).
 Argument marshalling only, as the rest of the binding: every step runs in the
 library's HIP kernels.  Tensors must be contiguous, on one GPU and of the stated
 type; outputs are created unless ``out`` gives them.  Work goes to the current
-stream, or to ``stream``.
+stream, or to ``stream``, and memory that a call creates (outputs, scratch,
+workspaces) belongs to the same stream.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 from typing import Optional, Tuple
 
@@ -31,6 +33,19 @@ def _call(name: str, device: torch.device, stream, *args) -> None:
             status = getattr(_LIBRARY, name)(*args, _stream(stream))
     if status != _lib.FM_OK:
         _lib.check(status, name)
+
+
+def _on(stream):
+    """The allocator's context for memory that work on ``stream`` uses: a block that another stream owns could be in
+    use there still, or be given out there again while this work runs."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _new(shape, dtype: torch.dtype, device: torch.device, stream) -> torch.Tensor:
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _on(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _float_rows(t, name: str) -> torch.Tensor:
@@ -64,7 +79,7 @@ def embed_lookup(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, 
     dev = table.device
     T = _vector(tokens, "tokens", dev)
     if out is None:
-        out = torch.empty((T, d), dtype=table.dtype, device=dev)
+        out = _new((T, d), table.dtype, dev, stream)
     else:
         _need(out, "out", table.dtype, (T, d), dev)
     _call("fm_embed_lookup", dev, stream, table.data_ptr(), V, d, _CODE[table.dtype], tokens.data_ptr(), T, scale,
@@ -84,7 +99,7 @@ def embed_pool(table: torch.Tensor, tokens: torch.Tensor, offsets: torch.Tensor,
     if B < 0:
         raise ValueError("offsets must hold at least one element")
     if out is None:
-        out = torch.empty((B, d), dtype=torch.bfloat16, device=dev)
+        out = _new((B, d), torch.bfloat16, dev, stream)
     else:
         _need(out, "out", torch.bfloat16, (B, d), dev)
     _call("fm_embed_pool", dev, stream, table.data_ptr(), V, d, _CODE[table.dtype], tokens.data_ptr(), T,
@@ -120,13 +135,14 @@ def embed_grad(dout: torch.Tensor, tokens: torch.Tensor, V: int, scale: float = 
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = torch.empty((V, d), dtype=torch.float32 if grad_dtype is None else grad_dtype, device=dev)
+        out = _new((V, d), torch.float32 if grad_dtype is None else grad_dtype, dev, stream)
     if grad_dtype is not None and out.dtype != grad_dtype:
         raise ValueError(f"out must be {grad_dtype}, got {out.dtype}")
     _float_rows(out, "out")
     _need(out, "out", out.dtype, (V, d), dev)
     if scratch is None:
-        scratch = EmbedGradScratch(T, V, dev)
+        with _on(stream):
+            scratch = EmbedGradScratch(T, V, dev)
     _need(scratch.buf, "scratch", torch.uint8, (scratch.nbytes,), dev)
     _call("fm_embed_grad", dev, stream, dout.data_ptr(), _CODE[dout.dtype], tokens.data_ptr(), T, V, d, scale,
           1 if accumulate else 0, out.data_ptr(), _CODE[out.dtype], scratch.buf.data_ptr(), scratch.nbytes,
@@ -150,8 +166,8 @@ def moe_route(x: torch.Tensor, gate: torch.Tensor, k: int, renorm: bool = False,
     if active is not None:
         _need(active, "active", torch.uint8, (T,), dev)
     if out is None:
-        out = (torch.empty((T, E), dtype=probs_dtype, device=dev), torch.empty((T, k), dtype=torch.int32, device=dev),
-               torch.empty((T, k), dtype=torch.float32, device=dev), torch.empty((T,), dtype=torch.int64, device=dev))
+        out = (_new((T, E), probs_dtype, dev, stream), _new((T, k), torch.int32, dev, stream),
+               _new((T, k), torch.float32, dev, stream), _new((T,), torch.int64, dev, stream))
     probs, ids, weight, mask = out
     if not isinstance(probs, torch.Tensor) or probs.dtype not in _CODE or probs.shape != (T, E) or probs.device != dev \
             or (E > 1 and probs.stride(1) != 1) or (T > 1 and probs.stride(0) < E):
@@ -206,15 +222,22 @@ class ExpertCache:
         """The expert is no longer held (its slot may be loaded again)."""
         self.slot_of[expert] = -1
 
-    def check(self) -> int:
-        """Synchronise and return the sticky FM_FLAG_* bits of the calls so far, cleared."""
-        f = int(self.flags.item())
-        self.flags.zero_()
+    def check(self, stream=None) -> int:
+        """Synchronise the stream and return the sticky FM_FLAG_* bits of the calls that it has seen, cleared."""
+        with _on(stream):
+            f = int(self.flags.item())
+            self.flags.zero_()
         return f
 
-    def ensure_workspace(self, T: int, K: int) -> "MoeWorkspace":
-        if self.workspace is None or moe_workspace_bytes(self.d, self.f, self._name(), max(T, 1), K) > self.workspace.nbytes:
-            self.workspace = MoeWorkspace(self, max(T, 1), K)
+    def ensure_workspace(self, T: int, K: int, stream=None) -> "MoeWorkspace":
+        """The cache's own workspace, made or enlarged for calls of T tokens of K experts each on the stream, which
+        the calls before must be ordered with."""
+        old = self.workspace
+        if old is None or moe_workspace_bytes(self.d, self.f, self._name(), max(T, 1), K) > old.nbytes:
+            with _on(stream):
+                self.workspace = MoeWorkspace(self, max(T, 1), K)
+                if old is not None:   # its memory is given out again after what this stream has waited for
+                    old.buf.record_stream(torch.cuda.current_stream(self.device))
         return self.workspace
 
     def _name(self) -> str:
@@ -253,10 +276,10 @@ def moe_experts(cache: ExpertCache, x: torch.Tensor, ids: torch.Tensor, weight: 
     if residual is not None:
         _need(residual, "residual", cache.dtype, (T, cache.d), dev)
     if out is None:
-        out = torch.empty((T, cache.d), dtype=cache.dtype, device=dev)
+        out = _new((T, cache.d), cache.dtype, dev, stream)
     else:
         _need(out, "out", cache.dtype, (T, cache.d), dev)
-    ws = workspace if workspace is not None else cache.ensure_workspace(T, K)
+    ws = workspace if workspace is not None else cache.ensure_workspace(T, K, stream)
     _call("fm_moe_experts", dev, stream, cache.desc, x.data_ptr(), ids.data_ptr(), weight.data_ptr(), T, K,
           _ptr(residual), out.data_ptr(), cache.flags.data_ptr(), ws.buf.data_ptr(), ws.nbytes)
     return out
