@@ -428,7 +428,8 @@ typedef struct {
 
 /* Bytes of workspace (device memory owned by the caller, 256-byte aligned)
  * for fm_moe_experts calls of up to T_max tokens of K experts each: the
- * activated products of one launch (up to 128 tokens) and its partial sums.
+ * activated products of one pass over the experts and its partial sums.  Above
+ * 128 tokens it does not depend on T_max.
  * Returns 0 for sizes that fm_moe_experts refuses or T_max < 1. */
 size_t fm_moe_workspace_bytes(int32_t d, int32_t f, fm_dtype dtype, int32_t T_max, int32_t K);
 
@@ -443,9 +444,9 @@ size_t fm_moe_workspace_bytes(int32_t d, int32_t f, fm_dtype dtype, int32_t T_ma
  * slots >= n_slots contribute nothing and set FM_FLAG_INDEX_RANGE.  An expert
  * that a token lists twice counts with the sum of its weights.  An expert
  * that every token takes (a shared expert of m times the width) is m experts
- * in every token's list.  Made for the few tokens of a decode iteration: a
- * launch takes up to 128 tokens and reads each expert in use once; longer
- * batches take several launches.  1 <= K <= 8.  The weights of one slot must
+ * in every token's list.  Up to 128 tokens (a decode iteration) each expert in
+ * use is read once; longer batches (prompts) take passes of up to 4,096 tokens,
+ * or of as many as 256 MB hold of K f float32 values.  1 <= K <= 8.  The weights of one slot must
  * not exceed 0xF0000000 bytes.  workspace: at least
  * fm_moe_workspace_bytes(d, f, dtype, T, K) bytes, rewritten by the call;
  * calls sharing one must be ordered. */

@@ -222,7 +222,8 @@ struct RouteArgs {
   uint64_t* mask;          // [T] or null
 };
 hipError_t launch_moe_route(const RouteArgs& a, fm_dtype dt, fm_dtype probs_dt, hipStream_t st);
-constexpr int kMoeTokens = 128;   // tokens of one launch of the experts' products
+constexpr int kMoeTokens = 128;   // tokens up to which the experts' products are bound by the weights' stream
+constexpr int kLongTokens = 4096;  // of one launch above
 size_t moe_workspace_bytes(int32_t d, int32_t f, fm_dtype dt, int32_t T, int32_t K);
 hipError_t launch_moe_experts(const fm_expert_cache& c, const void* x, const int32_t* ids, const float* weight,
                               int32_t T, int32_t K, const void* residual, void* out, uint32_t* flags, void* ws,

@@ -70,6 +70,9 @@ struct Plan {
   uint16_t tok[kPairs];            // token of each place
   float weight[kPairs];            // and its weight
   int32_t again;                   // some token lists an expert twice
+  // unit u of n entries of `blocks` row blocks each
+  static __device__ __forceinline__ int entry(int u, int blocks, int) { return u / blocks; }
+  static __device__ __forceinline__ int block(int u, int blocks, int) { return u % blocks; }
 };
 
 // Filled by the whole workgroup; ends with a barrier.
@@ -556,7 +559,7 @@ struct Slab {
 // next(slab) sets the slab after the one it set last (false: none left);
 // done(acc) takes the sums after a slab that is the last.  Called by the whole
 // workgroup; buf holds two slabs of columns.
-template <typename T, int C, int H, int R, int SG, typename Next, typename Done>
+template <typename T, int C, int H, int R, int SG, int HINT, typename Next, typename Done>
 __device__ __forceinline__ void stream_slabs(__amdgpu_buffer_rsrc_t rs_b, unsigned char* buf, Next next, Done done) {
   constexpr int kChunks = SG * 8;                       // 16-byte pieces of a column in a slab
   constexpr int kCol = SG * RowPairs::kBytes + 16;      // (the odd piece keeps the columns' banks apart)
@@ -571,14 +574,14 @@ __device__ __forceinline__ void stream_slabs(__amdgpu_buffer_rsrc_t rs_b, unsign
   uint32x4 piece[NB];
   uint32x4 fw[SG][R][2];
   floatx4 acc[R][C];
-  Slab<C, H, R> cur, nx;
-  auto load_b = [&](const Slab<C, H, R>& s) __attribute__((always_inline)) {
+  Slab<C, H, R> slab;   // that is being loaded
+  auto load_b = [&]() __attribute__((always_inline)) {
     const uint32_t at = static_cast<uint32_t>(tid % kChunks) * 16u;
-    const bool in = s.k + at < s.k_end;
-    const int ks = static_cast<int>(s.k < s.k_end ? s.k : 0u);
+    const bool in = slab.k + at < slab.k_end;
+    const int ks = static_cast<int>(slab.k < slab.k_end ? slab.k : 0u);
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      const uint32_t col = s.col[i / (NB / H)][i % (NB / H)];
+      const uint32_t col = slab.col[i / (NB / H)][i % (NB / H)];
       piece[i] = __builtin_amdgcn_raw_buffer_load_b128(
           rs_b, static_cast<int>(in && col != kOutside ? col + at : kOutside), ks, kKeep);
     }
@@ -588,24 +591,25 @@ __device__ __forceinline__ void stream_slabs(__amdgpu_buffer_rsrc_t rs_b, unsign
     for (int i = 0; i < NB; ++i)
       *reinterpret_cast<uint32x4*>(to + (i * kCols + tid / kChunks) * kCol + tid % kChunks * 16) = piece[i];
   };
-  auto load_w = [&](const Slab<C, H, R>& s, int p) __attribute__((always_inline)) {
+  auto load_w = [&](int p) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) s.rows[r].template load<kStream>(s.w, s.k + p * RowPairs::kBytes, s.k_end, fw[p][r]);
+    for (int r = 0; r < R; ++r)
+      slab.rows[r].template load<HINT>(slab.w, slab.k + p * RowPairs::kBytes, slab.k_end, fw[p][r]);
   };
   raw_barrier();   // the buffers are free
-  if (!next(cur)) return;
-  nx = cur;        // (its buffer stands also where nothing comes next)
-  load_b(cur);
+  if (!next(slab)) return;
+  load_b();
 #pragma unroll
-  for (int p = 0; p < SG; ++p) load_w(cur, p);
+  for (int p = 0; p < SG; ++p) load_w(p);
   store_b(buf);
   wait_lgkm0();
   raw_barrier();
   clear(acc);
   for (int turn = 0;; turn ^= 1) {
-    const bool more = next(nx);
-    if (!more) nx.k = nx.k_end = 0;
-    load_b(nx);
+    const bool last = slab.last;
+    const bool more = next(slab);
+    if (!more) slab.k = slab.k_end = 0;   // (its buffer stands)
+    load_b();
     const unsigned char* from = buf + turn * kSlab;
 #pragma unroll
     for (int p = 0; p < SG; ++p) {
@@ -623,9 +627,9 @@ __device__ __forceinline__ void stream_slabs(__amdgpu_buffer_rsrc_t rs_b, unsign
 #pragma unroll
             for (int r = 0; r < R; ++r) acc[r][j] = mma_step<T>(sw[r][s], b, acc[r][j]);
           }
-      load_w(nx, p);
+      load_w(p);
     }
-    if (cur.last) {
+    if (last) {
       done(acc);
       clear(acc);
     }
@@ -633,7 +637,6 @@ __device__ __forceinline__ void stream_slabs(__amdgpu_buffer_rsrc_t rs_b, unsign
     store_b(buf + (turn ^ 1) * kSlab);
     wait_lgkm0();
     raw_barrier();
-    cur = nx;
   }
 }
 
@@ -653,66 +656,78 @@ __device__ __forceinline__ void aim_columns(uint32_t (&col)[H][C], int n, int p0
     }
 }
 
-// Units of 128 gate and 128 up rows of one entry, 16 and 16 per wavefront.
-template <typename T, int C, int SG>
-__device__ __forceinline__ void up_rows(const MoeArgs& a, const Plan<kMoeTokens>& pl, int e0, int e1, unsigned char* buf) {
-  constexpr int kRows = 16 * kRowWaves;
+// Units of one entry and 128 M gate and up rows, 16 M of each per wavefront, for
+// the entries e0 .. e1 - 1 (all of C tiles); workgroup `me` of `grid` takes every
+// grid-th one.  HINT: whether other workgroups read the weights too.
+template <typename T, int C, int SG, int M, int HINT, typename Places>
+__device__ __forceinline__ void up_rows(const MoeArgs& a, const Places& pl, int e0, int e1, int me, int grid,
+                                        unsigned char* buf) {
+  constexpr int kRows = 16 * M * kRowWaves;
+  constexpr int R = 2 * M;
   const int lane = threadIdx.x % kWave;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const uint32_t rb = static_cast<uint32_t>(a.d) * sizeof(T);
   const int blocks = (a.f + kRows - 1) / kRows;
   const int slabs = static_cast<int>((rb + SG * RowPairs::kBytes - 1) / (SG * RowPairs::kBytes));
-  const int grid = static_cast<int>(gridDim.x);
   const int u_end = e1 * blocks;
   int u = e0 * blocks;
-  u += (static_cast<int>(blockIdx.x) - u % grid + grid) % grid;
+  u += (me - u % grid + grid) % grid;
   const size_t slot_bytes = static_cast<size_t>(3) * a.d * a.f * sizeof(T);
   int at = u;      // the unit of the slab set last,
   int i = -1;      // and that slab among the unit's
   int turn = 0;    // (rows of a power of two bytes: blocks start at different places)
   int unit = u;    // of the sums
-  auto next = [&](Slab<C, 1, 2>& s) __attribute__((always_inline)) {
+  auto next = [&](Slab<C, 1, R>& s) __attribute__((always_inline)) {
     if (++i == slabs) {
       i = 0;
       at += grid;
     }
     if (at >= u_end) return false;
-    const int e = at / blocks;
-    const int blk = at - e * blocks;
-    s.w = row_buffer(a.slots + __builtin_amdgcn_readfirstlane(pl.entry_slot[e]) * slot_bytes,
-                     static_cast<uint32_t>(slot_bytes));
-    s.rows[0] = RowPairs(blk * kRows + 16 * wv, a.f, rb, 0u);
-    s.rows[1] = RowPairs(blk * kRows + 16 * wv, a.f, rb, static_cast<uint32_t>(a.f) * rb);
-    aim_columns<SG>(s.col, pl.entry_n[e], pl.entry_place[e], 0u,
-                    [&](int p) { return static_cast<uint32_t>(pl.tok[p]) * rb; });
-    turn = static_cast<int>(static_cast<uint32_t>(blk) * 5u % static_cast<uint32_t>(slabs));
+    if (i == 0) {   // (the unit's other slabs find this set)
+      const int e = e0 + Places::entry(at - e0 * blocks, blocks, e1 - e0);
+      const int blk = Places::block(at - e0 * blocks, blocks, e1 - e0);
+      s.w = row_buffer(a.slots + __builtin_amdgcn_readfirstlane(pl.entry_slot[e]) * slot_bytes,
+                       static_cast<uint32_t>(slot_bytes));
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        s.rows[m] = RowPairs(blk * kRows + 16 * (wv * M + m), a.f, rb, 0u);
+        s.rows[M + m] = RowPairs(blk * kRows + 16 * (wv * M + m), a.f, rb, static_cast<uint32_t>(a.f) * rb);
+      }
+      aim_columns<SG>(s.col, pl.entry_n[e], pl.entry_place[e], 0u,
+                      [&](int p) { return static_cast<uint32_t>(pl.tok[p]) * rb; });
+      turn = static_cast<int>(static_cast<uint32_t>(blk) * 5u % static_cast<uint32_t>(slabs));
+    }
     const int q = i + turn < slabs ? i + turn : i + turn - slabs;
     s.k = static_cast<uint32_t>(q) * (SG * RowPairs::kBytes);
     s.k_end = rb;
     s.last = i + 1 == slabs;
     return true;
   };
-  auto done = [&](floatx4 (&acc)[2][C]) __attribute__((always_inline)) {
-    const int e = unit / blocks;
-    const int row = (unit - e * blocks) * kRows + 16 * wv + 4 * (lane / 16);
+  auto done = [&](floatx4 (&acc)[R][C]) __attribute__((always_inline)) {
+    const int e = e0 + Places::entry(unit - e0 * blocks, blocks, e1 - e0);
+    const int row0 = Places::block(unit - e0 * blocks, blocks, e1 - e0) * kRows + 16 * wv * M + 4 * (lane / 16);
     unit += grid;
-    if (row >= a.f) return;   // (f is a multiple of 8: four rows exist or none does)
 #pragma unroll
     for (int j = 0; j < C; ++j) {
       const int col = 16 * j + lane % 16;
       if (col >= pl.entry_n[e]) continue;
       const int place = pl.entry_place[e] + col;
       const float w = pl.weight[place];
-      floatx4 hv;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float gv = acc[0][j][r];
-        hv[r] = w * (gv / (1.0f + expf(-gv)) * acc[1][j][r]);
+      for (int m = 0; m < M; ++m) {
+        const int row = row0 + 16 * m;
+        if (row >= a.f) continue;   // (f is a multiple of 8: four rows exist or none does)
+        floatx4 hv;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float gv = acc[m][j][r];
+          hv[r] = w * (gv / (1.0f + expf(-gv)) * acc[M + m][j][r]);
+        }
+        store_h<T>(a, place, row, hv);
       }
-      store_h<T>(a, place, row, hv);
     }
   };
-  stream_slabs<T, C, 1, 2, SG>(row_buffer(a.x, static_cast<uint32_t>(a.T) * rb), buf, next, done);
+  stream_slabs<T, C, 1, R, SG, HINT>(row_buffer(a.x, static_cast<uint32_t>(a.T) * rb), buf, next, done);
 }
 
 constexpr int slab_bytes(int C, int H, int SG) { return 2 * H * C * 16 * (SG * 128 + 16); }
@@ -722,9 +737,10 @@ __global__ void __launch_bounds__(kRowWaves * kWave, 4) k_moe_up_rows(MoeArgs a)
   __shared__ Plan<kMoeTokens> pl;
   __shared__ __align__(16) unsigned char buf[slab_bytes(4, 1, 2) > slab_bytes(2, 1, 4) ? slab_bytes(4, 1, 2) : slab_bytes(2, 1, 4)];
   make_plan<kMoeTokens, kRowWaves * kWave>(a, pl);
-  up_rows<T, 1, 4>(a, pl, 0, pl.classes[0], buf);
-  up_rows<T, 2, 4>(a, pl, pl.classes[0], pl.classes[1], buf);
-  up_rows<T, 4, 2>(a, pl, pl.classes[1], pl.classes[2], buf);
+  const int me = static_cast<int>(blockIdx.x), grid = static_cast<int>(gridDim.x);
+  up_rows<T, 1, 4, 1, kStream>(a, pl, 0, pl.classes[0], me, grid, buf);
+  up_rows<T, 2, 4, 1, kStream>(a, pl, pl.classes[0], pl.classes[1], me, grid, buf);
+  up_rows<T, 4, 2, 1, kStream>(a, pl, pl.classes[1], pl.classes[2], me, grid, buf);
 }
 
 // Load groups [u, u1) of the concatenated entries, those among entries e0 .. e1 - 1
@@ -780,7 +796,7 @@ __device__ __forceinline__ void down_rows(const MoeArgs& a, const Plan<kMoeToken
     }
   };
   const uint32_t h_bytes = static_cast<uint32_t>(static_cast<size_t>(a.T) * a.K * a.f * 4);
-  stream_slabs<T, C, H, R, SG>(row_buffer(a.h, h_bytes), buf, next, done);
+  stream_slabs<T, C, H, R, SG, kStream>(row_buffer(a.h, h_bytes), buf, next, done);
 }
 
 // A workgroup owns 128 R output rows and one of the splits' shares of the load
@@ -828,6 +844,271 @@ __global__ void __launch_bounds__(256) k_moe_join(MoeArgs a) {
 #pragma unroll 8
   for (int s = 0; s < a.splits; ++s) v += *reinterpret_cast<const floatx4*>(a.partial + s * n + i);
   store_out<T>(a, i, v);
+}
+
+// ---------------------------------------------------------------- long batches
+
+// Above kMoeTokens an expert in use meets so many tokens that the matrix
+// instructions, not the weights' stream, come to bound the products.  The same
+// slabs then serve 64 weight rows per wavefront by 128 places: a piece of
+// activations out of LDS feeds four matrix instructions, a weight eight.  The
+// places are listed once, by a launch of one workgroup, and each place's product
+// is written by itself; a last launch adds a token's K.
+constexpr int kLongPlaces = 128;   // of an entry
+constexpr int kLongEntries = kMaxE + kLongTokens * kMaxK / kLongPlaces;
+
+struct LongPlan {
+  int32_t classes[4];   // ends of the entries of 1, 2, 4 and 8 tiles
+  int32_t slot[kLongEntries], place[kLongEntries], n[kLongEntries];
+};
+struct LongArgs {
+  MoeArgs m;
+  LongPlan* plan;
+  uint16_t* tok;        // [T K] token of each place
+  float* weight;        // and its weight
+  int32_t* place_of;    // [T][K] (-1: no product)
+};
+
+constexpr int kListWaves = 16;
+
+__global__ void __launch_bounds__(kListWaves * kWave) k_moe_list(LongArgs a) {
+  __shared__ int32_t count[kListWaves][kMaxE];   // then the next place of each wavefront's share
+  __shared__ int32_t slot[kMaxE];
+  const int tid = threadIdx.x;
+  const int lane = tid % kWave;
+  const int wv = tid / kWave;
+  const int pairs = a.m.T * a.m.K;
+  if (tid < kMaxE) slot[tid] = tid < a.m.E ? a.m.slot_of[tid] : -1;
+  count[wv][lane] = 0;
+  __syncthreads();
+  const int share = (pairs + kListWaves * kWave - 1) / (kListWaves * kWave) * kWave;
+  const int p0 = wv * share;
+  const int p1 = p0 + share < pairs ? p0 + share : pairs;
+  uint32_t bad = 0;
+  // a pair's expert, or -1
+  auto expert = [&](int p, bool report) {
+    int e = p < p1 ? a.m.ids[p] : -1;
+    if (e < 0) return -1;
+    const int s = e < a.m.E ? slot[e] : 0;
+    uint32_t b = 0;
+    if (e >= a.m.E || s >= a.m.n_slots) b = FM_FLAG_INDEX_RANGE;
+    else if (s < 0) b = FM_FLAG_EXPERT_MISSING;
+    if (report) bad |= b;
+    return b != 0 ? -1 : e;
+  };
+  // the lanes that hold the same expert
+  auto same = [&](int e) {
+    uint64_t m = __ballot(e >= 0);
+#pragma unroll
+    for (int b = 0; b < 6; ++b) {
+      const uint64_t one = __ballot((e >> b & 1) != 0);
+      m &= (e >> b & 1) != 0 ? one : ~one;
+    }
+    return m;
+  };
+  for (int p = p0; p < p1; p += kWave) {
+    const int e = expert(p + lane, true);
+    const uint64_t m = same(e);
+    if (e >= 0 && (m & ((1ull << lane) - 1ull)) == 0) atomicAdd(&count[wv][e], __popcll(m));
+  }
+  if (bad != 0 && a.m.flags != nullptr) atomicOr(a.m.flags, bad);
+  __syncthreads();
+  if (wv == 0) {   // an expert per lane
+    int n = 0;
+    for (int w = 0; w < kListWaves; ++w) n += count[w][lane];
+    auto scan = [&](int v) {   // exclusive
+      int incl = v;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const int u = __shfl_up(incl, o, kWave);
+        if (lane >= o) incl += u;
+      }
+      return incl - v;
+    };
+    const int first = scan(n);
+    int next = first;
+    for (int w = 0; w < kListWaves; ++w) {
+      const int c = count[w][lane];
+      count[w][lane] = next;
+      next += c;
+    }
+    const int rest = n % kLongPlaces;
+    int base = 0;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      // entries of this class: of the last one the expert's rest, and the whole ones
+      const bool mine = rest > (c == 0 ? 0 : 8 << c) && rest <= (c == 3 ? kLongPlaces : 16 << c);
+      const int have = (mine ? 1 : 0) + (c == 3 ? n / kLongPlaces : 0);
+      const int at = base + scan(have);
+      for (int j = 0; j < have; ++j) {
+        const int from = mine && j + 1 == have ? n - rest : j * kLongPlaces;
+        a.plan->slot[at + j] = slot[lane];
+        a.plan->place[at + j] = first + from;
+        a.plan->n[at + j] = n - from < kLongPlaces ? n - from : kLongPlaces;
+      }
+      base = __shfl(at + have, kWave - 1, kWave);
+      if (lane == 0) a.plan->classes[c] = base;
+    }
+  }
+  __syncthreads();
+  for (int p = p0; p < p1; p += kWave) {
+    const int e = expert(p + lane, false);
+    const uint64_t m = same(e);
+    const uint64_t before = m & ((1ull << lane) - 1ull);
+    int at = 0;
+    if (e >= 0 && before == 0) at = atomicAdd(&count[wv][e], __popcll(m));
+    at = __shfl(at, m != 0 ? __ffsll(static_cast<long long>(m)) - 1 : 0, kWave) + __popcll(before);
+    if (p + lane < p1) {
+      a.place_of[p + lane] = e >= 0 ? at : -1;
+      if (e >= 0) {
+        a.tok[at] = static_cast<uint16_t>((p + lane) / a.m.K);
+        a.weight[at] = a.m.weight[p + lane];
+      }
+    }
+  }
+}
+
+// The list as the products' kernels see it: the entries (and for the gate and up
+// projections the tokens) in LDS, read in every unit.
+struct LongPlaces {
+  const int32_t *entry_slot, *entry_place, *entry_n;
+  const uint16_t* tok;
+  const float* weight;
+  // the entries vary fastest: an expert's are neighbours and read the same
+  // weights, in workgroups of one XCD at the same time
+  static __device__ __forceinline__ int entry(int u, int, int n) { return u % n; }
+  static __device__ __forceinline__ int block(int u, int, int n) { return u / n; }
+};
+
+constexpr int kXcds = 8;
+// Consecutive workgroups go to different XCDs; this numbers those of an XCD in a row.
+__device__ __forceinline__ int xcd_order() {
+  return static_cast<int>(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds);
+}
+
+template <int H>
+constexpr int long_slab() {
+  constexpr int a = slab_bytes(2, H, 4), b = slab_bytes(8, H, 2);
+  return a > b ? a : b;
+}
+
+// The entries from the plan into LDS.
+__device__ __forceinline__ void stage_entries(const LongPlan& plan, int32_t (*e)[kLongEntries]) {
+  const int n = plan.classes[3];
+  for (int i = threadIdx.x; i < n; i += kRowWaves * kWave) {
+    e[0][i] = plan.slot[i];
+    e[1][i] = plan.place[i];
+    e[2][i] = plan.n[i];
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kRowWaves * kWave, 2) k_moe_up_long(LongArgs a) {
+  __shared__ int32_t entries[3][kLongEntries];
+  extern __shared__ __align__(16) unsigned char smem[];   // [slabs][tokens of the places]
+  uint16_t* tok = reinterpret_cast<uint16_t*>(smem + long_slab<1>());
+  stage_entries(*a.plan, entries);
+  for (int i = threadIdx.x * 2; i < a.m.T * a.m.K; i += kRowWaves * kWave * 2)
+    *reinterpret_cast<uint32_t*>(tok + i) = *reinterpret_cast<const uint32_t*>(a.tok + i);
+  __syncthreads();
+  const LongPlaces pl{entries[0], entries[1], entries[2], tok, a.weight};
+  const int32_t* cl = a.plan->classes;
+  const int me = xcd_order(), grid = static_cast<int>(gridDim.x);
+  up_rows<T, 8, 2, 2, kKeep>(a.m, pl, cl[2], cl[3], me, grid, smem);
+  up_rows<T, 4, 2, 2, kKeep>(a.m, pl, cl[1], cl[2], me, grid, smem);
+  up_rows<T, 2, 4, 2, kKeep>(a.m, pl, cl[0], cl[1], me, grid, smem);
+  up_rows<T, 1, 4, 2, kKeep>(a.m, pl, 0, cl[0], me, grid, smem);
+}
+
+// Units of one entry and 512 output rows, 64 per wavefront; each place's product
+// goes to its own row.
+template <typename T, int C, int SG>
+__device__ __forceinline__ void down_long(const MoeArgs& a, const LongPlaces& pl, int e0, int e1, int me, int grid,
+                                          unsigned char* buf) {
+  constexpr int H = sizeof(T) == 2 ? 2 : 1;   // planes of h
+  constexpr int R = 4;
+  constexpr int kRows = 16 * R * kRowWaves;
+  const int lane = threadIdx.x % kWave;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const uint32_t rb = static_cast<uint32_t>(a.f) * sizeof(T);
+  const uint32_t plane = static_cast<uint32_t>(a.T) * a.K * rb;
+  const int blocks = (a.d + kRows - 1) / kRows;
+  const int slabs = static_cast<int>((rb + SG * RowPairs::kBytes - 1) / (SG * RowPairs::kBytes));
+  const int u_end = e1 * blocks;
+  int u = e0 * blocks;
+  u += (me - u % grid + grid) % grid;
+  const size_t slot_elems = static_cast<size_t>(3) * a.d * a.f;
+  const uint32_t down_bytes = static_cast<uint32_t>(static_cast<size_t>(a.d) * a.f * sizeof(T));
+  int at = u, i = -1, turn = 0, unit = u;
+  auto next = [&](Slab<C, H, R>& s) __attribute__((always_inline)) {
+    if (++i == slabs) {
+      i = 0;
+      at += grid;
+    }
+    if (at >= u_end) return false;
+    if (i == 0) {
+      const int e = e0 + LongPlaces::entry(at - e0 * blocks, blocks, e1 - e0);
+      const int blk = LongPlaces::block(at - e0 * blocks, blocks, e1 - e0);
+      s.w = row_buffer(a.slots + (__builtin_amdgcn_readfirstlane(pl.entry_slot[e]) * slot_elems +
+                                  static_cast<size_t>(2) * a.d * a.f) * sizeof(T), down_bytes);
+#pragma unroll
+      for (int r = 0; r < R; ++r) s.rows[r] = RowPairs(blk * kRows + 16 * (wv * R + r), a.d, rb, 0u);
+      aim_columns<SG>(s.col, pl.entry_n[e], pl.entry_place[e], plane,
+                      [&](int p) { return static_cast<uint32_t>(p) * rb; });
+      turn = static_cast<int>(static_cast<uint32_t>(blk) * 5u % static_cast<uint32_t>(slabs));
+    }
+    const int q = i + turn < slabs ? i + turn : i + turn - slabs;
+    s.k = static_cast<uint32_t>(q) * (SG * RowPairs::kBytes);
+    s.k_end = rb;
+    s.last = i + 1 == slabs;
+    return true;
+  };
+  auto done = [&](floatx4 (&acc)[R][C]) __attribute__((always_inline)) {
+    const int e = e0 + LongPlaces::entry(unit - e0 * blocks, blocks, e1 - e0);
+    const int row0 = LongPlaces::block(unit - e0 * blocks, blocks, e1 - e0) * kRows + 16 * R * wv + 4 * (lane / 16);
+    unit += grid;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int col = 16 * j + lane % 16;
+      if (col >= pl.entry_n[e]) continue;
+      float* o = a.partial + static_cast<int64_t>(pl.entry_place[e] + col) * a.d + row0;
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (row0 + 16 * r < a.d) *reinterpret_cast<floatx4*>(o + 16 * r) = acc[r][j];
+    }
+  };
+  const uint32_t h_bytes = static_cast<uint32_t>(static_cast<size_t>(a.T) * a.K * a.f * 4);
+  stream_slabs<T, C, H, R, SG, kKeep>(row_buffer(a.h, h_bytes), buf, next, done);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kRowWaves * kWave, 2) k_moe_down_long(LongArgs a) {
+  __shared__ int32_t entries[3][kLongEntries];
+  extern __shared__ __align__(16) unsigned char smem[];   // slabs
+  stage_entries(*a.plan, entries);
+  __syncthreads();
+  const LongPlaces pl{entries[0], entries[1], entries[2], nullptr, nullptr};
+  const int32_t* cl = a.plan->classes;
+  const int me = xcd_order(), grid = static_cast<int>(gridDim.x);
+  down_long<T, 8, 2>(a.m, pl, cl[2], cl[3], me, grid, smem);
+  down_long<T, 4, 2>(a.m, pl, cl[1], cl[2], me, grid, smem);
+  down_long<T, 2, 4>(a.m, pl, cl[0], cl[1], me, grid, smem);
+  down_long<T, 1, 4>(a.m, pl, 0, cl[0], me, grid, smem);
+}
+
+// A token's products, in the order of its experts, and the residual.
+template <typename T>
+__global__ void __launch_bounds__(256) k_moe_sum(LongArgs a) {
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+  if (i >= static_cast<int64_t>(a.m.T) * a.m.d) return;
+  const int t = static_cast<int>(i / a.m.d);
+  const int row = static_cast<int>(i - static_cast<int64_t>(t) * a.m.d);
+  floatx4 v = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < a.m.K; ++k) {
+    const int p = a.place_of[t * a.m.K + k];
+    if (p >= 0) v += *reinterpret_cast<const floatx4*>(a.m.partial + static_cast<int64_t>(p) * a.m.d + row);
+  }
+  store_out<T>(a.m, i, v);
 }
 
 // ---------------------------------------------------------------- host
@@ -885,26 +1166,81 @@ hipError_t more_tokens(const MoeArgs& a, hipStream_t st) {
 }
 
 template <typename T>
+hipError_t long_batch(const LongArgs& a, hipStream_t st) {
+  constexpr int H = sizeof(T) == 2 ? 2 : 1;
+  const size_t up_lds = long_slab<1>() + align_up(static_cast<size_t>(a.m.T) * a.m.K * sizeof(uint16_t), 16);
+  const size_t down_lds = long_slab<H>();
+  auto up = k_moe_up_long<T>;
+  auto down = k_moe_down_long<T>;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(up), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                     static_cast<int>(up_lds));
+  if (e != hipSuccess) return e;
+  e = hipFuncSetAttribute(reinterpret_cast<const void*>(down), hipFuncAttributeMaxDynamicSharedMemorySize,
+                          static_cast<int>(down_lds));
+  if (e != hipSuccess) return e;
+  k_moe_list<<<1, kListWaves * kWave, 0, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  up<<<kCus, kRowWaves * kWave, up_lds, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  down<<<kCus, kRowWaves * kWave, down_lds, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t quads = static_cast<int64_t>(a.m.T) * a.m.d / 4;
+  k_moe_sum<T><<<static_cast<unsigned>((quads + 255) / 256), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T>
 hipError_t experts(const MoeArgs& a, hipStream_t st) {
   if (a.T <= kFewTokens) return few_tokens<T>(a, st);
   return a.T <= 64 ? more_tokens<T, 2>(a, st) : more_tokens<T, 1>(a, st);
 }
 
-// Workspace of one launch: [h][tickets][partial sums], each 256-byte aligned.
-size_t parts(int32_t d, int32_t f, int32_t T, int32_t K, size_t* ticket, size_t* partial) {
-  const size_t h = align_up(static_cast<size_t>(T) * K * f * 4, kAlign);
-  *ticket = h;
-  *partial = h + align_up(static_cast<size_t>((d + 31) / 32) * sizeof(uint32_t), kAlign);
-  return *partial + align_up(static_cast<size_t>(down_shape(d, T).splits) * T * d * sizeof(float), kAlign);
+// Tokens of one launch of a long batch: as many as 256 MB of h hold (the weights
+// in use are read once per launch).
+int32_t long_tokens(int32_t f, int32_t K) {
+  const int64_t fit = (int64_t{1} << 28) / (static_cast<int64_t>(K) * f * 4);
+  return fit < kLongTokens ? static_cast<int32_t>(fit) : kLongTokens;
+}
+
+// Workspace of one launch, its parts 256-byte aligned: [h][tickets][partial sums],
+// or of a long batch [h][plan][places' tokens][weights][pairs' places][products].
+struct Parts {
+  size_t ticket, partial, plan, tok, weight, place_of, bytes;
+};
+Parts parts(int32_t d, int32_t f, int32_t T, int32_t K) {
+  Parts p = {};
+  const size_t pairs = static_cast<size_t>(T) * K;
+  size_t at = align_up(pairs * f * 4, kAlign);
+  auto take = [&](size_t n) {
+    const size_t o = at;
+    at += align_up(n, kAlign);
+    return o;
+  };
+  if (T <= kMoeTokens) {
+    p.ticket = take(static_cast<size_t>((d + 31) / 32) * sizeof(uint32_t));
+    p.partial = take(static_cast<size_t>(down_shape(d, T).splits) * T * d * sizeof(float));
+  } else {
+    p.plan = take(sizeof(LongPlan));
+    p.tok = take(pairs * sizeof(uint16_t) + 2);
+    p.weight = take(pairs * sizeof(float));
+    p.place_of = take(pairs * sizeof(int32_t));
+    p.partial = take(pairs * d * sizeof(float));
+  }
+  p.bytes = at;
+  return p;
 }
 
 }  // namespace
 
 size_t moe_workspace_bytes(int32_t d, int32_t f, fm_dtype, int32_t T, int32_t K) {
-  // what the largest launch needs, and any smaller one
-  size_t most = 0, p, k;
+  // what the largest launch needs, and any smaller one; a long batch always gets
+  // a whole launch's, so that one size serves all of them
+  size_t most = T > kMoeTokens ? parts(d, f, long_tokens(f, K), K).bytes : 0;
   for (int32_t t : {kFewTokens, 64, kMoeTokens}) {
-    const size_t n = parts(d, f, T < t ? T : t, K, &p, &k);
+    const size_t n = parts(d, f, T < t ? T : t, K).bytes;
     most = n > most ? n : most;
   }
   return most;
@@ -915,11 +1251,13 @@ hipError_t launch_moe_experts(const fm_expert_cache& c, const void* x, const int
                               hipStream_t st) {
   const size_t es = c.dtype == FM_BF16 ? 2 : 4;
   const size_t row = static_cast<size_t>(c.d) * es;
-  for (int32_t t0 = 0; t0 < T; t0 += kMoeTokens) {
-    MoeArgs a;
-    a.T = T - t0 < kMoeTokens ? T - t0 : kMoeTokens;
-    size_t ticket, partial;
-    parts(c.d, c.f, a.T, K, &ticket, &partial);
+  const int32_t most = long_tokens(c.f, K);
+  char* base = static_cast<char*>(ws);
+  for (int32_t t0 = 0; t0 < T; t0 += most) {
+    LongArgs l;
+    MoeArgs& a = l.m;
+    a.T = T - t0 < most ? T - t0 : most;
+    const Parts p = parts(c.d, c.f, a.T, K);
     const DownShape s = down_shape(c.d, a.T);
     a.slots = static_cast<const char*>(c.slots);
     a.slot_of = c.slot_of;
@@ -928,9 +1266,9 @@ hipError_t launch_moe_experts(const fm_expert_cache& c, const void* x, const int
     a.weight = weight + static_cast<int64_t>(t0) * K;
     a.residual = residual == nullptr ? nullptr : static_cast<const char*>(residual) + t0 * row;
     a.out = static_cast<char*>(out) + t0 * row;
-    a.h = static_cast<char*>(ws);
-    a.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + partial);
-    a.ticket = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + ticket);
+    a.h = base;
+    a.partial = reinterpret_cast<float*>(base + p.partial);
+    a.ticket = reinterpret_cast<uint32_t*>(base + p.ticket);
     a.flags = flags;
     a.K = K;
     a.E = c.E;
@@ -939,7 +1277,16 @@ hipError_t launch_moe_experts(const fm_expert_cache& c, const void* x, const int
     a.f = c.f;
     a.splits = s.splits;
     a.row_blocks = s.blocks;
-    const hipError_t e = c.dtype == FM_BF16 ? experts<uint16_t>(a, st) : experts<float>(a, st);
+    hipError_t e;
+    if (a.T <= kMoeTokens) {
+      e = c.dtype == FM_BF16 ? experts<uint16_t>(a, st) : experts<float>(a, st);
+    } else {
+      l.plan = reinterpret_cast<LongPlan*>(base + p.plan);
+      l.tok = reinterpret_cast<uint16_t*>(base + p.tok);
+      l.weight = reinterpret_cast<float*>(base + p.weight);
+      l.place_of = reinterpret_cast<int32_t*>(base + p.place_of);
+      e = c.dtype == FM_BF16 ? long_batch<uint16_t>(l, st) : long_batch<float>(l, st);
+    }
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
