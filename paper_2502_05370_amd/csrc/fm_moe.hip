@@ -559,7 +559,7 @@ struct Slab {
 // next(slab) sets the slab after the one it set last (false: none left);
 // done(acc) takes the sums after a slab that is the last.  Called by the whole
 // workgroup; buf holds two slabs of columns.
-template <typename T, int C, int H, int R, int SG, int HINT, typename Next, typename Done>
+template <typename T, int C, int H, int R, int SG, typename Next, typename Done>
 __device__ __forceinline__ void stream_slabs(__amdgpu_buffer_rsrc_t rs_b, unsigned char* buf, Next next, Done done) {
   constexpr int kChunks = SG * 8;                       // 16-byte pieces of a column in a slab
   constexpr int kCol = SG * RowPairs::kBytes + 16;      // (the odd piece keeps the columns' banks apart)
@@ -594,7 +594,7 @@ __device__ __forceinline__ void stream_slabs(__amdgpu_buffer_rsrc_t rs_b, unsign
   auto load_w = [&](int p) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
-      slab.rows[r].template load<HINT>(slab.w, slab.k + p * RowPairs::kBytes, slab.k_end, fw[p][r]);
+      slab.rows[r].template load<kStream>(slab.w, slab.k + p * RowPairs::kBytes, slab.k_end, fw[p][r]);
   };
   raw_barrier();   // the buffers are free
   if (!next(slab)) return;
@@ -657,11 +657,11 @@ __device__ __forceinline__ void aim_columns(uint32_t (&col)[H][C], int n, int p0
 }
 
 // Units of one entry and 128 M gate and up rows, 16 M of each per wavefront, for
-// the entries e0 .. e1 - 1 (all of C tiles); workgroup `me` of `grid` takes every
-// grid-th one.  HINT: whether other workgroups read the weights too.
-template <typename T, int C, int SG, int M, int HINT, typename Places>
-__device__ __forceinline__ void up_rows(const MoeArgs& a, const Places& pl, int e0, int e1, int me, int grid,
-                                        unsigned char* buf) {
+// the entries e0 .. e1 - 1 (all of C tiles).  Workgroup `me` of `grid` takes every
+// grid-th unit, counted on from the `dealt` units before; returns the units dealt.
+template <typename T, int C, int SG, int M, typename Places>
+__device__ __forceinline__ int up_rows(const MoeArgs& a, const Places& pl, int e0, int e1, int dealt, int me, int grid,
+                                       unsigned char* buf) {
   constexpr int kRows = 16 * M * kRowWaves;
   constexpr int R = 2 * M;
   const int lane = threadIdx.x % kWave;
@@ -669,9 +669,8 @@ __device__ __forceinline__ void up_rows(const MoeArgs& a, const Places& pl, int 
   const uint32_t rb = static_cast<uint32_t>(a.d) * sizeof(T);
   const int blocks = (a.f + kRows - 1) / kRows;
   const int slabs = static_cast<int>((rb + SG * RowPairs::kBytes - 1) / (SG * RowPairs::kBytes));
-  const int u_end = e1 * blocks;
-  int u = e0 * blocks;
-  u += (me - u % grid + grid) % grid;
+  const int units = (e1 - e0) * blocks;
+  const int u = (me - dealt % grid + grid) % grid;
   const size_t slot_bytes = static_cast<size_t>(3) * a.d * a.f * sizeof(T);
   int at = u;      // the unit of the slab set last,
   int i = -1;      // and that slab among the unit's
@@ -682,10 +681,10 @@ __device__ __forceinline__ void up_rows(const MoeArgs& a, const Places& pl, int 
       i = 0;
       at += grid;
     }
-    if (at >= u_end) return false;
+    if (at >= units) return false;
     if (i == 0) {   // (the unit's other slabs find this set)
-      const int e = e0 + Places::entry(at - e0 * blocks, blocks, e1 - e0);
-      const int blk = Places::block(at - e0 * blocks, blocks, e1 - e0);
+      const int e = e0 + Places::entry(at, blocks, e1 - e0);
+      const int blk = Places::block(at, blocks, e1 - e0);
       s.w = row_buffer(a.slots + __builtin_amdgcn_readfirstlane(pl.entry_slot[e]) * slot_bytes,
                        static_cast<uint32_t>(slot_bytes));
 #pragma unroll
@@ -704,8 +703,8 @@ __device__ __forceinline__ void up_rows(const MoeArgs& a, const Places& pl, int 
     return true;
   };
   auto done = [&](floatx4 (&acc)[R][C]) __attribute__((always_inline)) {
-    const int e = e0 + Places::entry(unit - e0 * blocks, blocks, e1 - e0);
-    const int row0 = Places::block(unit - e0 * blocks, blocks, e1 - e0) * kRows + 16 * wv * M + 4 * (lane / 16);
+    const int e = e0 + Places::entry(unit, blocks, e1 - e0);
+    const int row0 = Places::block(unit, blocks, e1 - e0) * kRows + 16 * wv * M + 4 * (lane / 16);
     unit += grid;
 #pragma unroll
     for (int j = 0; j < C; ++j) {
@@ -727,7 +726,8 @@ __device__ __forceinline__ void up_rows(const MoeArgs& a, const Places& pl, int 
       }
     }
   };
-  stream_slabs<T, C, 1, R, SG, HINT>(row_buffer(a.x, static_cast<uint32_t>(a.T) * rb), buf, next, done);
+  stream_slabs<T, C, 1, R, SG>(row_buffer(a.x, static_cast<uint32_t>(a.T) * rb), buf, next, done);
+  return dealt + units;
 }
 
 constexpr int slab_bytes(int C, int H, int SG) { return 2 * H * C * 16 * (SG * 128 + 16); }
@@ -738,9 +738,9 @@ __global__ void __launch_bounds__(kRowWaves * kWave, 4) k_moe_up_rows(MoeArgs a)
   __shared__ __align__(16) unsigned char buf[slab_bytes(4, 1, 2) > slab_bytes(2, 1, 4) ? slab_bytes(4, 1, 2) : slab_bytes(2, 1, 4)];
   make_plan<kMoeTokens, kRowWaves * kWave>(a, pl);
   const int me = static_cast<int>(blockIdx.x), grid = static_cast<int>(gridDim.x);
-  up_rows<T, 1, 4, 1, kStream>(a, pl, 0, pl.classes[0], me, grid, buf);
-  up_rows<T, 2, 4, 1, kStream>(a, pl, pl.classes[0], pl.classes[1], me, grid, buf);
-  up_rows<T, 4, 2, 1, kStream>(a, pl, pl.classes[1], pl.classes[2], me, grid, buf);
+  int dealt = up_rows<T, 1, 4, 1>(a, pl, 0, pl.classes[0], 0, me, grid, buf);
+  dealt = up_rows<T, 2, 4, 1>(a, pl, pl.classes[0], pl.classes[1], dealt, me, grid, buf);
+  up_rows<T, 4, 2, 1>(a, pl, pl.classes[1], pl.classes[2], dealt, me, grid, buf);
 }
 
 // Load groups [u, u1) of the concatenated entries, those among entries e0 .. e1 - 1
@@ -796,7 +796,7 @@ __device__ __forceinline__ void down_rows(const MoeArgs& a, const Plan<kMoeToken
     }
   };
   const uint32_t h_bytes = static_cast<uint32_t>(static_cast<size_t>(a.T) * a.K * a.f * 4);
-  stream_slabs<T, C, H, R, SG, kStream>(row_buffer(a.h, h_bytes), buf, next, done);
+  stream_slabs<T, C, H, R, SG>(row_buffer(a.h, h_bytes), buf, next, done);
 }
 
 // A workgroup owns 128 R output rows and one of the splits' shares of the load
@@ -988,8 +988,16 @@ __device__ __forceinline__ int xcd_order() {
 
 template <int H>
 constexpr int long_slab() {
-  constexpr int a = slab_bytes(2, H, 4), b = slab_bytes(8, H, 2);
+  constexpr int a = slab_bytes(4, H, 4), b = slab_bytes(8, H, 2);
   return a > b ? a : b;
+}
+
+// Whether units of twice `rows` rows end sooner: per row they cost three quarters
+// (an activation out of LDS feeds four matrix instructions instead of two), but
+// there are half as many to deal among the workgroups.
+__device__ __forceinline__ bool wide_units(int entries, int all_rows, int rows, int grid) {
+  auto turns = [&](int n) { return (entries * ((all_rows + n - 1) / n) + grid - 1) / grid; };
+  return 3 * turns(2 * rows) <= 2 * turns(rows);
 }
 
 // The entries from the plan into LDS.
@@ -1014,19 +1022,22 @@ __global__ void __launch_bounds__(kRowWaves * kWave, 2) k_moe_up_long(LongArgs a
   const LongPlaces pl{entries[0], entries[1], entries[2], tok, a.weight};
   const int32_t* cl = a.plan->classes;
   const int me = xcd_order(), grid = static_cast<int>(gridDim.x);
-  up_rows<T, 8, 2, 2, kKeep>(a.m, pl, cl[2], cl[3], me, grid, smem);
-  up_rows<T, 4, 2, 2, kKeep>(a.m, pl, cl[1], cl[2], me, grid, smem);
-  up_rows<T, 2, 4, 2, kKeep>(a.m, pl, cl[0], cl[1], me, grid, smem);
-  up_rows<T, 1, 4, 2, kKeep>(a.m, pl, 0, cl[0], me, grid, smem);
+  int dealt;
+  if (wide_units(cl[3] - cl[2], a.m.f, 16 * kRowWaves, grid))
+    dealt = up_rows<T, 8, 2, 2>(a.m, pl, cl[2], cl[3], 0, me, grid, smem);
+  else
+    dealt = up_rows<T, 8, 2, 1>(a.m, pl, cl[2], cl[3], 0, me, grid, smem);
+  dealt = up_rows<T, 4, 4, 1>(a.m, pl, cl[1], cl[2], dealt, me, grid, smem);
+  dealt = up_rows<T, 2, 4, 1>(a.m, pl, cl[0], cl[1], dealt, me, grid, smem);
+  up_rows<T, 1, 4, 1>(a.m, pl, 0, cl[0], dealt, me, grid, smem);
 }
 
-// Units of one entry and 512 output rows, 64 per wavefront; each place's product
-// goes to its own row.
-template <typename T, int C, int SG>
-__device__ __forceinline__ void down_long(const MoeArgs& a, const LongPlaces& pl, int e0, int e1, int me, int grid,
-                                          unsigned char* buf) {
+// Units of one entry and 128 R output rows, 16 R per wavefront, dealt as up_rows
+// deals them; each place's product goes to its own row.
+template <typename T, int C, int R, int SG>
+__device__ __forceinline__ int down_long(const MoeArgs& a, const LongPlaces& pl, int e0, int e1, int dealt, int me,
+                                         int grid, unsigned char* buf) {
   constexpr int H = sizeof(T) == 2 ? 2 : 1;   // planes of h
-  constexpr int R = 4;
   constexpr int kRows = 16 * R * kRowWaves;
   const int lane = threadIdx.x % kWave;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -1034,9 +1045,8 @@ __device__ __forceinline__ void down_long(const MoeArgs& a, const LongPlaces& pl
   const uint32_t plane = static_cast<uint32_t>(a.T) * a.K * rb;
   const int blocks = (a.d + kRows - 1) / kRows;
   const int slabs = static_cast<int>((rb + SG * RowPairs::kBytes - 1) / (SG * RowPairs::kBytes));
-  const int u_end = e1 * blocks;
-  int u = e0 * blocks;
-  u += (me - u % grid + grid) % grid;
+  const int units = (e1 - e0) * blocks;
+  const int u = (me - dealt % grid + grid) % grid;
   const size_t slot_elems = static_cast<size_t>(3) * a.d * a.f;
   const uint32_t down_bytes = static_cast<uint32_t>(static_cast<size_t>(a.d) * a.f * sizeof(T));
   int at = u, i = -1, turn = 0, unit = u;
@@ -1045,10 +1055,10 @@ __device__ __forceinline__ void down_long(const MoeArgs& a, const LongPlaces& pl
       i = 0;
       at += grid;
     }
-    if (at >= u_end) return false;
+    if (at >= units) return false;
     if (i == 0) {
-      const int e = e0 + LongPlaces::entry(at - e0 * blocks, blocks, e1 - e0);
-      const int blk = LongPlaces::block(at - e0 * blocks, blocks, e1 - e0);
+      const int e = e0 + LongPlaces::entry(at, blocks, e1 - e0);
+      const int blk = LongPlaces::block(at, blocks, e1 - e0);
       s.w = row_buffer(a.slots + (__builtin_amdgcn_readfirstlane(pl.entry_slot[e]) * slot_elems +
                                   static_cast<size_t>(2) * a.d * a.f) * sizeof(T), down_bytes);
 #pragma unroll
@@ -1064,8 +1074,8 @@ __device__ __forceinline__ void down_long(const MoeArgs& a, const LongPlaces& pl
     return true;
   };
   auto done = [&](floatx4 (&acc)[R][C]) __attribute__((always_inline)) {
-    const int e = e0 + LongPlaces::entry(unit - e0 * blocks, blocks, e1 - e0);
-    const int row0 = LongPlaces::block(unit - e0 * blocks, blocks, e1 - e0) * kRows + 16 * R * wv + 4 * (lane / 16);
+    const int e = e0 + LongPlaces::entry(unit, blocks, e1 - e0);
+    const int row0 = LongPlaces::block(unit, blocks, e1 - e0) * kRows + 16 * R * wv + 4 * (lane / 16);
     unit += grid;
 #pragma unroll
     for (int j = 0; j < C; ++j) {
@@ -1078,7 +1088,8 @@ __device__ __forceinline__ void down_long(const MoeArgs& a, const LongPlaces& pl
     }
   };
   const uint32_t h_bytes = static_cast<uint32_t>(static_cast<size_t>(a.T) * a.K * a.f * 4);
-  stream_slabs<T, C, H, R, SG, kKeep>(row_buffer(a.h, h_bytes), buf, next, done);
+  stream_slabs<T, C, H, R, SG>(row_buffer(a.h, h_bytes), buf, next, done);
+  return dealt + units;
 }
 
 template <typename T>
@@ -1090,10 +1101,14 @@ __global__ void __launch_bounds__(kRowWaves * kWave, 2) k_moe_down_long(LongArgs
   const LongPlaces pl{entries[0], entries[1], entries[2], nullptr, nullptr};
   const int32_t* cl = a.plan->classes;
   const int me = xcd_order(), grid = static_cast<int>(gridDim.x);
-  down_long<T, 8, 2>(a.m, pl, cl[2], cl[3], me, grid, smem);
-  down_long<T, 4, 2>(a.m, pl, cl[1], cl[2], me, grid, smem);
-  down_long<T, 2, 4>(a.m, pl, cl[0], cl[1], me, grid, smem);
-  down_long<T, 1, 4>(a.m, pl, 0, cl[0], me, grid, smem);
+  int dealt;
+  if (wide_units(cl[3] - cl[2], a.m.d, 32 * kRowWaves, grid))
+    dealt = down_long<T, 8, 4, 2>(a.m, pl, cl[2], cl[3], 0, me, grid, smem);
+  else
+    dealt = down_long<T, 8, 2, 2>(a.m, pl, cl[2], cl[3], 0, me, grid, smem);
+  dealt = down_long<T, 4, 2, 4>(a.m, pl, cl[1], cl[2], dealt, me, grid, smem);
+  dealt = down_long<T, 2, 2, 4>(a.m, pl, cl[0], cl[1], dealt, me, grid, smem);
+  down_long<T, 1, 2, 4>(a.m, pl, 0, cl[0], dealt, me, grid, smem);
 }
 
 // A token's products, in the order of its experts, and the residual.

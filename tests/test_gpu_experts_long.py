@@ -23,7 +23,9 @@ def _chosen(rng, T, E, K, law):
 @pytest.mark.parametrize("T,d,f,E,K,law", [(129, 8, 8, 1, 1, "even"), (129, 264, 136, 4, 2, "even"),
                                            (257, 72, 264, 7, 3, "skewed"), (300, 1032, 72, 4, 2, "even"),
                                            (700, 136, 520, 9, 2, "skewed"), (1000, 104, 24, 64, 8, "skewed"),
-                                           (640, 512, 256, 5, 1, "even")])
+                                           (640, 512, 256, 5, 1, "even"),
+                                           # enough units of rows for the wide ones, of either product
+                                           (640, 64, 4104, 10, 2, "even"), (640, 8200, 64, 10, 2, "even")])
 def test_long_batch(T, d, f, E, K, law, dtype):
     print(f"experts T={T} d={d} f={f} E={E} K={K} {law} {dtype}", flush=True)
     fm = _fm()
