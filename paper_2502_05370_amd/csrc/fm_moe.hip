@@ -71,6 +71,8 @@ struct Plan {
   float weight[kPairs];            // and its weight
   int32_t again;                   // some token lists an expert twice
   // unit u of n entries of `blocks` row blocks each
+  __device__ __forceinline__ int token(int place) const { return tok[place]; }
+  __device__ __forceinline__ float weight_of(int place) const { return weight[place]; }
   static __device__ __forceinline__ int entry(int u, int blocks, int) { return u / blocks; }
   static __device__ __forceinline__ int block(int u, int blocks, int) { return u % blocks; }
 };
@@ -693,7 +695,7 @@ __device__ __forceinline__ int up_rows(const MoeArgs& a, const Places& pl, int e
         s.rows[M + m] = RowPairs(blk * kRows + 16 * (wv * M + m), a.f, rb, static_cast<uint32_t>(a.f) * rb);
       }
       aim_columns<SG>(s.col, pl.entry_n[e], pl.entry_place[e], 0u,
-                      [&](int p) { return static_cast<uint32_t>(pl.tok[p]) * rb; });
+                      [&](int p) { return static_cast<uint32_t>(pl.token(p)) * rb; });
       turn = static_cast<int>(static_cast<uint32_t>(blk) * 5u % static_cast<uint32_t>(slabs));
     }
     const int q = i + turn < slabs ? i + turn : i + turn - slabs;
@@ -711,7 +713,7 @@ __device__ __forceinline__ int up_rows(const MoeArgs& a, const Places& pl, int e
       const int col = 16 * j + lane % 16;
       if (col >= pl.entry_n[e]) continue;
       const int place = pl.entry_place[e] + col;
-      const float w = pl.weight[place];
+      const float w = pl.weight_of(place);
 #pragma unroll
       for (int m = 0; m < M; ++m) {
         const int row = row0 + 16 * m;
@@ -854,6 +856,12 @@ __global__ void __launch_bounds__(256) k_moe_join(MoeArgs a) {
 // activations out of LDS feeds four matrix instructions, a weight eight.  The
 // places are listed once, by a launch of one workgroup, and each place's product
 // is written by itself; a last launch adds a token's K.
+//
+// 2,048 tokens, two each of 16 experts of 4,096 x 6,400, bf16: 1.11 ms, 582 TFLOP/s
+// (776 with the products of h's second plane; the matrix units work 43-48% of the
+// time); 4,096 tokens 1.90 ms.  A slab and CU load 160 KB, 2.1 us in pairs of lanes,
+// and multiply for 1.7 us.  At 64 tokens this takes 589 us against the few rows'
+// 478, at 128 433 against 439, in float32 at 100 206 against 189.
 constexpr int kLongPlaces = 128;   // of an entry
 constexpr int kLongEntries = kMaxE + kLongTokens * kMaxK / kLongPlaces;
 
@@ -864,52 +872,67 @@ struct LongPlan {
 struct LongArgs {
   MoeArgs m;
   LongPlan* plan;
-  uint16_t* tok;        // [T K] token of each place
-  float* weight;        // and its weight
+  uint16_t* pair_of;    // [T K] pair (T, K) of each place
   int32_t* place_of;    // [T][K] (-1: no product)
 };
 
 constexpr int kListWaves = 16;
+constexpr uint16_t kNone = 0xFFFF;   // (a wavefront's pairs: at most 2,048)
 
 __global__ void __launch_bounds__(kListWaves * kWave) k_moe_list(LongArgs a) {
   __shared__ int32_t count[kListWaves][kMaxE];   // then the next place of each wavefront's share
   __shared__ int32_t slot[kMaxE];
+  // each pair's rank among its wavefront's of the expert, then each place's pair
+  extern __shared__ __align__(16) uint16_t rank[];   // [2][T K], each rounded up to 16 bytes
   const int tid = threadIdx.x;
   const int lane = tid % kWave;
   const int wv = tid / kWave;
   const int pairs = a.m.T * a.m.K;
+  uint16_t* pair_of = rank + (pairs + 7) / 8 * 8;
   if (tid < kMaxE) slot[tid] = tid < a.m.E ? a.m.slot_of[tid] : -1;
   count[wv][lane] = 0;
   __syncthreads();
   const int share = (pairs + kListWaves * kWave - 1) / (kListWaves * kWave) * kWave;
   const int p0 = wv * share;
   const int p1 = p0 + share < pairs ? p0 + share : pairs;
+  constexpr int U = 4;   // steps of 64 pairs whose loads go out together
   uint32_t bad = 0;
-  // a pair's expert, or -1
-  auto expert = [&](int p, bool report) {
-    int e = p < p1 ? a.m.ids[p] : -1;
-    if (e < 0) return -1;
-    const int s = e < a.m.E ? slot[e] : 0;
-    uint32_t b = 0;
-    if (e >= a.m.E || s >= a.m.n_slots) b = FM_FLAG_INDEX_RANGE;
-    else if (s < 0) b = FM_FLAG_EXPERT_MISSING;
-    if (report) bad |= b;
-    return b != 0 ? -1 : e;
-  };
-  // the lanes that hold the same expert
-  auto same = [&](int e) {
-    uint64_t m = __ballot(e >= 0);
+  for (int q = p0; q < p1; q += U * kWave) {
+    int id[U];
 #pragma unroll
-    for (int b = 0; b < 6; ++b) {
-      const uint64_t one = __ballot((e >> b & 1) != 0);
-      m &= (e >> b & 1) != 0 ? one : ~one;
+    for (int u = 0; u < U; ++u) id[u] = q + u * kWave + lane < p1 ? a.m.ids[q + u * kWave + lane] : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = q + u * kWave + lane;
+      if (q + u * kWave >= p1) break;
+      int e = id[u];
+      if (e >= 0) {
+        const int s = e < a.m.E ? slot[e] : 0;
+        const uint32_t b = e >= a.m.E || s >= a.m.n_slots ? FM_FLAG_INDEX_RANGE : (s < 0 ? FM_FLAG_EXPERT_MISSING : 0);
+        bad |= b;
+        if (b != 0) e = -1;
+      }
+      // the lanes that hold the same expert; the first of them counts for all
+      uint64_t m = __ballot(e >= 0);
+#pragma unroll
+      for (int b = 0; b < 6; ++b) {
+        const bool bit = (e >> b & 1) != 0;
+        const uint64_t one = __ballot(bit);
+        m &= bit ? one : ~one;
+      }
+      if (p >= p1) continue;
+      const int before = __popcll(m & ((1ull << lane) - 1ull));
+      if (e < 0) {
+        rank[p] = kNone;
+        continue;
+      }
+      // (a wavefront's LDS accesses happen in its order: every lane reads before
+      // the first one adds)
+      volatile int32_t* c = &count[wv][e];
+      const int n = *c;
+      rank[p] = static_cast<uint16_t>(n + before);
+      if (before == 0) *c = n + __popcll(m);
     }
-    return m;
-  };
-  for (int p = p0; p < p1; p += kWave) {
-    const int e = expert(p + lane, true);
-    const uint64_t m = same(e);
-    if (e >= 0 && (m & ((1ull << lane) - 1ull)) == 0) atomicAdd(&count[wv][e], __popcll(m));
   }
   if (bad != 0 && a.m.flags != nullptr) atomicOr(a.m.flags, bad);
   __syncthreads();
@@ -951,29 +974,29 @@ __global__ void __launch_bounds__(kListWaves * kWave) k_moe_list(LongArgs a) {
     }
   }
   __syncthreads();
-  for (int p = p0; p < p1; p += kWave) {
-    const int e = expert(p + lane, false);
-    const uint64_t m = same(e);
-    const uint64_t before = m & ((1ull << lane) - 1ull);
-    int at = 0;
-    if (e >= 0 && before == 0) at = atomicAdd(&count[wv][e], __popcll(m));
-    at = __shfl(at, m != 0 ? __ffsll(static_cast<long long>(m)) - 1 : 0, kWave) + __popcll(before);
-    if (p + lane < p1) {
-      a.place_of[p + lane] = e >= 0 ? at : -1;
-      if (e >= 0) {
-        a.tok[at] = static_cast<uint16_t>((p + lane) / a.m.K);
-        a.weight[at] = a.m.weight[p + lane];
-      }
-    }
+#pragma unroll 4
+  for (int p = p0 + lane; p < p1; p += kWave) {
+    const int e = a.m.ids[p];
+    const int at = rank[p] != kNone ? count[wv][e] + rank[p] : -1;
+    a.place_of[p] = at;
+    if (at >= 0) pair_of[at] = static_cast<uint16_t>(p);
   }
+  __syncthreads();
+  // (written here in order: places in the pairs' order scatter, and one CU's stores
+  // take a clock per lane then)
+  for (int i = tid; i < (pairs + 1) / 2; i += kListWaves * kWave)
+    reinterpret_cast<uint32_t*>(a.pair_of)[i] = reinterpret_cast<const uint32_t*>(pair_of)[i];
 }
 
 // The list as the products' kernels see it: the entries (and for the gate and up
-// projections the tokens) in LDS, read in every unit.
+// projections the pairs) in LDS, read in every unit.
 struct LongPlaces {
   const int32_t *entry_slot, *entry_place, *entry_n;
-  const uint16_t* tok;
-  const float* weight;
+  const uint16_t* pair_of;
+  const float* weights;   // [T][K]
+  int K;
+  __device__ __forceinline__ int token(int place) const { return pair_of[place] / K; }
+  __device__ __forceinline__ float weight_of(int place) const { return weights[pair_of[place]]; }
   // the entries vary fastest: an expert's are neighbours and read the same
   // weights, in workgroups of one XCD at the same time
   static __device__ __forceinline__ int entry(int u, int, int n) { return u % n; }
@@ -1013,13 +1036,13 @@ __device__ __forceinline__ void stage_entries(const LongPlan& plan, int32_t (*e)
 template <typename T>
 __global__ void __launch_bounds__(kRowWaves * kWave, 2) k_moe_up_long(LongArgs a) {
   __shared__ int32_t entries[3][kLongEntries];
-  extern __shared__ __align__(16) unsigned char smem[];   // [slabs][tokens of the places]
-  uint16_t* tok = reinterpret_cast<uint16_t*>(smem + long_slab<1>());
+  extern __shared__ __align__(16) unsigned char smem[];   // [slabs][pairs of the places]
+  uint32_t* pairs = reinterpret_cast<uint32_t*>(smem + long_slab<1>());
   stage_entries(*a.plan, entries);
-  for (int i = threadIdx.x * 2; i < a.m.T * a.m.K; i += kRowWaves * kWave * 2)
-    *reinterpret_cast<uint32_t*>(tok + i) = *reinterpret_cast<const uint32_t*>(a.tok + i);
+  for (int i = threadIdx.x; i < (a.m.T * a.m.K + 1) / 2; i += kRowWaves * kWave)
+    pairs[i] = reinterpret_cast<const uint32_t*>(a.pair_of)[i];
   __syncthreads();
-  const LongPlaces pl{entries[0], entries[1], entries[2], tok, a.weight};
+  const LongPlaces pl{entries[0], entries[1], entries[2], reinterpret_cast<const uint16_t*>(pairs), a.m.weight, a.m.K};
   const int32_t* cl = a.plan->classes;
   const int me = xcd_order(), grid = static_cast<int>(gridDim.x);
   int dealt;
@@ -1098,7 +1121,7 @@ __global__ void __launch_bounds__(kRowWaves * kWave, 2) k_moe_down_long(LongArgs
   extern __shared__ __align__(16) unsigned char smem[];   // slabs
   stage_entries(*a.plan, entries);
   __syncthreads();
-  const LongPlaces pl{entries[0], entries[1], entries[2], nullptr, nullptr};
+  const LongPlaces pl{entries[0], entries[1], entries[2], nullptr, nullptr, 0};
   const int32_t* cl = a.plan->classes;
   const int me = xcd_order(), grid = static_cast<int>(gridDim.x);
   int dealt;
@@ -1193,7 +1216,11 @@ hipError_t long_batch(const LongArgs& a, hipStream_t st) {
   e = hipFuncSetAttribute(reinterpret_cast<const void*>(down), hipFuncAttributeMaxDynamicSharedMemorySize,
                           static_cast<int>(down_lds));
   if (e != hipSuccess) return e;
-  k_moe_list<<<1, kListWaves * kWave, 0, st>>>(a);
+  const size_t list_lds = align_up(static_cast<size_t>(a.m.T) * a.m.K * sizeof(uint16_t), 16) * 2;
+  e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_moe_list), hipFuncAttributeMaxDynamicSharedMemorySize,
+                          static_cast<int>(list_lds));
+  if (e != hipSuccess) return e;
+  k_moe_list<<<1, kListWaves * kWave, list_lds, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   up<<<kCus, kRowWaves * kWave, up_lds, st>>>(a);
@@ -1221,9 +1248,9 @@ int32_t long_tokens(int32_t f, int32_t K) {
 }
 
 // Workspace of one launch, its parts 256-byte aligned: [h][tickets][partial sums],
-// or of a long batch [h][plan][places' tokens][weights][pairs' places][products].
+// or of a long batch [h][plan][places' pairs][pairs' places][products].
 struct Parts {
-  size_t ticket, partial, plan, tok, weight, place_of, bytes;
+  size_t ticket, partial, plan, pair_of, place_of, bytes;
 };
 Parts parts(int32_t d, int32_t f, int32_t T, int32_t K) {
   Parts p = {};
@@ -1239,8 +1266,7 @@ Parts parts(int32_t d, int32_t f, int32_t T, int32_t K) {
     p.partial = take(static_cast<size_t>(down_shape(d, T).splits) * T * d * sizeof(float));
   } else {
     p.plan = take(sizeof(LongPlan));
-    p.tok = take(pairs * sizeof(uint16_t) + 2);
-    p.weight = take(pairs * sizeof(float));
+    p.pair_of = take((pairs + 1) / 2 * sizeof(uint32_t));
     p.place_of = take(pairs * sizeof(int32_t));
     p.partial = take(pairs * d * sizeof(float));
   }
@@ -1297,8 +1323,7 @@ hipError_t launch_moe_experts(const fm_expert_cache& c, const void* x, const int
       e = c.dtype == FM_BF16 ? experts<uint16_t>(a, st) : experts<float>(a, st);
     } else {
       l.plan = reinterpret_cast<LongPlan*>(base + p.plan);
-      l.tok = reinterpret_cast<uint16_t*>(base + p.tok);
-      l.weight = reinterpret_cast<float*>(base + p.weight);
+      l.pair_of = reinterpret_cast<uint16_t*>(base + p.pair_of);
       l.place_of = reinterpret_cast<int32_t*>(base + p.place_of);
       e = c.dtype == FM_BF16 ? long_batch<uint16_t>(l, st) : long_batch<float>(l, st);
     }
