@@ -446,8 +446,8 @@ size_t fm_moe_workspace_bytes(int32_t d, int32_t f, fm_dtype dtype, int32_t T_ma
  * that every token takes (a shared expert of m times the width) is m experts
  * in every token's list.  Up to 128 tokens (a decode iteration) each expert in
  * use is read once; longer batches (prompts) take passes of up to 4,096 tokens,
- * or of as many as 256 MB hold of K f float32 values.  1 <= K <= 8.  The weights of one slot must
- * not exceed 0xF0000000 bytes.  workspace: at least
+ * or of as many as 256 MB hold of K max(d, f) float32 values.  1 <= K <= 8.  The
+ * weights of one slot must not exceed 0xF0000000 bytes.  workspace: at least
  * fm_moe_workspace_bytes(d, f, dtype, T, K) bytes, rewritten by the call;
  * calls sharing one must be ordered. */
 fm_status fm_moe_experts(const fm_expert_cache* cache, const void* x, const int32_t* ids, const float* weight,

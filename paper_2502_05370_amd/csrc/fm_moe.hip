@@ -1,5 +1,5 @@
-// The chosen experts' products of one MoE layer for the few tokens of a decode
-// iteration, on experts that sit in the slots of an expert cache.
+// The chosen experts' products of one MoE layer, on experts that sit in the slots
+// of an expert cache: for the few tokens of a decode iteration, and for prompts.
 //
 //   h[t,e]  = weight(t,e) * silu(Gate_e x[t]) * (Up_e x[t])
 //   out[t]  = residual[t] + sum over e of Down_e h[t,e]
@@ -13,18 +13,23 @@
 // loads in flight for any number of experts, their sums meet in LDS in a fixed
 // order, and the activations come from the caches.  More tokens take three
 // (k_moe_up_rows, k_moe_down_rows, k_moe_join): the wavefronts own weight rows and
-// share the activations through LDS.
+// share the activations through LDS.  Above 128 the matrix instructions come to
+// bound them, and four launches (k_moe_list, k_moe_up_long, k_moe_down_long,
+// k_moe_sum) take up to 4,096 tokens.
 //
 // Measured, one MI355X, bf16: 8 tokens through 16 experts of 4,096 x 6,400 (1.65
 // GB of weights in use) 162 + 89 us, 6.6 TB/s; 64 tokens through 8 of 4,096 x
 // 14,336 (2.82 GB) 330 + 146 + 5 us, 5.9 TB/s; one token through 4 of 60 of
 // 2,048 x 1,408 (69 MB) 15 + 13 us, of which reading takes 10: the plan, the first
-// loads' latency and the joins of two dependent launches are the rest.
+// loads' latency and the joins of two dependent launches are the rest; 2,048 tokens
+// through 16 of 4,096 x 6,400, two each, 8 + 595 + 490 + 18 us, 584 TFLOP/s.
 //
 // h keeps 16 bits of mantissa in bf16 models: it is stored as the nearest bf16
 // and the nearest bf16 of the rest, both multiplied, so that the only rounding
-// to bf16 that shows is the output's own.  The weights' stream bounds the
-// second product, and the extra matrix instructions hide behind it.
+// to bf16 that shows is the output's own.  With few tokens the weights' stream
+// bounds the second product, and the extra matrix instructions hide behind it; in
+// long batches they are a quarter of all, the price of results that do not depend
+// on the batch's length by more than sums' order.
 #include "fm_internal.h"
 #include "fm_mma.h"
 
@@ -857,11 +862,12 @@ __global__ void __launch_bounds__(256) k_moe_join(MoeArgs a) {
 // places are listed once, by a launch of one workgroup, and each place's product
 // is written by itself; a last launch adds a token's K.
 //
-// 2,048 tokens, two each of 16 experts of 4,096 x 6,400, bf16: 1.11 ms, 582 TFLOP/s
-// (776 with the products of h's second plane; the matrix units work 43-48% of the
-// time); 4,096 tokens 1.90 ms.  A slab and CU load 160 KB, 2.1 us in pairs of lanes,
-// and multiply for 1.7 us.  At 64 tokens this takes 589 us against the few rows'
-// 478, at 128 433 against 439, in float32 at 100 206 against 189.
+// 2,048 tokens, two each of 16 experts of 4,096 x 6,400, bf16: 1.10 ms, 584 TFLOP/s
+// (779 with the products of h's second plane; the matrix units work 43-48% of the
+// time); 4,096 tokens 1.87 ms.  A slab and CU load 160 KB, 2.1 us in pairs of lanes,
+// and multiply for 1.7 us.  Few tokens' kernels against these: 64 tokens through 8
+// of 4,096 x 14,336 478 and 589 us, 128 through 16 of 4,096 x 6,400 439 and 433, in
+// float32 100 through 24 of 2,048 x 1,408 189 and 206.
 constexpr int kLongPlaces = 128;   // of an entry
 constexpr int kLongEntries = kMaxE + kLongTokens * kMaxK / kLongPlaces;
 
@@ -1004,7 +1010,9 @@ struct LongPlaces {
 };
 
 constexpr int kXcds = 8;
-// Consecutive workgroups go to different XCDs; this numbers those of an XCD in a row.
+// Consecutive workgroups go to different XCDs; this numbers those of an XCD in a
+// row, so that an expert's entries share its L2 (2,048 tokens through 8 experts of
+// 4,096 x 14,336: 2.43 -> 2.04 ms).
 __device__ __forceinline__ int xcd_order() {
   return static_cast<int>(blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds);
 }
@@ -1240,10 +1248,10 @@ hipError_t experts(const MoeArgs& a, hipStream_t st) {
   return a.T <= 64 ? more_tokens<T, 2>(a, st) : more_tokens<T, 1>(a, st);
 }
 
-// Tokens of one launch of a long batch: as many as 256 MB of h hold (the weights
-// in use are read once per launch).
-int32_t long_tokens(int32_t f, int32_t K) {
-  const int64_t fit = (int64_t{1} << 28) / (static_cast<int64_t>(K) * f * 4);
+// Tokens of one pass of a long batch: as many as 256 MB hold of h and of the
+// places' products (the weights in use are read once per pass).
+int32_t long_tokens(int32_t d, int32_t f, int32_t K) {
+  const int64_t fit = (int64_t{1} << 28) / (static_cast<int64_t>(K) * (d > f ? d : f) * 4);
   return fit < kLongTokens ? static_cast<int32_t>(fit) : kLongTokens;
 }
 
@@ -1279,7 +1287,7 @@ Parts parts(int32_t d, int32_t f, int32_t T, int32_t K) {
 size_t moe_workspace_bytes(int32_t d, int32_t f, fm_dtype, int32_t T, int32_t K) {
   // what the largest launch needs, and any smaller one; a long batch always gets
   // a whole launch's, so that one size serves all of them
-  size_t most = T > kMoeTokens ? parts(d, f, long_tokens(f, K), K).bytes : 0;
+  size_t most = T > kMoeTokens ? parts(d, f, long_tokens(d, f, K), K).bytes : 0;
   for (int32_t t : {kFewTokens, 64, kMoeTokens}) {
     const size_t n = parts(d, f, T < t ? T : t, K).bytes;
     most = n > most ? n : most;
@@ -1292,7 +1300,7 @@ hipError_t launch_moe_experts(const fm_expert_cache& c, const void* x, const int
                               hipStream_t st) {
   const size_t es = c.dtype == FM_BF16 ? 2 : 4;
   const size_t row = static_cast<size_t>(c.d) * es;
-  const int32_t most = long_tokens(c.f, K);
+  const int32_t most = long_tokens(c.d, c.f, K);
   char* base = static_cast<char*>(ws);
   for (int32_t t0 = 0; t0 < T; t0 += most) {
     LongArgs l;

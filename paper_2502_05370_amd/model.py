@@ -250,7 +250,8 @@ def moe_workspace_bytes(d: int, f: int, dtype: str = "bf16", T_max: int = 256, K
 
 class MoeWorkspace:
     """Device scratch for moe_experts calls of up to T_max tokens of K experts each (every call rewrites what it
-    reads).  Calls sharing one workspace must be ordered."""
+    reads); above 128 tokens one size, of about half a GB at most, serves all.  Calls sharing one workspace must be
+    ordered."""
 
     def __init__(self, cache: ExpertCache, T_max: int = 256, K: int = 8):
         self.nbytes = moe_workspace_bytes(cache.d, cache.f, cache._name(), T_max, K)
@@ -263,7 +264,8 @@ def moe_experts(cache: ExpertCache, x: torch.Tensor, ids: torch.Tensor, weight: 
                 residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                 workspace: Optional[MoeWorkspace] = None, stream=None) -> torch.Tensor:
     """residual + the weighted products of each token's experts: x [T][d], ids [T][K] int32, weight [T][K] float32 as
-    moe_route gives them -> [T][d].  Experts that the cache does not hold are left out and flagged (cache.check())."""
+    moe_route gives them -> [T][d]; T from a decode iteration's few to a prompt's thousands.  Experts that the cache
+    does not hold are left out and flagged (cache.check())."""
     dev = cache.device
     _float_rows(x, "x")
     T = x.shape[0]
