@@ -202,6 +202,7 @@ class ExpertCache:
                                           self.slot_of.data_ptr())
         self.desc = C.byref(self._desc)
         self.workspace = None
+        self._replaced = []   # workspaces that calls of more tokens outgrew
 
     def load(self, expert: int, slot: int, gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor) -> None:
         """Put an expert (gate, up [f][d], down [d][f]) into a slot, on the current stream; an expert that the slot
@@ -231,13 +232,14 @@ class ExpertCache:
 
     def ensure_workspace(self, T: int, K: int, stream=None) -> "MoeWorkspace":
         """The cache's own workspace, made or enlarged for calls of T tokens of K experts each on the stream, which
-        the calls before must be ordered with."""
+        the calls before must be ordered with.  One that is replaced stays allocated as long as the cache: a captured
+        graph may hold its address.  Sizes are of powers of two of tokens, so that few are."""
         old = self.workspace
         if old is None or moe_workspace_bytes(self.d, self.f, self._name(), max(T, 1), K) > old.nbytes:
             with _on(stream):
-                self.workspace = MoeWorkspace(self, max(T, 1), K)
-                if old is not None:   # its memory is given out again after what this stream has waited for
-                    old.buf.record_stream(torch.cuda.current_stream(self.device))
+                self.workspace = MoeWorkspace(self, max(16, 1 << (T - 1).bit_length()), K)
+            if old is not None:
+                self._replaced.append(old)
         return self.workspace
 
     def _name(self) -> str:

@@ -1,0 +1,43 @@
+"""The workspace that an expert cache keeps for calls without one of their own:
+what the binding does with it, with host memory in the GPU's place (CPU only; no
+call is made)."""
+import types
+import weakref
+
+import pytest
+import torch
+
+import paper_2502_05370_amd as fm
+import paper_2502_05370_amd.model as model
+
+
+class _Buffer(torch.Tensor):
+    def record_stream(self, stream):
+        pass
+
+
+@pytest.fixture
+def cache(monkeypatch):
+    monkeypatch.setattr(model, "_aligned_bytes",
+                        lambda nbytes, device: torch.empty(nbytes, dtype=torch.uint8).as_subclass(_Buffer))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=0))
+    return fm.ExpertCache(2, 8, 64, 32, device="cpu")
+
+
+def test_an_enlarged_workspace_keeps_the_replaced_one(cache):
+    """A graph captured around a call holds the address of the workspace that the
+    call used; replays write there whatever calls came in between."""
+    buffers = []
+    for T in (1, 40, 100, 300):
+        buffers.append(weakref.ref(cache.ensure_workspace(T, 2).buf))
+    assert len({id(b()) for b in buffers}) == 4 and all(b() is not None for b in buffers)
+    assert cache.ensure_workspace(7, 2) is cache.workspace
+
+
+def test_few_workspaces_are_made(cache):
+    """Calls of one token more at a time: a buffer for each power of two, and one above 128."""
+    sizes = [cache.ensure_workspace(T, 2).nbytes for T in range(1, 400)]
+    assert sizes == sorted(sizes) and len(set(sizes)) == 5
+    for T, n in enumerate(sizes, 1):
+        assert n >= fm.moe_workspace_bytes(64, 32, "bf16", T, 2)
+    assert cache.ensure_workspace(0, 2) is cache.workspace

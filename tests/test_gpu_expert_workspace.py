@@ -1,0 +1,48 @@
+"""The workspace that an expert cache keeps for calls without one of their own,
+on the GPU: results while graphs hold it."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_operators import _fm, _layer, dev, drawn
+
+pytestmark = pytest.mark.gpu
+
+
+def _calls(rng, E, K, d, f, T):
+    """A filled cache and arguments of a call of T tokens."""
+    cache, _ = _layer(rng, E, E, d, f, "bf16")
+    cache.slot_of.copy_(torch.arange(E, device="cuda", dtype=torch.int32))
+    x, _ = drawn(rng, (T, d), "bf16")
+    ids = dev(np.stack([rng.permutation(E)[:K] for _ in range(T)]).astype(np.int32))
+    return cache, x, ids, torch.rand(T, K, device="cuda")
+
+
+def test_a_graph_outlives_the_growth_of_the_workspace():
+    """A decode call without a workspace of its own, captured; then a prompt, which
+    needs more; then memory that other work takes: replays neither write there nor
+    are disturbed."""
+    fm = _fm()
+    rng = np.random.default_rng(1)
+    T = 3
+    cache, x, ids, w = _calls(rng, 8, 2, 264, 136, 200)
+    y = torch.empty_like(x[:T])
+    want = fm.moe_experts(cache, x[:T], ids[:T], w[:T], workspace=fm.MoeWorkspace(cache, T, 2))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        fm.moe_experts(cache, x[:T], ids[:T], w[:T], out=y)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            fm.moe_experts(cache, x[:T], ids[:T], w[:T], out=y)
+        first = cache.workspace.nbytes
+        for n in (40, 200):
+            fm.moe_experts(cache, x[:n], ids[:n], w[:n])
+        assert cache.workspace.nbytes > first
+        other = [torch.full((first // k,), 85, dtype=torch.uint8, device="cuda") for k in (1, 1, 1, 2, 2) for _ in range(8)]
+        for _ in range(3):
+            y.zero_()
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(y, want) and all((t == 85).all() for t in other)
