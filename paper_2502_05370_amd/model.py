@@ -16,7 +16,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import _DTYPES, _TORCH, _aligned_bytes, _lib, _need, _ptr, _stream
+from . import _DTYPES, _TORCH, _aligned_bytes, _lib, _need, _ptr, _raw_stream, _stream
 
 _CODE = {torch.float32: _lib.FM_F32, torch.bfloat16: _lib.FM_BF16}
 _LIBRARY = _lib.load()
@@ -201,8 +201,9 @@ class ExpertCache:
         self._desc = _lib.ExpertCacheDesc(self.E, self.slots, self.d, self.f, _DTYPES[dtype], self.weights.data_ptr(),
                                           self.slot_of.data_ptr())
         self.desc = C.byref(self._desc)
-        self.workspace = None
-        self._replaced = []   # workspaces that calls of more tokens outgrew
+        self.workspace = None    # of the last call without one of its own
+        self._workspaces = {}    # stream handle -> the workspace of its calls
+        self._replaced = []      # workspaces that calls of more tokens outgrew
 
     def load(self, expert: int, slot: int, gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor) -> None:
         """Put an expert (gate, up [f][d], down [d][f]) into a slot, on the current stream; an expert that the slot
@@ -231,16 +232,29 @@ class ExpertCache:
         return f
 
     def ensure_workspace(self, T: int, K: int, stream=None) -> "MoeWorkspace":
-        """The cache's own workspace, made or enlarged for calls of T tokens of K experts each on the stream, which
-        the calls before must be ordered with.  One that is replaced stays allocated as long as the cache: a captured
-        graph may hold its address.  Sizes are of powers of two of tokens, so that few are."""
-        old = self.workspace
-        if old is None or moe_workspace_bytes(self.d, self.f, self._name(), max(T, 1), K) > old.nbytes:
+        """The cache's own workspace of the stream, made or enlarged for calls of T tokens of K experts each.  Each
+        stream has one, in memory of its own, so that calls on different streams need no order.  One that is replaced
+        stays allocated as long as the cache: a captured graph may hold its address.  Sizes are of powers of two of
+        tokens, so that few are."""
+        handle = self._handle(stream)
+        own = self._workspaces.get(handle)
+        if own is None or moe_workspace_bytes(self.d, self.f, self._name(), max(T, 1), K) > own.nbytes:
+            if own is not None:
+                self._replaced.append(own)
             with _on(stream):
-                self.workspace = MoeWorkspace(self, max(16, 1 << (T - 1).bit_length()), K)
-            if old is not None:
-                self._replaced.append(old)
-        return self.workspace
+                own = self._workspaces[handle] = MoeWorkspace(self, max(16, 1 << (T - 1).bit_length()), K)
+        self.workspace = own
+        return own
+
+    def _handle(self, stream) -> int:
+        """The hipStream_t of ``stream``, or of the current stream of the cache's device (0 for one that is no GPU)."""
+        if stream is not None:
+            return stream.cuda_stream
+        if self.device.type != "cuda":
+            return 0
+        if _raw_stream is None:
+            return torch.cuda.current_stream(self.device).cuda_stream
+        return _raw_stream(self.device.index)
 
     def _name(self) -> str:
         return "bf16" if self.dtype is torch.bfloat16 else "f32"
@@ -267,7 +281,9 @@ def moe_experts(cache: ExpertCache, x: torch.Tensor, ids: torch.Tensor, weight: 
                 workspace: Optional[MoeWorkspace] = None, stream=None) -> torch.Tensor:
     """residual + the weighted products of each token's experts: x [T][d], ids [T][K] int32, weight [T][K] float32 as
     moe_route gives them -> [T][d]; T from a decode iteration's few to a prompt's thousands.  Experts that the cache
-    does not hold are left out and flagged (cache.check())."""
+    does not hold are left out and flagged (cache.check()).  Without ``workspace`` the cache's own of the stream serves
+    the call; replays of a graph that captured such a call must be ordered with each other and with the later calls on
+    the stream of the capture, as with any workspace that they share."""
     dev = cache.device
     _float_rows(x, "x")
     T = x.shape[0]

@@ -41,3 +41,15 @@ def test_few_workspaces_are_made(cache):
     for T, n in enumerate(sizes, 1):
         assert n >= fm.moe_workspace_bytes(64, 32, "bf16", T, 2)
     assert cache.ensure_workspace(0, 2) is cache.workspace
+
+
+def test_streams_share_no_workspace(cache):
+    """Calls on two streams are not ordered, and each writes h, its tickets and its
+    partial sums to the workspace."""
+    one, two = (types.SimpleNamespace(cuda_stream=h) for h in (5, 9))
+    a, b, c = cache.ensure_workspace(9, 2, one), cache.ensure_workspace(9, 2, two), cache.ensure_workspace(9, 2)
+    spans = sorted((w.buf.data_ptr(), w.buf.data_ptr() + w.nbytes) for w in (a, b, c))
+    assert spans[0][1] <= spans[1][0] and spans[1][1] <= spans[2][0]
+    assert cache.ensure_workspace(3, 2, one) is a and cache.ensure_workspace(3, 2, two) is b
+    assert cache.ensure_workspace(3, 2) is c and cache.workspace is c
+    assert cache.ensure_workspace(300, 2, two) is not b and cache.ensure_workspace(3, 2, one) is a

@@ -1,5 +1,5 @@
 """The workspace that an expert cache keeps for calls without one of their own,
-on the GPU: results while graphs hold it."""
+on the GPU: results while graphs hold it, and on streams that are not ordered."""
 import numpy as np
 import pytest
 import torch
@@ -46,3 +46,28 @@ def test_a_graph_outlives_the_growth_of_the_workspace():
             graph.replay()
             side.synchronize()
             assert torch.equal(y, want) and all((t == 85).all() for t in other)
+
+
+def test_unordered_streams():
+    """Calls of different tokens on two streams at once, on one cache, and the
+    memory of each stream's workspace after the cache is gone."""
+    fm = _fm()
+    rng = np.random.default_rng(2)
+    cache, x, ids, w = _calls(rng, 16, 2, 1032, 520, 24)
+    halves = [(x[:12], ids[:12], w[:12]), (x[12:], ids[12:], w[12:])]
+    ws = fm.MoeWorkspace(cache, 12, 2)
+    want = [fm.moe_experts(cache, *h, workspace=ws) for h in halves]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(40):
+        got[0].append(fm.moe_experts(cache, *halves[0]))
+        got[1].append(fm.moe_experts(cache, *halves[1], stream=side))
+    mine, theirs = (cache.ensure_workspace(12, 2, s) for s in (None, side))
+    assert mine is not theirs
+    lo, n = theirs.buf.data_ptr(), theirs.nbytes
+    del cache, mine, theirs
+    taken = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(20)]
+    assert not any(t.data_ptr() < lo + n and lo < t.data_ptr() + n for t in taken)
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, v) for gs, v in zip(got, want) for g in gs)
