@@ -24,9 +24,9 @@
 // loads' latency and the joins of two dependent launches are the rest; 2,048 tokens
 // through 16 of 4,096 x 6,400, two each, 8 + 595 + 490 + 18 us, 584 TFLOP/s.
 //
-// h keeps 16 bits of mantissa in bf16 models: it is stored as the nearest bf16
-// and the nearest bf16 of the rest, both multiplied, so that the only rounding
-// to bf16 that shows is the output's own.  With few tokens the weights' stream
+// h keeps 16 bits of mantissa in bf16 models: it is stored as the bf16 below it (in
+// magnitude) and the nearest bf16 of the rest, 2^-16 of h at most from it, both
+// multiplied, so that the only rounding to bf16 that shows is the output's own.  With few tokens the weights' stream
 // bounds the second product, and the extra matrix instructions hide behind it; in
 // long batches they are a quarter of all, the price of results that do not depend
 // on the batch's length by more than sums' order.
@@ -238,6 +238,8 @@ __device__ __forceinline__ void clear(floatx4 (&acc)[R][C]) {
     for (int j = 0; j < C; ++j) acc[r][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 }
 
+constexpr uint16_t kNanBf16 = 0x7FC0;
+
 // Four rows of h of one place.
 template <typename T>
 __device__ __forceinline__ void store_h(const MoeArgs& a, int place, int row, floatx4 hv) {
@@ -247,10 +249,11 @@ __device__ __forceinline__ void store_h(const MoeArgs& a, int place, int row, fl
     u16x4 hi, lo;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      hi[r] = to_bf16(hv[r]);
+      // towards zero: a finite h beyond the largest bf16 stays finite
+      hi[r] = hv[r] == hv[r] ? static_cast<uint16_t>(__float_as_uint(hv[r]) >> 16) : kNanBf16;
       // an infinite h has no rest (inf - inf would make it NaN)
       const float rest = hv[r] - bf16_to_f32(hi[r]);
-      lo[r] = __builtin_fabsf(bf16_to_f32(hi[r])) < __builtin_inff() ? to_bf16(rest) : static_cast<uint16_t>(0);
+      lo[r] = __builtin_fabsf(hv[r]) < __builtin_inff() ? to_bf16(rest) : static_cast<uint16_t>(0);
     }
     uint16_t* h = reinterpret_cast<uint16_t*>(a.h);
     *reinterpret_cast<u16x4*>(h + o) = hi;
