@@ -239,6 +239,7 @@ __device__ __forceinline__ void clear(floatx4 (&acc)[R][C]) {
 }
 
 constexpr uint16_t kNanBf16 = 0x7FC0;
+constexpr float kLeast = 0x1p-126f;   // the least normal bf16 (and float32)
 
 // Four rows of h of one place.
 template <typename T>
@@ -251,9 +252,12 @@ __device__ __forceinline__ void store_h(const MoeArgs& a, int place, int row, fl
     for (int r = 0; r < 4; ++r) {
       // towards zero: a finite h beyond the largest bf16 stays finite
       hi[r] = hv[r] == hv[r] ? static_cast<uint16_t>(__float_as_uint(hv[r]) >> 16) : kNanBf16;
-      // an infinite h has no rest (inf - inf would make it NaN)
+      // The rest has h's sign and is zero only if h is, so that its product with an
+      // infinite weight is the first one's infinity, no NaN.  Where nothing is left
+      // (or h is infinite) 2^-126 stands for it, below a float32's normal range.
       const float rest = hv[r] - bf16_to_f32(hi[r]);
-      lo[r] = __builtin_fabsf(hv[r]) < __builtin_inff() ? to_bf16(rest) : static_cast<uint16_t>(0);
+      const float least = hv[r] == 0.0f ? 0.0f : __builtin_copysignf(kLeast, hv[r]);
+      lo[r] = to_bf16(__builtin_fabsf(rest) >= kLeast ? rest : least);
     }
     uint16_t* h = reinterpret_cast<uint16_t*>(a.h);
     *reinterpret_cast<u16x4*>(h + o) = hi;
