@@ -82,6 +82,7 @@ __global__ void __launch_bounds__(kLookThreads) k_embed_lookup(const T* __restri
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (kLookThreads >> lanes_log) + (threadIdx.x >> lanes_log);
   if (t >= n_tok) return;
   const int row = row_of(tokens[t], V, flags);
+  if (row < 0) scale = 0.0f;   // zeros whatever the scale
   const int col0 = (static_cast<int>(blockIdx.y) * U * lanes + (threadIdx.x & (lanes - 1))) * N;
   const T* src = table + static_cast<int64_t>(row < 0 ? 0 : row) * d;
   T* dst = out + t * d;
