@@ -185,7 +185,7 @@ def moe_route(x: torch.Tensor, gate: torch.Tensor, k: int, renorm: bool = False,
 class ExpertCache:
     """Experts of one MoE layer held on the GPU: ``weights`` [slots][3 d f] (a slot is one expert's gate and up
     projections [f][d], then its down projection [d][f], one block), ``slot_of`` [E] int32 (-1: not held).  Both are
-    plain tensors that the owner may also fill itself."""
+    plain tensors that the owner may also fill itself, in place: calls read the memory that they had at first."""
 
     def __init__(self, slots: int, E: int, d: int, f: int, dtype: str = "bf16", device="cuda"):
         self.slots, self.E, self.d, self.f = int(slots), int(E), int(d), int(f)
@@ -195,15 +195,36 @@ class ExpertCache:
             self.device = torch.device("cuda", torch.cuda.current_device())
         if not (1 <= self.E <= 64 and self.slots >= 1) or moe_workspace_bytes(self.d, self.f, dtype, 1, 1) == 0:
             raise ValueError(f"invalid expert cache slots={slots} E={E} d={d} f={f}")
-        self.weights = torch.empty((self.slots, 3 * self.d * self.f), dtype=self.dtype, device=self.device)
-        self.slot_of = torch.full((self.E,), -1, dtype=torch.int32, device=self.device)
+        self._weights = torch.empty((self.slots, 3 * self.d * self.f), dtype=self.dtype, device=self.device)
+        self._slot_of = torch.full((self.E,), -1, dtype=torch.int32, device=self.device)
         self.flags = torch.zeros(1, dtype=torch.int32, device=self.device)
-        self._desc = _lib.ExpertCacheDesc(self.E, self.slots, self.d, self.f, _DTYPES[dtype], self.weights.data_ptr(),
-                                          self.slot_of.data_ptr())
+        self._desc = _lib.ExpertCacheDesc(self.E, self.slots, self.d, self.f, _DTYPES[dtype], self._weights.data_ptr(),
+                                          self._slot_of.data_ptr())
         self.desc = C.byref(self._desc)
         self.workspace = None    # of the last call without one of its own
         self._workspaces = {}    # stream handle -> the workspace of its calls
         self._replaced = []      # workspaces that calls of more tokens outgrew
+
+    @property
+    def weights(self) -> torch.Tensor:
+        return self._weights
+
+    @weights.setter
+    def weights(self, t):
+        self._same(t, self._weights, "weights")
+
+    @property
+    def slot_of(self) -> torch.Tensor:
+        return self._slot_of
+
+    @slot_of.setter
+    def slot_of(self, t):
+        self._same(t, self._slot_of, "slot_of")
+
+    @staticmethod
+    def _same(t, own, name: str) -> None:
+        if t is not own:   # (cache.weights *= 2 ends in such an assignment)
+            raise AttributeError(f"{name} cannot be replaced: write into it")
 
     def load(self, expert: int, slot: int, gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor) -> None:
         """Put an expert (gate, up [f][d], down [d][f]) into a slot, on the current stream; an expert that the slot

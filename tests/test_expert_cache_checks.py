@@ -20,3 +20,18 @@ def test_workspace_on_another_device():
     ws.buf = torch.zeros(8, dtype=torch.uint8)
     with pytest.raises(ValueError, match="workspace must have shape"):
         fm.moe_experts(cache, x, ids, w, workspace=ws)
+
+
+def test_the_memory_that_calls_read_stays_the_caches():
+    """Calls read weights and slots at addresses taken when the cache was made; another
+    tensor in their place would leave those to whatever is allocated there next."""
+    cache = _cache()
+    with pytest.raises(AttributeError, match="slot_of cannot be replaced"):
+        cache.slot_of = torch.arange(4, dtype=torch.int32)
+    with pytest.raises(AttributeError, match="weights cannot be replaced"):
+        cache.weights = torch.zeros_like(cache.weights)
+    cache.slot_of[1] = 0
+    cache.weights[0].fill_(1)
+    cache.weights *= 2
+    assert cache._desc.slot_of == cache.slot_of.data_ptr() and cache._desc.slots == cache.weights.data_ptr()
+    assert cache.slot_of.tolist() == [-1, 0, -1, -1] and (cache.weights[0] == 2).all()
