@@ -137,7 +137,14 @@ class Model:
             found += sum(e in layer.held for e in need)
             x = self._experts(layer, h, ids, weight, need, x)
             loaded += len(need)
-        self.store.insert(maps, query) if self.store.size + B <= c.store else self.store.insert_dedup(maps, query, c.distance)
+        # (a batch slot without a request has no iteration: its map of zeros would be the best match of any request
+        # that is unlike all others)
+        live = [b for b, p in enumerate(prompts) if p]
+        done, keys = (maps, query) if len(live) == B else (maps[live], query[live])
+        if live and self.store.size + len(live) <= c.store:
+            self.store.insert(done, keys)
+        elif live:
+            self.store.insert_dedup(done, keys, c.distance)
         return x, maps, found, loaded - found
 
     def tune(self, tokens, wanted, rate: float) -> float:
