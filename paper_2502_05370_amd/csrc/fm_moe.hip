@@ -6,7 +6,8 @@
 //
 // With few tokens each weight meets a handful of columns, so reading every
 // expert in use once from HBM bounds both products (6 T K d f operations on
-// 6 d f bytes per expert in bf16).  Weights go straight from memory to the
+// 6 d f bytes per expert in bf16; one with more than 64 of up to 128 tokens is
+// read once per 64).  Weights go straight from memory to the
 // registers of the matrix instructions, 16 rows by 128 contiguous bytes per load
 // group.  Up to 16 tokens two launches, k_moe_up (Gate and Up, joined to h) and
 // k_moe_down: the wavefronts of a workgroup split the long axis, which keeps many

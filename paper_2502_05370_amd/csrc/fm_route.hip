@@ -6,9 +6,10 @@
 // A batch of decode tokens is bound by latency (one workgroup reads E d values,
 // 246 KB for 60 experts of 2,048: 11 us, 5 of them without the gate), a prefill by
 // reading x (8,192 x 4,096 bf16, 16 experts: 18 us, 3.8 TB/s of x and the gate's
-// 64 MB from the L2).  A workgroup takes 16
-// tokens per tile; its wavefronts split d, so that every load of a decode call
-// is in flight at once, and join their sums in LDS in a fixed order.  One
+// 64 MB from the L2).  A workgroup takes 16 tokens per tile; its wavefronts split d, so that the loads of a decode call are
+// in flight at once (of rows of up to 4 KB; longer ones take another turn per 4 KB),
+// and join their sums in LDS in a fixed order.  One workgroup thus reads the whole
+// gate for up to 16 tokens: the time grows with E d (64 experts of 8,192: 28 us).  One
 // wavefront then holds one token's logits, an expert per lane.
 #include "fm_internal.h"
 #include "fm_mma.h"
@@ -146,9 +147,15 @@ __global__ void __launch_bounds__(NW * kWave) k_route(RouteArgs a, bool probs_bf
 
 template <typename T, int NE>
 void route(const RouteArgs& a, bool probs_bf16, hipStream_t st) {
-  // Few tokens: every load of the gate in flight at once.  Many: as many
-  // wavefronts per CU on 16 tokens each, or 32 where the gate's tiles outweigh
-  // the tokens' (its lines come from the L2 once per workgroup).
+  // Few tokens: 16 wavefronts on 16 tokens, 4 KB of every row in flight.  Many:
+  // eight wavefronts, two workgroups per CU, on 16 tokens each, or 32 where the
+  // gate's tiles outweigh the tokens' (its lines come from the L2 once per
+  // workgroup).  Us of the first and the second form at 2,048 and 8,192 tokens,
+  // bf16: E 16 d 4,096 9.9 and 10.1, 20.1 and 18.6; E 60 d 2,048 14.7 and 20.0, 30.0
+  // and 22.0; E 32 d 1,024 8.4 and 7.5, 15.1 and 10.9; float32 E 60 d 2,048 21.9 and
+  // 35.6, 43.1 and 39.6.  The first takes a second turn of workgroups only from
+  // 4,097 tokens on and is ahead until then at E 60 (4,096 tokens: 16.2 and 21.4),
+  // while at E 16 they are within 6%.
   constexpr int TT = NE == 4 ? 2 : 1;
   if (a.T <= 2048) {
     k_route<T, 1, NE, 16, 2><<<static_cast<unsigned>((a.T + 15) / 16), 16 * kWave, 0, st>>>(a, probs_bf16);

@@ -6,7 +6,9 @@ Argument marshalling only, as the rest of the binding: every step runs in the
 library's HIP kernels.  Tensors must be contiguous, on one GPU and of the stated
 type; outputs are created unless ``out`` gives them.  Work goes to the current
 stream, or to ``stream``, and memory that a call creates (outputs, scratch,
-workspaces) belongs to the same stream.
+workspaces) belongs to the same stream.  The calls stand outside torch's
+autograd: no output requires a gradient, whatever the inputs do, and embed_grad
+is the lookup's.
 """
 from __future__ import annotations
 
@@ -246,7 +248,8 @@ class ExpertCache:
         self.slot_of[expert] = -1
 
     def check(self, stream=None) -> int:
-        """Synchronise the stream and return the sticky FM_FLAG_* bits of the calls that it has seen, cleared."""
+        """Synchronise the stream and return the sticky FM_FLAG_* bits of the calls that it has seen, cleared.  Calls on
+        other streams must have ended: a bit that one sets in the meantime may be cleared unseen."""
         with _on(stream):
             f = int(self.flags.item())
             self.flags.zero_()
@@ -288,7 +291,7 @@ def moe_workspace_bytes(d: int, f: int, dtype: str = "bf16", T_max: int = 256, K
 class MoeWorkspace:
     """Device scratch for moe_experts calls of up to T_max tokens of K experts each (every call rewrites what it
     reads); above 128 tokens one size, of about half a GB at most, serves all.  Calls sharing one workspace must be
-    ordered."""
+    ordered; the caches of all layers of a model may share one, where each would otherwise make its own."""
 
     def __init__(self, cache: ExpertCache, T_max: int = 256, K: int = 8):
         self.nbytes = moe_workspace_bytes(cache.d, cache.f, cache._name(), T_max, K)
