@@ -263,10 +263,11 @@ class ExpertCache:
         handle = self._handle(stream)
         own = self._workspaces.get(handle)
         if own is None or moe_workspace_bytes(self.d, self.f, self._name(), max(T, 1), K) > own.nbytes:
+            with _on(stream):
+                made = MoeWorkspace(self, max(16, 1 << (T - 1).bit_length()), K)
             if own is not None:
                 self._replaced.append(own)
-            with _on(stream):
-                own = self._workspaces[handle] = MoeWorkspace(self, max(16, 1 << (T - 1).bit_length()), K)
+            own = self._workspaces[handle] = made
         self.workspace = own
         return own
 

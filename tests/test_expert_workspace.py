@@ -53,3 +53,15 @@ def test_streams_share_no_workspace(cache):
     assert cache.ensure_workspace(3, 2, one) is a and cache.ensure_workspace(3, 2, two) is b
     assert cache.ensure_workspace(3, 2) is c and cache.workspace is c
     assert cache.ensure_workspace(300, 2, two) is not b and cache.ensure_workspace(3, 2, one) is a
+
+
+def test_a_workspace_that_cannot_be_made_replaces_nothing(cache, monkeypatch):
+    first = cache.ensure_workspace(3, 2)
+
+    def full(nbytes, device):
+        raise torch.cuda.OutOfMemoryError("no memory")
+    monkeypatch.setattr(model, "_aligned_bytes", full)
+    for _ in range(3):
+        with pytest.raises(torch.cuda.OutOfMemoryError):
+            cache.ensure_workspace(300, 2)
+    assert cache.ensure_workspace(3, 2) is first and cache._replaced == []

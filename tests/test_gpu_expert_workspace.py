@@ -71,3 +71,35 @@ def test_unordered_streams():
     assert not any(t.data_ptr() < lo + n and lo < t.data_ptr() + n for t in taken)
     torch.cuda.synchronize()
     assert all(torch.equal(g, v) for gs, v in zip(got, want) for g in gs)
+
+
+def test_workspaces_made_during_captures():
+    """Captures on a stream that has had no call: the workspace is made there, in
+    the graph's memory, and outlives the graph."""
+    fm = _fm()
+    rng = np.random.default_rng(3)
+    cache, x, ids, w = _calls(rng, 8, 2, 264, 136, 100)
+    want = [fm.moe_experts(cache, x[:n], ids[:n], w[:n], workspace=fm.MoeWorkspace(cache, n, 2)) for n in (5, 100)]
+    outs = [torch.empty_like(v) for v in want]
+    graphs = []
+    for y, n in zip(outs, (5, 100)):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            fm.moe_experts(cache, x[:n], ids[:n], w[:n], out=y)
+        graphs.append(g)
+
+    def replay(which):
+        for i in which:
+            outs[i].zero_()
+            graphs[i].replay()
+            eager = fm.moe_experts(cache, x[:40], ids[:40], w[:40])
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i], want[i])
+            torch.testing.assert_close(eager.float(), want[1][:40].float(), rtol=2.0 ** -7, atol=2.0 ** -10)
+
+    replay([0, 1, 0, 1])
+    graphs[0] = None
+    torch.cuda.empty_cache()
+    held = [torch.full((cache.workspace.nbytes,), 85, dtype=torch.uint8, device="cuda") for _ in range(10)]
+    replay([1, 1])
+    assert all((t == 85).all() for t in held)
