@@ -327,5 +327,5 @@ def moe_experts(cache: ExpertCache, x: torch.Tensor, ids: torch.Tensor, weight: 
     ws = workspace if workspace is not None else cache.ensure_workspace(T, K, stream)
     _need(ws.buf, "workspace", torch.uint8, (ws.nbytes,), dev)
     _call("fm_moe_experts", dev, stream, cache.desc, x.data_ptr(), ids.data_ptr(), weight.data_ptr(), T, K,
-          _ptr(residual), out.data_ptr(), cache.flags.data_ptr(), ws.buf.data_ptr(), ws.nbytes)
+          _ptr(residual), out.data_ptr(), _flags(cache.flags, dev), ws.buf.data_ptr(), ws.nbytes)
     return out

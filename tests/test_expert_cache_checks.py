@@ -35,3 +35,12 @@ def test_the_memory_that_calls_read_stays_the_caches():
     cache.weights *= 2
     assert cache._desc.slot_of == cache.slot_of.data_ptr() and cache._desc.slots == cache.weights.data_ptr()
     assert cache.slot_of.tolist() == [-1, 0, -1, -1] and (cache.weights[0] == 2).all()
+
+
+def test_flags_that_no_kernel_could_write():
+    cache = _cache()
+    x, ids, w = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2)
+    for flags in (torch.zeros(1, dtype=torch.int32, device="meta"), torch.zeros(1), torch.zeros(0, dtype=torch.int32)):
+        cache.flags = flags
+        with pytest.raises(ValueError, match="flags"):
+            fm.moe_experts(cache, x, ids, w)
