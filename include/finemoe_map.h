@@ -84,6 +84,8 @@ typedef enum { FM_PRI_PREFETCH = 0, FM_PRI_EVICT = 1, FM_PRI_ENUM_INT32_ = 0x7ff
 #define FM_FLAG_VALUE_RANGE   0x8u   /* a float32 map or trajectory-query value exceeds 8 in magnitude (gate
                                         probabilities lie in [0, 1]); float32 trajectory scores are then unspecified */
 #define FM_FLAG_EXPERT_MISSING 0x10u /* fm_moe_experts: an expert that a token takes is in no slot (left out) */
+#define FM_FLAG_PAGES_FULL     0x20u /* fm_kv_resize: a slot's tokens found no page or passed its table (not added) */
+#define FM_FLAG_PAGE_SHARED    0x40u /* fm_kv_write: a token lies in a page that several slots hold (not written) */
 
 typedef struct fm_store fm_store;   /* opaque host-side handle */
 
@@ -458,6 +460,186 @@ size_t fm_moe_workspace_bytes(int32_t d, int32_t f, fm_dtype dtype, int32_t T_ma
 fm_status fm_moe_experts(const fm_expert_cache* cache, const void* x, const int32_t* ids, const float* weight,
                          int32_t T, int32_t K, const void* residual, void* out, uint32_t* flags, void* workspace,
                          size_t workspace_bytes, void* stream);
+
+/* ---- Attention of one new token over a paged cache --------------------
+ *
+ * The other half of a serving iteration's layer: keys and values of a batch's
+ * requests in pages, and each request's new token attending to its own.  Under
+ * the conventions of the model operators above: the current device must hold
+ * every buffer, flags is a device uint32 or NULL, sums are float32, results do
+ * not depend on timing.
+ *
+ * A cache serves n_slots requests (batch slots).  Slot s holds length[s]
+ * tokens; token t lies in page table[s][t / page], at place t % page.  A page
+ * holds `page` tokens of all layers and heads as one block, so that copying or
+ * moving it is one copy.  Several slots may hold the same page (after
+ * fm_kv_fork): refs[p] counts them, and a page with refs[p] == 0 is free.  A
+ * caller starts with length and refs of zeros and a table of -1, and may fill
+ * or restore the arrays itself as long as they agree; pages need no
+ * initialisation.  Table entries from a slot's last page on are -1.
+ *
+ * Layout of a page: [layers][2: keys, values][heads][page / 16 blocks of 16
+ * tokens], every block in pieces of 1 KB that hold 64 bytes of each of its
+ * tokens' rows (head_dim is padded with zeros to such a multiple): 32 bf16 or
+ * 16 float32 values.  With n = 16 / sizeof(element) and lane = 0..63, a piece p
+ * of keys holds at 16-byte place `lane` the dimensions 4 n p + n (lane / 16) ..
+ * + n - 1 of token lane % 16; a piece of values holds there, for i = 0 ..
+ * n / 4 - 1 and j = 0..3, dimension 4 n p + 16 i + lane % 16 of token
+ * 4 (lane / 16) + j at element 4 i + j.
+ *
+ * Calls that change a cache (fm_kv_resize, _fork, _compact, _copy, _write) must
+ * be ordered with every other call on it; the others need no order among
+ * themselves.  A page number outside [0, n_pages) in a visible place of a table
+ * is never followed: its tokens are left out and FM_FLAG_INDEX_RANGE is set.
+ * Lengths are taken as clamped to [0, max_pages * page]. */
+typedef struct {
+    int32_t n_slots;     /* requests, 1..65536 */
+    int32_t max_pages;   /* pages of one slot, >= 1; max_pages * page <= 2^30, n_slots * max_pages <= 2^28 */
+    int32_t n_pages;     /* pages of the pool, 1..2^24 */
+    int32_t page;        /* tokens of a page, a multiple of 16 in 16..1024 */
+    int32_t layers;      /* 1..1024 */
+    int32_t heads;       /* key (and value) heads, 1..1024 */
+    int32_t head_dim;    /* a multiple of 8 in 8..256 */
+    fm_dtype dtype;      /* of keys and values, and of queries and outputs */
+    void* pages;         /* device [n_pages][fm_kv_page_bytes(...)], 256-byte aligned */
+    int32_t* table;      /* device [n_slots][max_pages] */
+    int32_t* length;     /* device [n_slots] */
+    int32_t* refs;       /* device [n_pages] */
+} fm_kv_cache;
+
+/* Bytes of one page (at most 2^31).  Returns 0 for sizes that the calls below refuse. */
+size_t fm_kv_page_bytes(int32_t layers, int32_t heads, int32_t head_dim, int32_t page, fm_dtype dtype);
+
+/* Bytes of scratch (device memory owned by the caller, 256-byte aligned,
+ * rewritten by every call) for fm_kv_resize, _fork, _compact and _copy on a
+ * cache of these sizes (its pointers are not looked at).  Returns 0 for sizes
+ * that they refuse. */
+size_t fm_kv_scratch_bytes(const fm_kv_cache* cache);
+
+/* Tokens come and go: delta[s] > 0 makes room for that many tokens behind slot
+ * s, delta[s] < 0 drops its last -delta[s] (all of them if it has fewer: any
+ * request ends with -2^31), 0 leaves it alone.  delta: device [n_slots] int32.
+ * Dropping comes first: pages without a token left are released (refs - 1).
+ * Then slots grow in order of their numbers.  New pages are the free ones of
+ * the lowest numbers (that are free after the drops); a partly filled last page
+ * that other slots hold too is copied to a new page first, so that no token is
+ * ever added to a shared page (slots that share one and grow in the same call
+ * get a copy each, and the original is released if all of its holders do).
+ * A slot whose pages do not fit any more is refused (its length, pages and the
+ * free ones stay), and so is every later one that needs a page; one that would
+ * pass max_pages is refused alone.  Refusals set FM_FLAG_PAGES_FULL.
+ * granted_out: device [n_slots] uint8 or NULL: 1 where tokens were added, else
+ * 0: the `active` of the calls that follow. */
+fm_status fm_kv_resize(const fm_kv_cache* cache, const int32_t* delta, uint8_t* granted_out, uint32_t* flags,
+                       void* scratch, size_t scratch_bytes, void* stream);
+
+/* Slots go on from other slots: slot s becomes what slot parent[s] was before
+ * the call, sharing its pages, and releases its own.  parent: device [n_slots]
+ * int32; -1 (or s itself) leaves slot s alone; a parent >= n_slots does too and
+ * sets FM_FLAG_INDEX_RANGE.  Any parents are fine: many of one, chains, cycles. */
+fm_status fm_kv_fork(const fm_kv_cache* cache, const int32_t* parent, uint32_t* flags, void* scratch,
+                     size_t scratch_bytes, void* stream);
+
+/* Live pages to the front: of the n pages that are held, those numbered n and
+ * above move to the free numbers below n, in order, and the tables follow, so
+ * that the pool's upper part is free (for expert slots, say).  Entries that a
+ * slot does not use are left as they are if they are -1.  live_out: device int32 or
+ * NULL: n. */
+fm_status fm_kv_compact(const fm_kv_cache* cache, int32_t* live_out, uint32_t* flags, void* scratch,
+                        size_t scratch_bytes, void* stream);
+
+/* Contents of page src[i] to page dst[i], i < n <= n_pages; tables and counts
+ * stay.  src, dst: device [n] int32.  A pair is left out, and sets
+ * FM_FLAG_INDEX_RANGE, if one of its pages is outside the pool, or its
+ * destination occurs again among the sources or destinations. */
+fm_status fm_kv_copy(const fm_kv_cache* cache, const int32_t* src, const int32_t* dst, int32_t n, uint32_t* flags,
+                     void* scratch, size_t scratch_bytes, void* stream);
+
+/* Keys and values of new tokens into their pages of one layer.  k, v: device
+ * [T][heads][head_dim] of the cache's dtype, rows of k_stride and v_stride
+ * elements (the parts of one projection's output, say), 16-byte aligned, strides
+ * multiples of 16 bytes.  offsets NULL: T = n_slots, and row s is slot s's last token.  Otherwise
+ * offsets: device [n_slots + 1] int32, clamped to [0, T], and rows offsets[s]
+ * .. offsets[s + 1] - 1 are the last tokens of slot s (an end before its start:
+ * none).  active: device [n_slots] uint8 or NULL; a slot with 0 writes nothing,
+ * nor does one without a token (offsets NULL).  A slot with more rows than
+ * tokens writes nothing and sets FM_FLAG_INDEX_RANGE; tokens in a page that
+ * several slots hold are not written and set FM_FLAG_PAGE_SHARED. */
+fm_status fm_kv_write(const fm_kv_cache* cache, int32_t layer, const void* k, int64_t k_stride, const void* v,
+                      int64_t v_stride, const int32_t* offsets, int32_t T, const uint8_t* active, uint32_t* flags,
+                      void* stream);
+
+/* The reverse of fm_kv_write: the slots' last tokens out of their pages (to
+ * store a prefix elsewhere, say).  Arguments as there; rows that it would not
+ * write are not touched, tokens in shared pages are read. */
+fm_status fm_kv_read(const fm_kv_cache* cache, int32_t layer, void* k, int64_t k_stride, void* v, int64_t v_stride,
+                     const int32_t* offsets, int32_t T, const uint8_t* active, uint32_t* flags, void* stream);
+
+/* Bytes of workspace (device memory owned by the caller, 256-byte aligned,
+ * rewritten by every call) for fm_attn_decode calls with q_heads query heads on
+ * a cache of these sizes.  Returns 0 for sizes that it refuses. */
+size_t fm_attn_workspace_bytes(const fm_kv_cache* cache, int32_t q_heads);
+
+/* Attention of every slot's last token over the slot's tokens in one layer:
+ *   out[s][h] = sum over j of p_j v_j / sum over j of p_j,   p_j = exp(scale q[s][h] . k_j),
+ * j from max(0, first[s], length[s] - window if window > 0) up to length[s] - 1;
+ * query head h reads key head h / (q_heads / heads).  q: device
+ * [n_slots][q_heads][head_dim] of the cache's dtype, 16-byte aligned, rows of
+ * q_stride elements (a multiple of 16 bytes); q_heads a multiple of heads, at
+ * most 1024.  first: device [n_slots] int32 or NULL.  active: device
+ * [n_slots] uint8 or NULL: a slot with 0 has no query.  out: device
+ * [n_slots][q_heads][head_dim] of the cache's dtype, apart from q, 16-byte
+ * aligned.  lse_out: device [n_slots][q_heads] float32 or NULL: log of the sum
+ * of p_j, for joining with attention over other tokens.  A query that sees no
+ * token, or only tokens whose score is minus infinity, gives zeros and -inf;
+ * tokens outside the range have no part in the result, whatever their pages
+ * hold; other infinities and NaN follow the formula.  bf16 caches: p_j meets
+ * v_j as two bf16 (2^-15 relative).  Calls sharing a workspace must be
+ * ordered. */
+fm_status fm_attn_decode(const fm_kv_cache* cache, int32_t layer, const void* q, int64_t q_stride, int32_t q_heads,
+                         float scale, int32_t window, const int32_t* first, const uint8_t* active, void* out,
+                         float* lse_out, uint32_t* flags, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Norms around a block ----------------------------------------------
+ *
+ * A block's output y joins the residual stream x and the next block's input is
+ * normed, in one pass:
+ *   n[t] = y[t] * rsqrt(mean(y[t]^2) + eps) * post      (post NULL: n = y)
+ *   r[t] = x[t] + scale * gate * n[t]                    (gate NULL: 1)
+ *   h[t] = r[t] * rsqrt(mean(r[t]^2) + eps) * pre        (pre NULL: no h)
+ * y NULL: r = x, the norm before a first block (post and gate NULL, r_out NULL).
+ * gate is [d] (FM_GATE_CHANNEL), [T] (FM_GATE_TOKEN) or [T][d] (FM_GATE_EACH).
+ * All of dtype, d a multiple of 8, [T][d] and [d] tensors 16-byte aligned; h
+ * comes from r before its rounding.  r_out may be x or y, h_out may be y
+ * (no other overlap).  eps >= 0. */
+typedef enum {
+    FM_GATE_NONE = 0, FM_GATE_CHANNEL = 1, FM_GATE_TOKEN = 2, FM_GATE_EACH = 3, FM_GATE_ENUM_INT32_ = 0x7fffffff
+} fm_gate_kind;
+
+fm_status fm_block_norm(const void* x, const void* y, const void* post, const void* gate, fm_gate_kind gate_kind,
+                        float scale, const void* pre, float eps, int32_t T, int32_t d, fm_dtype dtype, void* r_out,
+                        void* h_out, void* stream);
+
+/* Bytes of scratch (device memory owned by the caller, 256-byte aligned,
+ * rewritten by every call) for fm_block_norm_grad calls of up to T_max tokens.
+ * Returns 0 for sizes that it refuses (T_max = 0 is fine). */
+size_t fm_block_norm_scratch_bytes(int32_t T_max, int32_t d);
+
+/* Gradient of fm_block_norm: dr is the gradient of r from elsewhere (NULL:
+ * zeros), dh that of h (NULL exactly where pre is; one of the two is given).
+ * x, y and the rest are the forward call's arguments.  dx, dy (NULL where y
+ * is): device [T][d] of dtype; dpost, dpre, dgate of FM_GATE_CHANNEL: device
+ * [d] float32, sums over the tokens in a fixed order, with accumulate != 0
+ * added to what is there; dgate of FM_GATE_TOKEN: device [T] float32, of
+ * FM_GATE_EACH [T][d] of dtype, both written.  A gradient is given exactly
+ * where its input is.  dx may be dr, dy may be y or dh, dgate of FM_GATE_EACH
+ * may be gate (no other overlap).  T == 0 with accumulate == 0 writes zeros to
+ * the [d] gradients. */
+fm_status fm_block_norm_grad(const void* dr, const void* dh, const void* x, const void* y, const void* post,
+                             const void* gate, fm_gate_kind gate_kind, float scale, const void* pre, float eps,
+                             int32_t T, int32_t d, fm_dtype dtype, int32_t accumulate, void* dx, void* dy,
+                             float* dpost, void* dgate, float* dpre, void* scratch, size_t scratch_bytes,
+                             void* stream);
 
 /* Test support: the dense float32 score matrix of a trajectory (q, depth
  * non-NULL) or semantic (q_sem non-NULL) search, written to scores_out device

@@ -26,6 +26,15 @@ and the model operators around it (paper_2502_05370_amd/model.py):
     probs, ids, w, mask = moe_route(x, gate, k=4)       # a layer's gate: one row of an expert map
     cache = ExpertCache(slots, E, d, f)                 # experts on the GPU
     y = moe_experts(cache, x, ids, w, residual=x)       # the chosen experts' products
+
+with the attention half of a layer (paper_2502_05370_amd/layer.py):
+
+    kv = KvCache(slots, max_tokens, pages, layers, heads, head_dim)   # keys and values in pages
+    active = kv_resize(kv, delta)                       # room for new tokens; dropped ones' pages go back
+    kv_fork(kv, parent); kv_compact(kv)                 # slots that share pages; live pages to the front
+    kv_write(kv, layer, k, v, active=active)            # the new tokens' keys and values
+    y = attn_decode(kv, layer, q, active=active)        # each slot's new token over its own
+    x, h = block_norm(x, y, post, gate, scale, pre)     # y normed, gated, added; the next block's input
 """
 from __future__ import annotations
 
@@ -36,7 +45,8 @@ import torch
 
 from . import _lib
 from ._lib import (FM_BF16, FM_BLEND_NONE, FM_BLEND_SCORE, FM_F32, FM_FLAG_DEPTH_CLAMPED,  # noqa: F401
-                   FM_FLAG_EXPERT_MISSING, FM_FLAG_INDEX_RANGE, FM_FLAG_STATE_STALE, FM_PRI_EVICT, FM_PRI_PREFETCH, FM_TAU_DYNAMIC, FM_TAU_FIXED, FmError, SelectParams)
+                   FM_FLAG_EXPERT_MISSING, FM_FLAG_INDEX_RANGE, FM_FLAG_PAGES_FULL, FM_FLAG_PAGE_SHARED,
+                   FM_FLAG_STATE_STALE, FM_PRI_EVICT, FM_PRI_PREFETCH, FM_TAU_DYNAMIC, FM_TAU_FIXED, FmError, SelectParams)
 
 _lib.load()
 
@@ -46,6 +56,9 @@ __all__ = ["Store", "Workspace", "match_semantic", "match_trajectory", "match_tr
            "map_bytes", "store_bytes", "workspace_bytes", "dedup_scratch_bytes", "traj_state_bytes", "TrajPass",
            "embed_lookup", "embed_pool", "embed_grad", "embed_grad_scratch_bytes", "EmbedGradScratch", "moe_route",
            "ExpertCache", "MoeWorkspace", "moe_workspace_bytes", "moe_experts",
+           "KvCache", "kv_page_bytes", "kv_resize", "kv_fork", "kv_compact", "kv_copy", "kv_write", "kv_read",
+           "AttnWorkspace", "attn_workspace_bytes", "attn_decode",
+           "block_norm", "block_norm_grad", "block_norm_scratch_bytes", "BlockNormScratch",
            "FmError"]
 
 _DTYPES = {"f32": FM_F32, "bf16": FM_BF16}
@@ -505,3 +518,6 @@ def debug_scan_name(L: int, E: int, n: int, B: int, k: int = 1, map_dtype: str =
 
 from .model import (EmbedGradScratch, ExpertCache, MoeWorkspace, embed_grad, embed_grad_scratch_bytes,  # noqa: E402
                     embed_lookup, embed_pool, moe_experts, moe_route, moe_workspace_bytes)
+from .layer import (AttnWorkspace, BlockNormScratch, KvCache, attn_decode, attn_workspace_bytes,  # noqa: E402,F401
+                    block_norm, block_norm_grad, block_norm_scratch_bytes, kv_compact, kv_copy, kv_fork, kv_page_bytes,
+                    kv_read, kv_resize, kv_write)

@@ -23,6 +23,8 @@ FM_FLAG_INDEX_RANGE = 0x2
 FM_FLAG_STATE_STALE = 0x4
 FM_FLAG_VALUE_RANGE = 0x8
 FM_FLAG_EXPERT_MISSING = 0x10
+FM_FLAG_PAGES_FULL = 0x20
+FM_FLAG_PAGE_SHARED = 0x40
 
 STATUS_NAMES = {0: "FM_OK", 1: "FM_ERR_INVALID", 2: "FM_ERR_UNSUPPORTED", 3: "FM_ERR_FULL",
                 4: "FM_ERR_HIP", 5: "FM_ERR_DEVICE"}
@@ -47,6 +49,16 @@ class ExpertCacheDesc(C.Structure):
     _fields_ = [("E", C.c_int32), ("n_slots", C.c_int32), ("d", C.c_int32), ("f", C.c_int32), ("dtype", C.c_int),
                 ("slots", C.c_void_p), ("slot_of", C.c_void_p)]
 
+
+class KvCacheDesc(C.Structure):
+    _fields_ = [("n_slots", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32), ("page", C.c_int32),
+                ("layers", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int),
+                ("pages", C.c_void_p), ("table", C.c_void_p), ("length", C.c_void_p), ("refs", C.c_void_p)]
+
+
+_kv = C.POINTER(KvCacheDesc)
+_i64 = C.c_int64
+_f32 = C.c_float
 
 SIGNATURES = {
     "fm_map_bytes": (_sz, [_i32, _i32, _i32, C.c_int]),
@@ -81,6 +93,20 @@ SIGNATURES = {
                                _vp, _vp]),
     "fm_moe_workspace_bytes": (_sz, [_i32, _i32, C.c_int, _i32, _i32]),
     "fm_moe_experts": (C.c_int, [C.POINTER(ExpertCacheDesc), _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "fm_kv_page_bytes": (_sz, [_i32, _i32, _i32, _i32, C.c_int]),
+    "fm_kv_scratch_bytes": (_sz, [_kv]),
+    "fm_kv_resize": (C.c_int, [_kv, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "fm_kv_fork": (C.c_int, [_kv, _vp, _vp, _vp, _sz, _vp]),
+    "fm_kv_compact": (C.c_int, [_kv, _vp, _vp, _vp, _sz, _vp]),
+    "fm_kv_copy": (C.c_int, [_kv, _vp, _vp, _i32, _vp, _vp, _sz, _vp]),
+    "fm_kv_write": (C.c_int, [_kv, _i32, _vp, _i64, _vp, _i64, _vp, _i32, _vp, _vp, _vp]),
+    "fm_kv_read": (C.c_int, [_kv, _i32, _vp, _i64, _vp, _i64, _vp, _i32, _vp, _vp, _vp]),
+    "fm_attn_workspace_bytes": (_sz, [_kv, _i32]),
+    "fm_attn_decode": (C.c_int, [_kv, _i32, _vp, _i64, _i32, _f32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "fm_block_norm": (C.c_int, [_vp, _vp, _vp, _vp, C.c_int, _f32, _vp, _f32, _i32, _i32, C.c_int, _vp, _vp, _vp]),
+    "fm_block_norm_scratch_bytes": (_sz, [_i32, _i32]),
+    "fm_block_norm_grad": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, C.c_int, _f32, _vp, _f32, _i32, _i32, C.c_int, _i32,
+                                     _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "fm_debug_scores": (C.c_int, [_vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _sz, _vp]),
     "fm_debug_scan_name": (C.c_char_p, [_i32, _i32, _i32, C.c_int, _i32, _i32, _i32, _i32]),
     "fm_debug_scan_events": (C.c_int, [_vp, _vp]),

@@ -24,7 +24,8 @@ BUILD_DIR = os.path.join(HERE, "_build")
 ARCH = "gfx950"
 
 SOURCES = ["fm_api.cpp", "fm_store.hip", "fm_traj.hip", "fm_sem.hip", "fm_sem_mm.hip", "fm_sem_split.hip", "fm_traj_mm.hip", "fm_traj_split.hip", "fm_select.hip", "fm_dedup.hip", "fm_step.hip", "fm_priority.hip",
-           "fm_model_api.cpp", "fm_embed.hip", "fm_route.hip", "fm_moe.hip"]
+           "fm_model_api.cpp", "fm_embed.hip", "fm_route.hip", "fm_moe.hip",
+           "fm_layer_api.cpp", "fm_kv.hip", "fm_attn.hip", "fm_norm.hip"]
 
 # Packed float32 instructions are kept out of every kernel; hipcc's host pass
 # warns that it does not know the feature, which is harmless.

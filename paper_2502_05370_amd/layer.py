@@ -1,0 +1,388 @@
+"""The attention half of a serving iteration's layer: keys and values in pages,
+the attention of each slot's new token over them, and the norms around a block
+with their gradient (fm_kv_*, fm_attn_*, fm_block_norm* of
+include/finemoe_map.h).
+
+Argument marshalling only, under the conventions of model.py.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Tuple
+
+import torch
+
+from . import _DTYPES, _TORCH, _aligned_bytes, _lib, _need, _ptr, _raw_stream
+from .model import _CODE, _call, _flags, _float_rows, _new, _on
+
+
+def kv_page_bytes(layers: int, heads: int, head_dim: int, page: int = 64, dtype: str = "bf16") -> int:
+    return int(_lib.load().fm_kv_page_bytes(layers, heads, head_dim, page, _DTYPES[dtype]))
+
+
+class KvCache:
+    """Keys and values of a batch's requests on the GPU, in pages that all layers of ``page`` tokens share.
+
+    ``pages`` [n_pages][elements of a page], ``table`` [slots][max_pages] int32, ``length`` [slots] int32 (tokens of a
+    slot) and ``refs`` [n_pages] int32 (slots that hold a page) are plain tensors that the owner may also fill itself, in
+    place and in agreement with each other: calls read the memory that they had at first.  Calls that change the cache
+    must be ordered with every other call on it."""
+
+    def __init__(self, slots: int, max_tokens: int, pages: int, layers: int, heads: int, head_dim: int,
+                 dtype: str = "bf16", page: int = 64, device="cuda"):
+        self.slots, self.n_pages, self.page = int(slots), int(pages), int(page)
+        self.layers, self.heads, self.head_dim = int(layers), int(heads), int(head_dim)
+        self.dtype = _TORCH[_DTYPES[dtype]]
+        self.page_bytes = kv_page_bytes(self.layers, self.heads, self.head_dim, self.page, dtype)
+        if self.page_bytes == 0:
+            raise ValueError(f"invalid cache page={page} layers={layers} heads={heads} head_dim={head_dim}")
+        self.max_pages = (int(max_tokens) + self.page - 1) // self.page
+        self._desc = _lib.KvCacheDesc(self.slots, self.max_pages, self.n_pages, self.page, self.layers, self.heads,
+                                      self.head_dim, _DTYPES[dtype], None, None, None, None)
+        self.desc = C.byref(self._desc)
+        scratch = int(_lib.load().fm_kv_scratch_bytes(self.desc))
+        if scratch == 0:
+            raise ValueError(f"invalid cache slots={slots} max_tokens={max_tokens} pages={pages}")
+        self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._pages = _aligned_bytes(self.n_pages * self.page_bytes, self.device).view(self.dtype).view(self.n_pages, -1)
+        self._table = torch.full((self.slots, self.max_pages), -1, dtype=torch.int32, device=self.device)
+        self._length = torch.zeros(self.slots, dtype=torch.int32, device=self.device)
+        self._refs = torch.zeros(self.n_pages, dtype=torch.int32, device=self.device)
+        self.flags = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._scratch = _aligned_bytes(scratch, self.device)
+        for name in ("pages", "table", "length", "refs"):
+            setattr(self._desc, name, getattr(self, name).data_ptr())
+        self._workspaces = {}    # stream handle -> the workspace of its calls
+        self._replaced = []      # workspaces that calls of more query heads outgrew
+
+    @property
+    def pages(self) -> torch.Tensor:
+        return self._pages
+
+    @pages.setter
+    def pages(self, t):
+        self._same(t, self._pages, "pages")
+
+    @property
+    def table(self) -> torch.Tensor:
+        return self._table
+
+    @table.setter
+    def table(self, t):
+        self._same(t, self._table, "table")
+
+    @property
+    def length(self) -> torch.Tensor:
+        return self._length
+
+    @length.setter
+    def length(self, t):
+        self._same(t, self._length, "length")
+
+    @property
+    def refs(self) -> torch.Tensor:
+        return self._refs
+
+    @refs.setter
+    def refs(self, t):
+        self._same(t, self._refs, "refs")
+
+    @staticmethod
+    def _same(t, own, name: str) -> None:
+        if t is not own:   # (cache.length += 1 ends in such an assignment)
+            raise AttributeError(f"{name} cannot be replaced: write into it")
+
+    def check(self, stream=None) -> int:
+        """Synchronise the stream and return the sticky FM_FLAG_* bits of the calls that it has seen, cleared.  Calls on
+        other streams must have ended: a bit that one sets in the meantime may be cleared unseen."""
+        with _on(stream):
+            f = int(self.flags.item())
+            self.flags.zero_()
+        return f
+
+    def ensure_workspace(self, q_heads: int, stream=None) -> "AttnWorkspace":
+        """The cache's own workspace of the stream, made or enlarged for attn_decode calls of q_heads query heads.  Each
+        stream has one; one that is replaced stays allocated as long as the cache: a captured graph may hold its
+        address."""
+        handle = self._handle(stream)
+        own = self._workspaces.get(handle)
+        if own is None or attn_workspace_bytes(self, q_heads) > own.nbytes:
+            with _on(stream):
+                made = AttnWorkspace(self, q_heads)
+            if own is not None:
+                self._replaced.append(own)
+            own = self._workspaces[handle] = made
+        return own
+
+    def _handle(self, stream) -> int:
+        """The hipStream_t of ``stream``, or of the current stream of the cache's device (0 for one that is no GPU)."""
+        if stream is not None:
+            return stream.cuda_stream
+        if self.device.type != "cuda":
+            return 0
+        if _raw_stream is None:
+            return torch.cuda.current_stream(self.device).cuda_stream
+        return _raw_stream(self.device.index)
+
+
+def attn_workspace_bytes(cache: KvCache, q_heads: int) -> int:
+    return int(_lib.load().fm_attn_workspace_bytes(cache.desc, q_heads))
+
+
+class AttnWorkspace:
+    """Device scratch for attn_decode calls of q_heads query heads on a cache (every call rewrites what it reads).
+    Calls sharing one must be ordered; all layers may share one."""
+
+    def __init__(self, cache: KvCache, q_heads: int):
+        self.nbytes = attn_workspace_bytes(cache, q_heads)
+        if self.nbytes == 0:
+            raise ValueError(f"invalid workspace request q_heads={q_heads} for {cache.heads} heads")
+        self.buf = _aligned_bytes(self.nbytes, cache.device)
+
+
+def _change(name: str, cache: KvCache, stream, *args) -> None:
+    _call(name, cache.device, stream, cache.desc, *args, _flags(cache.flags, cache.device), cache._scratch.data_ptr(),
+          cache._scratch.numel())
+
+
+def kv_resize(cache: KvCache, delta: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Room for delta[s] more tokens behind slot s (> 0), or its last -delta[s] dropped (< 0; -2^31 ends any request):
+    delta [slots] int32 -> granted [slots] uint8, 1 where tokens were added: the ``active`` of the calls that follow.
+    Slots that find no free page are refused and flagged (cache.check())."""
+    _need(delta, "delta", torch.int32, (cache.slots,), cache.device)
+    if out is None:
+        out = _new((cache.slots,), torch.uint8, cache.device, stream)
+    else:
+        _need(out, "out", torch.uint8, (cache.slots,), cache.device)
+    _change("fm_kv_resize", cache, stream, delta.data_ptr(), out.data_ptr())
+    return out
+
+
+def kv_fork(cache: KvCache, parent: torch.Tensor, stream=None) -> None:
+    """Slot s becomes what slot parent[s] was, sharing its pages; -1 leaves it alone.  parent [slots] int32."""
+    _need(parent, "parent", torch.int32, (cache.slots,), cache.device)
+    _change("fm_kv_fork", cache, stream, parent.data_ptr())
+
+
+def kv_compact(cache: KvCache, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Move the live pages to the lowest numbers -> how many there are, [1] int32: cache.pages from there on is free."""
+    if out is None:
+        out = _new((1,), torch.int32, cache.device, stream)
+    else:
+        _need(out, "out", torch.int32, (1,), cache.device)
+    _change("fm_kv_compact", cache, stream, out.data_ptr())
+    return out
+
+
+def kv_copy(cache: KvCache, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
+    """Contents of the pages src [n] int32 to the pages dst [n]; tables and counts stay.  Pairs whose destination is
+    named twice, or that name no page, are left out and flagged."""
+    _need(src, "src", torch.int32, (None,), cache.device)
+    _need(dst, "dst", torch.int32, (src.shape[0],), cache.device)
+    _change("fm_kv_copy", cache, stream, src.data_ptr(), dst.data_ptr(), src.shape[0])
+
+
+def _rows(t, name: str, dtype, shape, device) -> Tuple[int, int]:
+    """Address and row stride of a [T][heads][head_dim] tensor whose rows need not follow each other."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
+    if t.device != device or t.dtype != dtype or t.dim() != 3 or any(w is not None and g != w
+                                                                    for g, w in zip(t.shape, shape)):
+        want = "x".join("*" if w is None else str(w) for w in shape)
+        raise ValueError(f"{name} must be a {dtype} [{want}] tensor on {device}, got {t.dtype} {list(t.shape)} on "
+                         f"{t.device}")
+    T, H, D = t.shape
+    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D) or (T > 1 and t.stride(0) < H * D):
+        raise ValueError(f"{name} must have contiguous rows, got strides {t.stride()}")
+    return t.data_ptr(), t.stride(0) if T > 1 else H * D
+
+
+def _token_rows(name: str, cache: KvCache, layer: int, k, v, offsets, active, stream) -> None:
+    dev = cache.device
+    shape = (cache.slots if offsets is None else None, cache.heads, cache.head_dim)
+    ks, vs = _rows(k, "k", cache.dtype, shape, dev), _rows(v, "v", cache.dtype, shape, dev)
+    if k.shape[0] != v.shape[0]:
+        raise ValueError(f"k and v must have as many rows, got {k.shape[0]} and {v.shape[0]}")
+    if offsets is not None:
+        _need(offsets, "offsets", torch.int32, (cache.slots + 1,), dev)
+    if active is not None:
+        _need(active, "active", torch.uint8, (cache.slots,), dev)
+    _call(name, dev, stream, cache.desc, layer, *ks, *vs, _ptr(offsets), k.shape[0], _ptr(active),
+          _flags(cache.flags, dev))
+
+
+def kv_write(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, offsets: Optional[torch.Tensor] = None,
+             active: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Keys and values of new tokens into a layer's pages: k, v [T][heads][head_dim], whose rows may be parts of longer
+    ones.  Without ``offsets`` row s is slot s's last token; otherwise rows offsets[s] .. offsets[s + 1] - 1 are its last
+    ones (offsets [slots + 1] int32).  Slots where active [slots] uint8 is 0 write nothing."""
+    _token_rows("fm_kv_write", cache, layer, k, v, offsets, active, stream)
+
+
+def kv_read(cache: KvCache, layer: int, T: Optional[int] = None, offsets: Optional[torch.Tensor] = None,
+            active: Optional[torch.Tensor] = None, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None):
+    """The reverse of kv_write: -> (k, v), rows that belong to no slot left as they are (zeros without ``out``).  With
+    ``offsets`` and without ``out``, T says how many rows there are."""
+    if out is None:
+        if T is None:
+            if offsets is not None:
+                raise ValueError("offsets need T or out")
+            T = cache.slots
+        with _on(stream):
+            out = tuple(torch.zeros((T, cache.heads, cache.head_dim), dtype=cache.dtype, device=cache.device)
+                        for _ in range(2))
+    elif T is not None and any(t.shape[0] != T for t in out):
+        raise ValueError(f"out must have T={T} rows")
+    _token_rows("fm_kv_read", cache, layer, out[0], out[1], offsets, active, stream)
+    return out
+
+
+def attn_decode(cache: KvCache, layer: int, q: torch.Tensor, scale: Optional[float] = None, window: int = 0,
+                first: Optional[torch.Tensor] = None, active: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                workspace: Optional[AttnWorkspace] = None, stream=None) -> torch.Tensor:
+    """Attention of every slot's last token over the slot's tokens of a layer: q [slots][q_heads][head_dim] (rows may be
+    parts of longer ones) -> [slots][q_heads][head_dim].  scale defaults to head_dim ** -0.5; the last ``window`` tokens
+    are seen (0: all), from place first[s] on (int32 [slots]); slots where active [slots] uint8 is 0, and queries that
+    see no token, give zeros.  ``lse`` [slots][q_heads] float32 takes the log of each query's sum of weights.  Without
+    ``workspace`` the cache's own of the stream serves the call; replays of a graph that captured such a call must be
+    ordered with each other and with the later calls on the stream of the capture."""
+    dev = cache.device
+    q_ptr, q_stride = _rows(q, "q", cache.dtype, (cache.slots, None, cache.head_dim), dev)
+    q_heads = q.shape[1]
+    if out is None:
+        out = _new((cache.slots, q_heads, cache.head_dim), cache.dtype, dev, stream)
+    else:
+        _need(out, "out", cache.dtype, (cache.slots, q_heads, cache.head_dim), dev)
+        if out.data_ptr() == q_ptr:
+            raise ValueError("out must not be q")
+    if first is not None:
+        _need(first, "first", torch.int32, (cache.slots,), dev)
+    if active is not None:
+        _need(active, "active", torch.uint8, (cache.slots,), dev)
+    if lse is not None:
+        _need(lse, "lse", torch.float32, (cache.slots, q_heads), dev)
+    if workspace is None:
+        if q_heads < 1 or q_heads % cache.heads != 0:
+            raise ValueError(f"q has {q_heads} heads, not a multiple of the cache's {cache.heads}")
+        workspace = cache.ensure_workspace(q_heads, stream)
+    _need(workspace.buf, "workspace", torch.uint8, (workspace.nbytes,), dev)
+    _call("fm_attn_decode", dev, stream, cache.desc, layer, q_ptr, q_stride, q_heads,
+          cache.head_dim ** -0.5 if scale is None else scale, window, _ptr(first), _ptr(active), out.data_ptr(),
+          _ptr(lse), _flags(cache.flags, dev), workspace.buf.data_ptr(), workspace.nbytes)
+    return out
+
+
+def _norm_inputs(x, y, post, gate, pre):
+    """Check the inputs that a norm and its gradient share -> the gate's kind."""
+    _float_rows(x, "x")
+    T, d = x.shape
+    dev = x.device
+    if y is not None:
+        _need(y, "y", x.dtype, (T, d), dev)
+    for name, t in (("post", post), ("pre", pre)):
+        if t is not None:
+            _need(t, name, x.dtype, (d,), dev)
+    if gate is None:
+        return 0
+    if not isinstance(gate, torch.Tensor):
+        raise TypeError(f"gate must be a torch.Tensor, got {type(gate).__name__}")
+    kind = {(d,): 1, (T, 1): 2, (T, d): 3}.get(tuple(gate.shape))
+    if kind is None:
+        raise ValueError(f"gate must have shape [{d}], [{T}x1] or [{T}x{d}], got {list(gate.shape)}")
+    _need(gate, "gate", x.dtype, tuple(gate.shape), dev)
+    return kind
+
+
+def block_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None, post: Optional[torch.Tensor] = None,
+               gate: Optional[torch.Tensor] = None, scale: float = 1.0, pre: Optional[torch.Tensor] = None,
+               eps: float = 1e-6, out=None, stream=None):
+    """A block's output into the residual stream, and the norm before the next block, in one pass:
+    r = x + scale * gate * norm(y) * post, h = norm(r) * pre, norm(z) = z / sqrt(mean(z^2) + eps) -> (r, h).
+    x, y [T][d], post and pre [d], gate [d], [T][1] or [T][d].  Without post y is not normed, without pre h is None,
+    without y (the norm before a first block) r is x itself.  ``out`` gives (r, h): r may be x or y, h may be y."""
+    kind = _norm_inputs(x, y, post, gate, pre)
+    T, d = x.shape
+    r, h = (None, None) if out is None else out
+    if y is None:
+        if r is not None and r is not x:
+            raise ValueError("out[0] (r) must be None or x without y")
+        if pre is None or post is not None or kind:
+            raise ValueError("without y there is only the norm by pre")
+        r = None
+    elif r is None:
+        r = _new((T, d), x.dtype, x.device, stream)
+    else:
+        _need(r, "out[0] (r)", x.dtype, (T, d), x.device)
+    if pre is None:
+        if h is not None:
+            raise ValueError("out[1] (h) must be None without pre")
+    elif h is None:
+        h = _new((T, d), x.dtype, x.device, stream)
+    else:
+        _need(h, "out[1] (h)", x.dtype, (T, d), x.device)
+    _call("fm_block_norm", x.device, stream, x.data_ptr(), _ptr(y), _ptr(post), _ptr(gate), kind, scale, _ptr(pre), eps, T,
+          d, _CODE[x.dtype], _ptr(r), _ptr(h))
+    return (x if r is None else r), h
+
+
+def block_norm_scratch_bytes(T_max: int, d: int) -> int:
+    return int(_lib.load().fm_block_norm_scratch_bytes(T_max, d))
+
+
+class BlockNormScratch:
+    """Device scratch for block_norm_grad calls of up to T_max tokens (every call rewrites what it reads).  Calls
+    sharing one must be ordered."""
+
+    def __init__(self, T_max: int, d: int, device="cuda"):
+        self.nbytes = block_norm_scratch_bytes(T_max, d)
+        if self.nbytes == 0:
+            raise ValueError(f"invalid scratch request T_max={T_max} d={d}")
+        self.buf = _aligned_bytes(self.nbytes, device)
+
+
+def block_norm_grad(dr: Optional[torch.Tensor], dh: Optional[torch.Tensor], x: torch.Tensor,
+                    y: Optional[torch.Tensor] = None, post: Optional[torch.Tensor] = None,
+                    gate: Optional[torch.Tensor] = None, scale: float = 1.0, pre: Optional[torch.Tensor] = None,
+                    eps: float = 1e-6, accumulate: bool = False, out=None, scratch: Optional[BlockNormScratch] = None,
+                    stream=None):
+    """Gradient of block_norm, whose inputs come again: dr and dh are the gradients of r and h (dr may be None, dh is
+    given exactly where pre is) -> (dx, dy, dpost, dgate, dpre), None where the input is.  dx and dy are of x's type; dpost,
+    dpre and the gradient of a gate per channel or token float32, of a full gate x's type.  accumulate adds the sums
+    over tokens (dpost, dpre, a channel gate's) to what ``out`` holds.  dx may be dr, dy may be y or dh."""
+    kind = _norm_inputs(x, y, post, gate, pre)
+    T, d = x.shape
+    dev = x.device
+    for name, t in (("dr", dr), ("dh", dh)):
+        if t is not None:
+            _need(t, name, x.dtype, (T, d), dev)
+    if y is None and (post is not None or kind):
+        raise ValueError("post and gate need y")
+    if (dh is None) != (pre is None):
+        raise ValueError("dh must be given exactly where pre is")
+    if dr is None and dh is None:
+        raise ValueError("dr or dh is required")
+    gate_dtype = x.dtype if kind == 3 else torch.float32
+    want = ((T, d), x.dtype, True), ((T, d), x.dtype, y is not None), ((d,), torch.float32, post is not None), \
+        (None if kind == 0 else tuple(gate.shape), gate_dtype, kind != 0), ((d,), torch.float32, pre is not None)
+    names = "dx", "dy", "dpost", "dgate", "dpre"
+    if out is None:
+        if accumulate and (post is not None or pre is not None or kind == 1):
+            raise ValueError("accumulate needs out")
+        out = tuple(_new(shape, dtype, dev, stream) if there else None for shape, dtype, there in want)
+    for i, (t, name, (shape, dtype, there)) in enumerate(zip(out, names, want)):
+        if there:
+            _need(t, f"out[{i}] ({name})", dtype, shape, dev)
+        elif t is not None:
+            raise ValueError(f"out[{i}] ({name}) must be None: its input is")
+    if scratch is None:
+        with _on(stream):
+            scratch = BlockNormScratch(T, d, dev)
+    _need(scratch.buf, "scratch", torch.uint8, (scratch.nbytes,), dev)
+    dx, dy, dpost, dgate, dpre = out
+    _call("fm_block_norm_grad", dev, stream, _ptr(dr), _ptr(dh), x.data_ptr(), _ptr(y), _ptr(post), _ptr(gate), kind,
+          scale, _ptr(pre), eps, T, d, _CODE[x.dtype], 1 if accumulate else 0, dx.data_ptr(), _ptr(dy), _ptr(dpost),
+          _ptr(dgate), _ptr(dpre), scratch.buf.data_ptr(), scratch.nbytes)
+    return out
