@@ -575,9 +575,12 @@ fm_status fm_kv_write(const fm_kv_cache* cache, int32_t layer, const void* k, in
 fm_status fm_kv_read(const fm_kv_cache* cache, int32_t layer, void* k, int64_t k_stride, void* v, int64_t v_stride,
                      const int32_t* offsets, int32_t T, const uint8_t* active, uint32_t* flags, void* stream);
 
-/* Bytes of workspace (device memory owned by the caller, 256-byte aligned,
- * rewritten by every call) for fm_attn_decode calls with q_heads query heads on
- * a cache of these sizes.  Returns 0 for sizes that it refuses. */
+/* Bytes of workspace (device memory owned by the caller, 256-byte aligned) for
+ * fm_attn_decode calls with q_heads query heads on a cache of these sizes.  It
+ * must be zero before its first call; every call leaves its first
+ * FM_ATTN_TICKET_BYTES bytes zero (they count which parts of split sequences are
+ * there) and needs no more.  Returns 0 for sizes that it refuses. */
+#define FM_ATTN_TICKET_BYTES 2048
 size_t fm_attn_workspace_bytes(const fm_kv_cache* cache, int32_t q_heads);
 
 /* Attention of every slot's last token over the slot's tokens in one layer:

@@ -25,6 +25,7 @@ FM_FLAG_VALUE_RANGE = 0x8
 FM_FLAG_EXPERT_MISSING = 0x10
 FM_FLAG_PAGES_FULL = 0x20
 FM_FLAG_PAGE_SHARED = 0x40
+FM_ATTN_TICKET_BYTES = 2048
 
 STATUS_NAMES = {0: "FM_OK", 1: "FM_ERR_INVALID", 2: "FM_ERR_UNSUPPORTED", 3: "FM_ERR_FULL",
                 4: "FM_ERR_HIP", 5: "FM_ERR_DEVICE"}

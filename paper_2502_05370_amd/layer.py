@@ -132,14 +132,15 @@ def attn_workspace_bytes(cache: KvCache, q_heads: int) -> int:
 
 
 class AttnWorkspace:
-    """Device scratch for attn_decode calls of q_heads query heads on a cache (every call rewrites what it reads).
-    Calls sharing one must be ordered; all layers may share one."""
+    """Device scratch for attn_decode calls of q_heads query heads on a cache.  Calls sharing one must be ordered; all
+    layers may share one.  Its first bytes count parts of split sequences: zeros between calls."""
 
     def __init__(self, cache: KvCache, q_heads: int):
         self.nbytes = attn_workspace_bytes(cache, q_heads)
         if self.nbytes == 0:
             raise ValueError(f"invalid workspace request q_heads={q_heads} for {cache.heads} heads")
         self.buf = _aligned_bytes(self.nbytes, cache.device)
+        self.buf[:_lib.FM_ATTN_TICKET_BYTES].zero_()
 
 
 def _change(name: str, cache: KvCache, stream, *args) -> None:
