@@ -55,17 +55,21 @@ struct Seen {
 };
 __device__ __forceinline__ Seen seen_of(const AttnArgs& a, int s) {
   const int32_t len = a.c.tokens(a.c.length[s]);
-  int32_t lo = a.first != nullptr ? a.first[s] : 0;
-  lo = lo < 0 ? 0 : lo;
+  // (a null array's place is taken by the lengths, and what is read there not used)
+  const int32_t from = (a.first != nullptr ? a.first : a.c.length)[s];
+  const uint8_t on = a.active != nullptr ? a.active[s] : 1;
+  int32_t lo = a.first != nullptr && from > 0 ? from : 0;
   if (a.window > 0 && len - a.window > lo) lo = len - a.window;
-  if (a.active != nullptr && a.active[s] == 0) lo = len;
+  if (on == 0) lo = len;
   return Seen{lo, len};
 }
 
 template <typename T, int NP>
 struct Wave {
   static constexpr bool kBf = sizeof(T) == 2;
-  static constexpr int SB = kBf ? 2 : 1;       // blocks of a step
+  // Blocks of a step: 8 KB of keys or more (bf16 takes blocks in pairs), so that a
+  // CU's four wavefronts have 64 KB and more on their way.
+  static constexpr int SB = NP >= 8 ? (kBf ? 2 : 1) : (NP >= 4 ? 2 : (NP == 1 ? 8 : 4));
   static constexpr int OT = NP * (kBf ? 2 : 1);   // tiles of 16 dimensions
   uint32x4 q[NP];
   uint32x4 k[SB][NP], v[SB][NP];
@@ -91,20 +95,34 @@ struct Wave {
       for (int t = 0; t < NP; ++t) s[b] = mma_step<T>(k[b][t], q[t], s[b]);
     }
   }
-  // Scores to probabilities, in place.  MASK: tokens of block b outside [lo[b],
-  // hi[b]) have no part, nor have their values.
-  template <bool MASK>
-  __device__ __forceinline__ void weigh(floatx4 (&s)[SB], float scale2, const int (&lo)[SB], const int (&hi)[SB]) {
+  // Tokens of block b outside [lo[b], hi[b]) have no part, nor have their values.
+  __device__ __forceinline__ void mask(floatx4 (&s)[SB], const int (&lo)[SB], const int (&hi)[SB]) {
     const int row = threadIdx.x % kWave / 16 * 4;
-    float top = -__builtin_inff();
 #pragma unroll
     for (int b = 0; b < SB; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float t = s[b][r] * scale2;
-        if (MASK && !(row + r >= lo[b] && row + r < hi[b])) t = -__builtin_inff();
-        top = fmaxf(top, t);
+        const bool in = row + r >= lo[b] && row + r < hi[b];
+        s[b][r] = in ? s[b][r] : -__builtin_inff();
+#pragma unroll
+        for (int t = 0; t < NP; ++t) {
+          if constexpr (kBf) {
+            const uint32_t keep = in ? 0xFFFFFFFFu : (r % 2 == 0 ? 0xFFFF0000u : 0x0000FFFFu);
+            v[b][t][r / 2] &= keep;
+            v[b][t][2 + r / 2] &= keep;
+          } else {
+            v[b][t][r] = in ? v[b][t][r] : 0u;
+          }
+        }
       }
+  }
+  // Scores (as powers of two) to weights, in place.
+  __device__ __forceinline__ void weigh(floatx4 (&s)[SB]) {
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int b = 0; b < SB; ++b)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, s[b][r]);
     top = max_of_groups(top);
     if (__any(top > m)) {
       const float grown = fmaxf(m, top);
@@ -120,29 +138,9 @@ struct Wave {
     for (int b = 0; b < SB; ++b)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], scale2, -base));
-        if (MASK && !(row + r >= lo[b] && row + r < hi[b])) p = 0.0f;
-        s[b][r] = p;
-        l += p;
+        s[b][r] = __builtin_amdgcn_exp2f(s[b][r] - base);
+        l += s[b][r];
       }
-    if constexpr (MASK) {
-#pragma unroll
-      for (int b = 0; b < SB; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const bool in = row + r >= lo[b] && row + r < hi[b];
-#pragma unroll
-          for (int t = 0; t < NP; ++t) {
-            if constexpr (kBf) {
-              const uint32_t keep = in ? 0xFFFFFFFFu : (r % 2 == 0 ? 0xFFFF0000u : 0x0000FFFFu);
-              v[b][t][r / 2] &= keep;
-              v[b][t][2 + r / 2] &= keep;
-            } else {
-              v[b][t][r] = in ? v[b][t][r] : 0u;
-            }
-          }
-        }
-    }
   }
   __device__ __forceinline__ void add(const floatx4 (&p)[SB]) {
     if constexpr (kBf) {
@@ -151,22 +149,27 @@ struct Wave {
       // infinite value gives infinity and not the NaN of infinity times zero.
       uint32x4 hi, lo;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = p[i / 2][i % 2 * 2], y = p[i / 2][i % 2 * 2 + 1];
-        hi[i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
-        lo[i] = pack_bf16(rest(x, hi[i] << 16), rest(y, hi[i] & 0xFFFF0000u));
-      }
+      for (int b = 0; b < SB; b += 2) {
 #pragma unroll
-      for (int t = 0; t < NP; ++t)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32x4 w = {v[0][t][2 * i], v[0][t][2 * i + 1], v[1][t][2 * i], v[1][t][2 * i + 1]};
-          o[2 * t + i] = mma_step<T>(w, hi, o[2 * t + i]);
-          o[2 * t + i] = mma_step<T>(w, lo, o[2 * t + i]);
+        for (int i = 0; i < 4; ++i) {
+          const float x = p[b + i / 2][i % 2 * 2], y = p[b + i / 2][i % 2 * 2 + 1];
+          hi[i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+          lo[i] = pack_bf16(rest(x, hi[i] << 16), rest(y, hi[i] & 0xFFFF0000u));
         }
+#pragma unroll
+        for (int t = 0; t < NP; ++t)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32x4 w = {v[b][t][2 * i], v[b][t][2 * i + 1], v[b + 1][t][2 * i], v[b + 1][t][2 * i + 1]};
+            o[2 * t + i] = mma_step<T>(w, hi, o[2 * t + i]);
+            o[2 * t + i] = mma_step<T>(w, lo, o[2 * t + i]);
+          }
+      }
     } else {
 #pragma unroll
-      for (int t = 0; t < NP; ++t) o[t] = mma_step<T>(v[0][t], __builtin_bit_cast(uint32x4, p[0]), o[t]);
+      for (int b = 0; b < SB; ++b)
+#pragma unroll
+        for (int t = 0; t < NP; ++t) o[t] = mma_step<T>(v[b][t], __builtin_bit_cast(uint32x4, p[b]), o[t]);
     }
   }
 };
@@ -183,6 +186,9 @@ __device__ __forceinline__ void walk(const AttnArgs& a, Wave<T, NP>& w, int slot
   const int32_t* row = a.c.table + static_cast<int64_t>(slot) * a.c.max_pages;
   const char* keys = a.c.pages + a.c.head_offset(a.layer, 0, head);
   const int64_t to_values = a.c.head_offset(0, 1, 0);
+  // (through an instruction of its own: a plain load next to a vector product is
+  // widened over its neighbours, which puts those into scratch memory)
+  const float scale2 = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(a.scale2)));
   const int b0 = seen.lo / kBlockTokens;
   const int b1 = (seen.hi + kBlockTokens - 1) / kBlockTokens;
 
@@ -213,39 +219,43 @@ __device__ __forceinline__ void walk(const AttnArgs& a, Wave<T, NP>& w, int slot
       at[i] = keys + page * a.c.page_bytes + static_cast<int64_t>(bb - entry * per_page) * block_bytes;
     }
   };
+  // Keys are sent for when the step before has used its own, values likewise.  The
+  // first turn only sends: one copy of the code, which comes from memory when the
+  // caches hold keys.
   const char* at[SB];
-  int lo[SB], hi[SB];
-  if (first >= last) return;
-  locate(first, at, lo, hi);
+  int lo[SB], hi[SB], lo0[SB], hi0[SB];
+  floatx4 s[SB];
+  bool have = false;
+  for (int step = first;; step += stride) {
+    const bool more = step < last;
+    if (!(have || more)) break;
+    if (have) {
+      w.scores(s);
 #pragma unroll
-  for (int i = 0; i < SB; ++i) W::load(at[i], w.k[i]);
-#pragma unroll
-  for (int i = 0; i < SB; ++i) W::load(at[i] + to_values, w.v[i]);
-  for (int step = first; step < last; step += stride) {
-    int lo0[SB], hi0[SB];   // of this step
-#pragma unroll
-    for (int i = 0; i < SB; ++i) {
-      lo0[i] = lo[i];
-      hi0[i] = hi[i];
+      for (int i = 0; i < SB; ++i) {
+        s[i] *= scale2;
+        lo0[i] = lo[i];
+        hi0[i] = hi[i];
+      }
     }
-    const bool more = step + stride < last;
-    floatx4 s[SB];
-    w.scores(s);
     if (more) {
-      locate(step + stride, at, lo, hi);
+      locate(step, at, lo, hi);
 #pragma unroll
       for (int i = 0; i < SB; ++i) W::load(at[i], w.k[i]);
     }
-    bool whole = true;
+    if (have) {
+      bool whole = true;
 #pragma unroll
-    for (int i = 0; i < SB; ++i) whole = whole && lo0[i] <= 0 && hi0[i] >= kBlockTokens;
-    if (whole) w.template weigh<false>(s, a.scale2, lo0, hi0);
-    else w.template weigh<true>(s, a.scale2, lo0, hi0);
-    w.add(s);
+      for (int i = 0; i < SB; ++i) whole = whole && lo0[i] <= 0 && hi0[i] >= kBlockTokens;
+      if (!whole) w.mask(s, lo0, hi0);
+      w.weigh(s);
+      w.add(s);
+    }
     if (more) {
 #pragma unroll
       for (int i = 0; i < SB; ++i) W::load(at[i] + to_values, w.v[i]);
     }
+    have = more;
   }
 }
 
@@ -283,16 +293,12 @@ struct Joined {
 };
 
 // A part in the workspace: m [16], l [16], outputs [queries of a tile][padded row].
-__host__ __device__ inline int64_t part_floats(int32_t group, int dims) {
-  return 32 + static_cast<int64_t>(group < 16 ? group : 16) * dims;
+__host__ __device__ inline uint32_t part_bytes(int32_t group, int dims) {
+  return static_cast<uint32_t>(32 + (group < 16 ? group : 16) * dims) * sizeof(float);
 }
-
-__device__ __forceinline__ void put(float* p, float v) {
-  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float get(const float* p) {
-  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
+// Parts are written and read past the caches of the XCDs (SC1, the bit of accesses
+// of agent scope), 16 bytes a lane.
+constexpr int kAgent = 16;
 
 // How much of a part counts in a sum relative to the maximum `top`.  A part that saw
 // no score has the maximum minus infinity, and one that saw only NaN too.
@@ -300,105 +306,181 @@ __device__ __forceinline__ float share(float m, float l, float top) {
   return m == -__builtin_inff() ? (l == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m - top);
 }
 
-// The four entries of `sh` together: to the output, or as a part to the workspace.
+// Query qi's maximum over the four entries of `sh`, and their sum relative to it.
+template <int DIMS>
+__device__ __forceinline__ float total_of(const Joined<DIMS>& sh, int qi, float (&f)[kAttnWaves], float& top) {
+  top = -__builtin_inff();
+#pragma unroll
+  for (int u = 0; u < kAttnWaves; ++u) top = fmaxf(top, sh.m[u][qi]);
+  float all = 0.0f;
+#pragma unroll
+  for (int u = 0; u < kAttnWaves; ++u) {
+    f[u] = share(sh.m[u][qi], sh.l[u][qi], top);
+    all += f[u] * sh.l[u][qi];
+  }
+  return all;
+}
+
+// The entries of `sh` together, to the output.
 template <typename T, int DIMS>
-__device__ __forceinline__ void finish(const AttnArgs& a, const Joined<DIMS>& sh, int slot, int q0, int queries,
-                                       float* part) {
-  const int quads = a.c.head_dim / 4;
-  for (int i = threadIdx.x; i < queries * quads; i += kAttnWaves * kWave) {
-    const int qi = i / quads, d = i % quads * 4;
-    float top = -__builtin_inff();
-#pragma unroll
-    for (int u = 0; u < kAttnWaves; ++u) top = fmaxf(top, sh.m[u][qi]);
+__device__ __forceinline__ void finish(const AttnArgs& a, const Joined<DIMS>& sh, int row0, int queries) {
+  for (int i = threadIdx.x; i < queries * (DIMS / 4); i += kAttnWaves * kWave) {
+    const int qi = i / (DIMS / 4), d = i % (DIMS / 4) * 4;
+    if (d >= a.c.head_dim) continue;
+    float f[kAttnWaves], top;
+    const float all = total_of<DIMS>(sh, qi, f, top);
     floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-    float all = 0.0f;
 #pragma unroll
-    for (int u = 0; u < kAttnWaves; ++u) {
-      const float f = share(sh.m[u][qi], sh.l[u][qi], top);
-      all += f * sh.l[u][qi];
-      sum += f * *reinterpret_cast<const floatx4*>(&sh.o[u][qi][d]);
-    }
-    if (part != nullptr) {
-      if (d == 0) {
-        put(part + qi, top);
-        put(part + 16 + qi, all);
-      }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) put(part + 32 + qi * DIMS + d + r, sum[r]);
-      continue;
-    }
-    const int64_t at = static_cast<int64_t>(slot) * a.q_heads + q0 + qi;
+    for (int u = 0; u < kAttnWaves; ++u) sum += f[u] * *reinterpret_cast<const floatx4*>(&sh.o[u][qi][d]);
     const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
-    store4<T>(a.out, at * a.c.head_dim + d, all == 0.0f ? zero : sum / all);
+    store4<T>(a.out, static_cast<int64_t>(row0 + qi) * a.c.head_dim + d, all == 0.0f ? zero : sum / all);
     if (d == 0 && a.lse != nullptr)
-      a.lse[at] = all == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(all)) * kLn2;
+      a.lse[row0 + qi] = all == 0.0f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(all)) * kLn2;
   }
 }
 
-// Parts first .. first + n - 1 of a tile (part(i) their addresses) into `sh`, a
-// wavefront every fourth of them.
-template <int DIMS, typename Part>
-__device__ __forceinline__ void collect(const AttnArgs& a, Joined<DIMS>& sh, int queries, int n, Part part) {
-  constexpr int U = 8;   // parts whose loads are in flight together
-  const int lane = threadIdx.x % kWave;
-  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int quads = a.c.head_dim / 4;
-  for (int i = lane; i < queries * quads; i += kWave) {
-    const int qi = i / quads, d = i % quads * 4;
-    float m = -__builtin_inff(), l = 0.0f;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = wv; p0 < n; p0 += U * kAttnWaves) {
-      float pm[U], pl[U];
-      floatx4 po[U];
+// The entries of `sh` together, as a part.
+template <int DIMS>
+__device__ __forceinline__ void store_part(const Joined<DIMS>& sh, int queries, __amdgpu_buffer_rsrc_t rs,
+                                           uint32_t part) {
+  for (int i = threadIdx.x; i < queries * (DIMS / 4); i += kAttnWaves * kWave) {
+    const int qi = i / (DIMS / 4), d = i % (DIMS / 4) * 4;
+    float f[kAttnWaves], top;
+    const float all = total_of<DIMS>(sh, qi, f, top);
+    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int p = p0 + u * kAttnWaves;
-        const float* at = part(p < n ? p : wv);
-        pm[u] = get(at + qi);
-        pl[u] = get(at + 16 + qi);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) po[u][r] = get(at + 32 + qi * DIMS + d + r);
-      }
-      float top = m;
-#pragma unroll
-      for (int u = 0; u < U; ++u) top = p0 + u * kAttnWaves < n ? fmaxf(top, pm[u]) : top;
-      const float f = share(m, l, top);
-      l *= f;
-      o *= f;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (p0 + u * kAttnWaves >= n) continue;
-        const float g = share(pm[u], pl[u], top);
-        l += g * pl[u];
-        o += g * po[u];
-      }
-      m = top;
-    }
-    *reinterpret_cast<floatx4*>(&sh.o[wv][qi][d]) = o;
+    for (int u = 0; u < kAttnWaves; ++u) sum += f[u] * *reinterpret_cast<const floatx4*>(&sh.o[u][qi][d]);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint32x4, sum), rs, static_cast<int>(part + 128u + 16u * i),
+                                           0, kAgent);
     if (d == 0) {
-      sh.m[wv][qi] = m;
-      sh.l[wv][qi] = l;
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(top), rs, static_cast<int>(part + 4u * qi), 0, kAgent);
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(all), rs, static_cast<int>(part + 64u + 4u * qi), 0, kAgent);
     }
   }
+}
+
+// n parts of a tile (part(i) their offsets) into `sh`, a wavefront every fourth of
+// them: 32 parts at a time, whose values are on their way while their maxima and
+// sums decide how much each counts.
+constexpr int kTurn = 32;   // parts
+struct Weights {
+  float top[16][16];       // by group of threads and query
+  float scale[16];         // of what is there already
+  float f[kTurn][16];
+};
+template <int DIMS, typename Part>
+__device__ __forceinline__ void collect(Joined<DIMS>& sh, Weights& wt, int queries, int n, __amdgpu_buffer_rsrc_t rs,
+                                        Part part) {
+  constexpr int U = kTurn / kAttnWaves;   // parts of a wavefront
+  constexpr int E = 2;                    // fours of values of a lane in flight, per part
+  const int tid = threadIdx.x;
+  const int lane = tid % kWave;
+  const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int pg = tid / 16, pq = tid % 16;   // weights: parts pg and pg + 16 of a turn, query pq
+  const int quads = queries * (DIMS / 4);
+  float l = 0.0f, top = -__builtin_inff();   // of query pq; l: this thread's parts
+  for (int p0 = 0; p0 < n; p0 += kTurn) {
+    float m[2], s[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int p = p0 + pg + 16 * j;
+      const bool in = p < n && pq < queries;
+      const uint32_t at = in ? part(p) + 4u * pq : kOutside;
+      m[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, static_cast<int>(at), 0, kAgent));
+      s[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, static_cast<int>(in ? at + 64u : at), 0, kAgent));
+      if (!in) m[j] = -__builtin_inff();
+    }
+    for (int e0 = 0; e0 < quads; e0 += E * kWave) {
+      uint32x4 x[U][E];   // zeros past the parts and past their rows
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int p = p0 + wv + u * kAttnWaves;
+        const uint32_t at = part(p < n ? p : n - 1) + 128u + 16u * (e0 + lane);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          x[u][e] = __builtin_amdgcn_raw_buffer_load_b128(
+              rs, static_cast<int>(p < n && e0 + e * kWave + lane < quads ? at + e * (16u * kWave) : kOutside), 0, kAgent);
+      }
+      if (e0 == 0) {
+        wt.top[pg][pq] = fmaxf(m[0], m[1]);
+        __syncthreads();
+        float now = top;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) now = fmaxf(now, wt.top[j][pq]);
+        l *= share(top, l, now);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float f = share(m[j], s[j], now);
+          wt.f[pg + 16 * j][pq] = f;
+          l += f * s[j];
+        }
+        if (pg == 0) wt.scale[pq] = top == now ? 1.0f : share(top, 1.0f, now);
+        top = now;
+        __syncthreads();
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int i = e0 + e * kWave + lane;
+        if (i >= quads) continue;
+        const int qi = i / (DIMS / 4), d = i % (DIMS / 4) * 4;
+        floatx4* to = reinterpret_cast<floatx4*>(&sh.o[wv][qi][d]);
+        floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+        if (p0 > 0) sum = *to * wt.scale[qi];
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum += wt.f[wv + u * kAttnWaves][qi] * __builtin_bit_cast(floatx4, x[u][e]);
+        *to = sum;
+      }
+    }
+    __syncthreads();
+  }
+  wt.top[pg][pq] = l;
+  __syncthreads();
+  if (pg < kAttnWaves) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum += wt.top[pg * 4 + j][pq];
+    sh.m[pg][pq] = top;
+    sh.l[pg][pq] = sum;
+  }
+  __syncthreads();
+}
+
+// n / d rounded down, d > 0, |n / d| < 2^20, without the long code of a division.
+__device__ __forceinline__ int ratio(int n, int d) {
+  int q = static_cast<int>(static_cast<float>(n) / static_cast<float>(d));
+  while (static_cast<int64_t>(q) * d > n) --q;
+  while (static_cast<int64_t>(q + 1) * d <= n) ++q;
+  return q;
 }
 
 // The batch's work is a line: slot after slot, in it key head after key head (and
 // tile after tile of its queries), in it kOverhead units and one per step.  Every
 // workgroup takes as much of the line, whatever the lengths are.  What it has of a
 // tile is a part; a tile of several workgroups is joined by the last of them that
-// is done (tickets, no wait), in the order of the line.
-constexpr int kWorkers = 512;    // workgroups that the line is cut for: two on every CU
-constexpr int kOverhead = 4;     // units of a tile besides its steps
-constexpr int kLeast = 8;        // units of a workgroup at least
+// is done (tickets, no wait), in the order of the line.  No part is shorter than
+// kPart steps: a cut closer to an end of its tile moves there.
+constexpr int kWorkers = 256;    // workgroups that the line is cut for: one on every CU
+constexpr int kOverhead = 8;     // units of a tile besides its steps
+constexpr int kLeast = 8;        // units of a workgroup at least: few tiles have one each
+constexpr int kPart = 4;
+constexpr int64_t kLongest = int64_t{kWorkers} << 30;   // a workgroup's places are int32
+__device__ __forceinline__ int cut(int x, int steps) {   // x: from the tile's first step on
+  if (x <= 0) return 0;
+  if (x >= steps) return steps;
+  return x < kPart ? 0 : (x > steps - kPart ? steps : x);
+}
 
 template <typename T, int NP>
-__global__ void __launch_bounds__(kAttnWaves* kWave, (Wave<T, NP>::OT <= 10 ? 2 : 1)) k_attn(AttnArgs a, uint32_t* tickets, float* parts) {
+__global__ void __launch_bounds__(kAttnWaves* kWave, 1)
+    k_attn(AttnArgs a, uint32_t* tickets, char* parts, uint32_t parts_bytes) {
   using W = Wave<T, NP>;
   constexpr int kDims = NP * kRowPiece / static_cast<int>(sizeof(T));
   constexpr int NT = kAttnWaves * kWave;
   __shared__ Joined<kDims> sh;
+  __shared__ Weights weights;
   __shared__ int64_t sums[kAttnWaves];
   __shared__ int64_t where[2];
+  __shared__ Seen begin;
   __shared__ int32_t is_last;
   const int tid = threadIdx.x;
   const int lane = tid % kWave;
@@ -409,75 +491,86 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, (Wave<T, NP>::OT <= 10 ? 2 
     const int blocks = w.none() ? 0 : (w.hi + kBlockTokens - 1) / kBlockTokens - w.lo / kBlockTokens;
     return (blocks + W::SB - 1) / W::SB;
   };
-  auto cost_of = [&](int s) __attribute__((always_inline)) {
-    return s < a.c.n_slots ? static_cast<int64_t>(per_slot) * (kOverhead + steps_of(seen_of(a, s))) : int64_t{0};
-  };
-  auto block_sum = [&](int64_t v, int64_t& before) __attribute__((always_inline)) {   // -> all; before: of lower threads
-    int64_t upto = v;
-#pragma unroll
-    for (int m = 1; m < kWave; m <<= 1) {
-      const int64_t o = __shfl_up(upto, m, kWave);
-      if (lane >= m) upto += o;
-    }
-    __syncthreads();
-    if (lane == kWave - 1) sums[wv] = upto;
-    __syncthreads();
-    int64_t all = 0;
-    before = upto - v;
-#pragma unroll
-    for (int w = 0; w < kAttnWaves; ++w) {
-      before += w < wv ? sums[w] : 0;
-      all += sums[w];
-    }
-    return all;
-  };
 
-  // the line's length, and the slot in which this workgroup's piece of it begins
-  const int64_t first_cost = cost_of(tid);
-  int64_t mine = first_cost;
-  for (int s = tid + NT; s < a.c.n_slots; s += NT) mine += cost_of(s);
-  int64_t before;
-  const int64_t total = block_sum(mine, before);
-  int64_t each = (total + kWorkers - 1) / kWorkers;
-  if (each < kLeast) each = kLeast;
-  const int64_t from = each * blockIdx.x;
-  if (from >= total) return;
-  const int64_t to = from + each < total ? from + each : total;
-  int64_t passed = 0;
-  for (int s0 = 0;; s0 += NT) {   // (ends: from < total)
-    const int64_t cost = s0 == 0 ? first_cost : cost_of(s0 + tid);
-    const int64_t all = block_sum(cost, before);
-    if (from >= passed + before && from < passed + before + cost) {
-      where[0] = s0 + tid;
-      where[1] = passed + before;
+  // First pass: the line's length.  Second pass: the slot in which this workgroup's
+  // piece of it begins (slots that one round holds are not summed again).
+  int64_t from = 0;   // the piece: `mine` units from there on
+  int each = 0, mine = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    int64_t passed = 0, cost = 0, before = 0;
+    Seen own{0, 0};
+    auto begins_here = [&](int s) __attribute__((always_inline)) {
+      if (from >= before && from < before + cost) {
+        where[0] = s;
+        where[1] = before - from;
+        begin = own;
+      }
+    };
+    for (int s0 = 0; s0 < a.c.n_slots; s0 += NT) {
+      cost = 0;
+      if (s0 + tid < a.c.n_slots) {
+        own = seen_of(a, s0 + tid);
+        cost = static_cast<int64_t>(per_slot) * (kOverhead + steps_of(own));
+      }
+      int64_t upto = cost;
+#pragma unroll
+      for (int m = 1; m < kWave; m <<= 1) {
+        const int64_t o = __shfl_up(upto, m, kWave);
+        if (lane >= m) upto += o;
+      }
+      __syncthreads();
+      if (lane == kWave - 1) sums[wv] = upto;
+      __syncthreads();
+      before = passed + upto - cost;
+#pragma unroll
+      for (int w = 0; w < kAttnWaves; ++w) {
+        before += w < wv ? sums[w] : 0;
+        passed += sums[w];
+      }
+      if (pass == 1) begins_here(s0 + tid);
+      if (pass == 1 && passed > from) break;
     }
-    passed += all;
-    if (passed > from) break;
+    if (pass == 1) break;
+    each = static_cast<int>((passed + kWorkers - 1) / kWorkers);
+    if (each < kLeast) each = kLeast;
+    from = static_cast<int64_t>(each) * blockIdx.x;
+    if (from >= passed) return;
+    mine = passed - from < each ? static_cast<int>(passed - from) : each;
+    if (a.c.n_slots <= NT) {
+      begins_here(tid);
+      break;
+    }
   }
   __syncthreads();
   int slot = __builtin_amdgcn_readfirstlane(static_cast<int>(where[0]));
-  int64_t slot_at = where[1];
   uint32_t bad = 0;
-  Seen seen = seen_of(a, slot);
-  int steps = steps_of(seen);
-  int64_t k = (from - slot_at) / (kOverhead + steps);   // head and tile of it
-  for (;;) {
-    const int64_t at = slot_at + k * (kOverhead + steps);
-    if (at >= to) break;
-    const int head = __builtin_amdgcn_readfirstlane(static_cast<int>(k) / a.tiles);
-    const int tile = __builtin_amdgcn_readfirstlane(static_cast<int>(k) % a.tiles);
+  Seen seen = begin;
+  int steps = __builtin_amdgcn_readfirstlane(steps_of(seen));
+  // the tile that the piece begins in, and where it begins itself: places are
+  // counted from the piece's begin
+  const int64_t back = -where[1];
+  int tile0 = static_cast<int>(static_cast<float>(back) / static_cast<float>(kOverhead + steps));
+  while (static_cast<int64_t>(tile0) * (kOverhead + steps) > back) --tile0;
+  while (static_cast<int64_t>(tile0 + 1) * (kOverhead + steps) <= back) ++tile0;
+  tile0 = __builtin_amdgcn_readfirstlane(tile0);
+  int at = __builtin_amdgcn_readfirstlane(
+      static_cast<int>(static_cast<int64_t>(tile0) * (kOverhead + steps) - back));
+  int head = tile0 / a.tiles, tile = tile0 % a.tiles;
+  mine = __builtin_amdgcn_readfirstlane(mine);
+  each = __builtin_amdgcn_readfirstlane(each);
+  const uint32_t size = part_bytes(a.group, kDims);
+  const __amdgpu_buffer_rsrc_t rs = row_buffer(parts, parts_bytes);
+  while (at < mine) {
     const int queries = a.group - tile * 16 < 16 ? a.group - tile * 16 : 16;
-    const int q0 = head * a.group + tile * 16;
+    const int row0 = slot * a.q_heads + head * a.group + tile * 16;
     // this workgroup's steps of the tile
-    const int64_t step0 = at + kOverhead;
-    const int lo = __builtin_amdgcn_readfirstlane(from > step0 ? static_cast<int>(from - step0) : 0);
-    const int hi = __builtin_amdgcn_readfirstlane(to - step0 < steps ? static_cast<int>(to - step0) : steps);
-    if (steps == 0 && at >= from) {
+    const int step0 = at + kOverhead;
+    const int lo = cut(-step0, steps);
+    const int hi = cut(mine - step0, steps);
+    if (steps == 0 && at >= 0) {
       for (int i = tid; i < queries * a.c.head_dim / 4; i += NT)
-        store4<T>(a.out, (static_cast<int64_t>(slot) * a.q_heads + q0) * a.c.head_dim + i * 4,
-                  floatx4{0.f, 0.f, 0.f, 0.f});
-      if (a.lse != nullptr && tid < queries)
-        a.lse[static_cast<int64_t>(slot) * a.q_heads + q0 + tid] = -__builtin_inff();
+        store4<T>(a.out, static_cast<int64_t>(row0) * a.c.head_dim + i * 4, floatx4{0.f, 0.f, 0.f, 0.f});
+      if (a.lse != nullptr && tid < queries) a.lse[row0 + tid] = -__builtin_inff();
     }
     if (lo < hi) {
       W w;
@@ -493,64 +586,69 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, (Wave<T, NP>::OT <= 10 ? 2 
 #pragma unroll
       for (int t = 0; t < W::OT; ++t) *reinterpret_cast<floatx4*>(&sh.o[wv][c][16 * t + 4 * g]) = w.o[t];
       __syncthreads();
-      if (lo == 0 && hi == steps) {
-        finish<T, kDims>(a, sh, slot, q0, queries, nullptr);
-      } else {
+      bool ends = lo == 0 && hi == steps;
+      if (!ends) {
         // a workgroup has two parts at most: of a tile that began before its piece
         // of the line, and of one that goes on behind it
-        const int64_t floats = part_floats(a.group, kDims);
-        finish<T, kDims>(a, sh, slot, q0, queries, parts + (2 * static_cast<int64_t>(blockIdx.x) + (lo == 0)) * floats);
-        const int w0 = static_cast<int>(step0 / each), w1 = static_cast<int>((step0 + steps - 1) / each);
+        store_part<kDims>(sh, queries, rs, (2 * blockIdx.x + (lo == 0 ? 1u : 0u)) * size);
+        // the workgroups that have the tile's first part and its last
+        const int w0 = static_cast<int>(blockIdx.x) + ratio(step0 + kPart - 1, each);
+        const int w1 = static_cast<int>(blockIdx.x) + ratio(step0 + steps - kPart, each);
         wait_vmcnt<0>();
         __syncthreads();
         if (tid == 0)
           is_last = __hip_atomic_fetch_add(&tickets[w1], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
                     static_cast<uint32_t>(w1 - w0);
         __syncthreads();
-        if (is_last) {
-          collect<kDims>(a, sh, queries, w1 - w0 + 1, [&](int p) __attribute__((always_inline)) {
-            return parts + (2 * static_cast<int64_t>(w0 + p) + (p == 0)) * floats;
+        ends = is_last != 0;
+        if (ends) {
+          collect<kDims>(sh, weights, queries, w1 - w0 + 1, rs, [&](int p) __attribute__((always_inline)) {
+            return (2u * static_cast<uint32_t>(w0 + p) + (p == 0 ? 1u : 0u)) * size;
           });
-          __syncthreads();
-          finish<T, kDims>(a, sh, slot, q0, queries, nullptr);
           if (tid == 0) __hip_atomic_store(&tickets[w1], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
       }
+      if (ends) finish<T, kDims>(a, sh, row0, queries);
     }
-    if (++k == per_slot) {
-      slot_at += static_cast<int64_t>(per_slot) * (kOverhead + steps);
-      if (slot_at >= to) break;
-      ++slot;
-      seen = seen_of(a, slot);
-      steps = steps_of(seen);
-      k = 0;
+    at += kOverhead + steps;
+    if (++tile == a.tiles) {
+      tile = 0;
+      if (++head == a.c.heads) {
+        head = 0;
+        if (at >= mine) break;
+        ++slot;
+        seen = seen_of(a, slot);
+        steps = __builtin_amdgcn_readfirstlane(steps_of(seen));
+      }
     }
   }
   if (bad != 0 && a.flags != nullptr) atomicOr(a.flags, bad);
 }
+
+uint32_t parts_bytes(int32_t group, int dims) { return 2u * kWorkers * part_bytes(group, dims); }
 
 template <typename T, int NP>
 hipError_t launch(const AttnArgs& a, void* workspace, hipStream_t st) {
   // no more workgroups than the longest line would have pieces
   constexpr int SB = Wave<T, NP>::SB;
   const int64_t longest = kOverhead + 1 + (static_cast<int64_t>(a.c.max_pages) * a.c.page / kBlockTokens + SB) / SB;
-  const int64_t pieces = (longest * a.c.n_slots * a.c.heads * a.tiles + kLeast - 1) / kLeast;
+  const int64_t line = longest * a.c.n_slots * a.c.heads * a.tiles;
+  if (line >= kLongest) return hipErrorInvalidValue;
+  const int64_t pieces = (line + kLeast - 1) / kLeast;
   uint32_t* tickets = static_cast<uint32_t*>(workspace);
-  float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + align_up(kWorkers * sizeof(uint32_t), kAlign));
   k_attn<T, NP><<<static_cast<unsigned>(pieces < kWorkers ? pieces : kWorkers), kAttnWaves * kWave, 0, st>>>(
-      a, tickets, parts);
+      a, tickets, static_cast<char*>(workspace) + FM_ATTN_TICKET_BYTES,
+      parts_bytes(a.group, NP * kRowPiece / static_cast<int>(sizeof(T))));
   return hipGetLastError();
 }
 
 }  // namespace
 
-static_assert(kWorkers * sizeof(uint32_t) <= FM_ATTN_TICKET_BYTES, "tickets");
-size_t attn_ticket_bytes() { return align_up(kWorkers * sizeof(uint32_t), kAlign); }
+static_assert(kWorkers * sizeof(uint32_t) <= FM_ATTN_TICKET_BYTES && FM_ATTN_TICKET_BYTES % kAlign == 0, "tickets");
 
 size_t attn_workspace_bytes(const fm_kv_cache& c, int32_t q_heads) {
   const int dims = kv_pieces(c.head_dim, c.dtype) * kRowPiece / (c.dtype == FM_BF16 ? 2 : 4);
-  const size_t floats = static_cast<size_t>(2 * kWorkers) * static_cast<size_t>(part_floats(q_heads / c.heads, dims));
-  return attn_ticket_bytes() + align_up(floats * sizeof(float), kAlign);
+  return FM_ATTN_TICKET_BYTES + align_up(parts_bytes(q_heads / c.heads, dims), kAlign);
 }
 
 hipError_t launch_attn(const AttnArgs& a, fm_dtype dt, void* workspace, hipStream_t st) {
