@@ -33,7 +33,7 @@ struct NormGradArgs {
   float* dpre;
   float* partial;     // [lists][3][d]
 };
-int norm_grad_lists(int32_t d);   // partial sums at most, a multiple of 4
+constexpr int kNormLists = 256;   // partial sums at most: a workgroup on every CU
 size_t norm_scratch_bytes(int32_t T_max, int32_t d);
 hipError_t launch_norm_grad(const NormGradArgs& a, fm_dtype dt, hipStream_t st);
 

@@ -15,6 +15,8 @@ import torch
 from . import _DTYPES, _TORCH, _aligned_bytes, _lib, _need, _ptr, _raw_stream
 from .model import _CODE, _call, _flags, _float_rows, _new, _on
 
+_GRADS = "dx", "dy", "dpost", "dgate", "dpre"
+
 
 def kv_page_bytes(layers: int, heads: int, head_dim: int, page: int = 64, dtype: str = "bf16") -> int:
     return int(_lib.load().fm_kv_page_bytes(layers, heads, head_dim, page, _DTYPES[dtype]))
@@ -185,32 +187,36 @@ def kv_copy(cache: KvCache, src: torch.Tensor, dst: torch.Tensor, stream=None) -
     _change("fm_kv_copy", cache, stream, src.data_ptr(), dst.data_ptr(), src.shape[0])
 
 
-def _rows(t, name: str, dtype, shape, device) -> Tuple[int, int]:
-    """Address and row stride of a [T][heads][head_dim] tensor whose rows need not follow each other."""
+def _rows(t, name: str, dtype, T: Optional[int], heads: Optional[int], head_dim: int, device) -> Tuple[int, int, int, int]:
+    """Address, row stride, T and heads of a [T][heads][head_dim] tensor whose rows need not follow each other (None:
+    any)."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
-    if t.device != device or t.dtype != dtype or t.dim() != 3 or any(w is not None and g != w
-                                                                    for g, w in zip(t.shape, shape)):
-        want = "x".join("*" if w is None else str(w) for w in shape)
-        raise ValueError(f"{name} must be a {dtype} [{want}] tensor on {device}, got {t.dtype} {list(t.shape)} on "
+    shape = t.shape
+    if t.dtype is not dtype or len(shape) != 3 or shape[2] != head_dim or (heads is not None and shape[1] != heads) \
+            or (T is not None and shape[0] != T) or t.device != device:
+        want = "x".join("*" if w is None else str(w) for w in (T, heads, head_dim))
+        raise ValueError(f"{name} must be a {dtype} [{want}] tensor on {device}, got {t.dtype} {list(shape)} on "
                          f"{t.device}")
-    T, H, D = t.shape
-    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D) or (T > 1 and t.stride(0) < H * D):
+    T, H, D = shape
+    row, head, one = t.stride()
+    if (one != 1 and D > 1) or (head != D and H > 1) or (row < H * D and T > 1):
         raise ValueError(f"{name} must have contiguous rows, got strides {t.stride()}")
-    return t.data_ptr(), t.stride(0) if T > 1 else H * D
+    return t.data_ptr(), row if T > 1 else H * D, T, H
 
 
 def _token_rows(name: str, cache: KvCache, layer: int, k, v, offsets, active, stream) -> None:
     dev = cache.device
-    shape = (cache.slots if offsets is None else None, cache.heads, cache.head_dim)
-    ks, vs = _rows(k, "k", cache.dtype, shape, dev), _rows(v, "v", cache.dtype, shape, dev)
-    if k.shape[0] != v.shape[0]:
-        raise ValueError(f"k and v must have as many rows, got {k.shape[0]} and {v.shape[0]}")
+    slots = cache.slots if offsets is None else None
+    k_ptr, k_stride, T, _ = _rows(k, "k", cache.dtype, slots, cache.heads, cache.head_dim, dev)
+    v_ptr, v_stride, rows, _ = _rows(v, "v", cache.dtype, slots, cache.heads, cache.head_dim, dev)
+    if T != rows:
+        raise ValueError(f"k and v must have as many rows, got {T} and {rows}")
     if offsets is not None:
         _need(offsets, "offsets", torch.int32, (cache.slots + 1,), dev)
     if active is not None:
         _need(active, "active", torch.uint8, (cache.slots,), dev)
-    _call(name, dev, stream, cache.desc, layer, *ks, *vs, _ptr(offsets), k.shape[0], _ptr(active),
+    _call(name, dev, stream, cache.desc, layer, k_ptr, k_stride, v_ptr, v_stride, _ptr(offsets), T, _ptr(active),
           _flags(cache.flags, dev))
 
 
@@ -251,8 +257,7 @@ def attn_decode(cache: KvCache, layer: int, q: torch.Tensor, scale: Optional[flo
     ``workspace`` the cache's own of the stream serves the call; replays of a graph that captured such a call must be
     ordered with each other and with the later calls on the stream of the capture."""
     dev = cache.device
-    q_ptr, q_stride = _rows(q, "q", cache.dtype, (cache.slots, None, cache.head_dim), dev)
-    q_heads = q.shape[1]
+    q_ptr, q_stride, _, q_heads = _rows(q, "q", cache.dtype, cache.slots, None, cache.head_dim, dev)
     if out is None:
         out = _new((cache.slots, q_heads, cache.head_dim), cache.dtype, dev, stream)
     else:
@@ -276,25 +281,33 @@ def attn_decode(cache: KvCache, layer: int, q: torch.Tensor, scale: Optional[flo
     return out
 
 
+def _usual(t, dtype, shape, device) -> bool:
+    """Whether _need has nothing to say about t."""
+    return type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous()
+
+
 def _norm_inputs(x, y, post, gate, pre):
-    """Check the inputs that a norm and its gradient share -> the gate's kind."""
+    """Check the inputs that a norm and its gradient share -> the gate's kind, x's shape, type and device."""
     _float_rows(x, "x")
-    T, d = x.shape
-    dev = x.device
-    if y is not None:
-        _need(y, "y", x.dtype, (T, d), dev)
-    for name, t in (("post", post), ("pre", pre)):
-        if t is not None:
-            _need(t, name, x.dtype, (d,), dev)
+    shape, dtype, dev = x.shape, x.dtype, x.device
+    T, d = shape
+    row = (d,)
+    if y is not None and not _usual(y, dtype, shape, dev):
+        _need(y, "y", dtype, (T, d), dev)
+    if post is not None and not _usual(post, dtype, row, dev):
+        _need(post, "post", dtype, row, dev)
+    if pre is not None and not _usual(pre, dtype, row, dev):
+        _need(pre, "pre", dtype, row, dev)
     if gate is None:
-        return 0
+        return 0, shape, dtype, dev
     if not isinstance(gate, torch.Tensor):
         raise TypeError(f"gate must be a torch.Tensor, got {type(gate).__name__}")
-    kind = {(d,): 1, (T, 1): 2, (T, d): 3}.get(tuple(gate.shape))
-    if kind is None:
-        raise ValueError(f"gate must have shape [{d}], [{T}x1] or [{T}x{d}], got {list(gate.shape)}")
-    _need(gate, "gate", x.dtype, tuple(gate.shape), dev)
-    return kind
+    g = gate.shape
+    kind = 1 if g == row else 3 if g == shape else 2 if g == (T, 1) else 0
+    if kind == 0:
+        raise ValueError(f"gate must have shape [{d}], [{T}x1] or [{T}x{d}], got {list(g)}")
+    _need(gate, "gate", dtype, g, dev)
+    return kind, shape, dtype, dev
 
 
 def block_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None, post: Optional[torch.Tensor] = None,
@@ -304,8 +317,7 @@ def block_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None, post: Optional
     r = x + scale * gate * norm(y) * post, h = norm(r) * pre, norm(z) = z / sqrt(mean(z^2) + eps) -> (r, h).
     x, y [T][d], post and pre [d], gate [d], [T][1] or [T][d].  Without post y is not normed, without pre h is None,
     without y (the norm before a first block) r is x itself.  ``out`` gives (r, h): r may be x or y, h may be y."""
-    kind = _norm_inputs(x, y, post, gate, pre)
-    T, d = x.shape
+    kind, shape, dtype, dev = _norm_inputs(x, y, post, gate, pre)
     r, h = (None, None) if out is None else out
     if y is None:
         if r is not None and r is not x:
@@ -314,18 +326,18 @@ def block_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None, post: Optional
             raise ValueError("without y there is only the norm by pre")
         r = None
     elif r is None:
-        r = _new((T, d), x.dtype, x.device, stream)
-    else:
-        _need(r, "out[0] (r)", x.dtype, (T, d), x.device)
+        r = _new(shape, dtype, dev, stream)
+    elif not _usual(r, dtype, shape, dev):
+        _need(r, "out[0] (r)", dtype, shape, dev)
     if pre is None:
         if h is not None:
             raise ValueError("out[1] (h) must be None without pre")
     elif h is None:
-        h = _new((T, d), x.dtype, x.device, stream)
-    else:
-        _need(h, "out[1] (h)", x.dtype, (T, d), x.device)
-    _call("fm_block_norm", x.device, stream, x.data_ptr(), _ptr(y), _ptr(post), _ptr(gate), kind, scale, _ptr(pre), eps, T,
-          d, _CODE[x.dtype], _ptr(r), _ptr(h))
+        h = _new(shape, dtype, dev, stream)
+    elif not _usual(h, dtype, shape, dev):
+        _need(h, "out[1] (h)", dtype, shape, dev)
+    _call("fm_block_norm", dev, stream, x.data_ptr(), _ptr(y), _ptr(post), _ptr(gate), kind, scale, _ptr(pre), eps,
+          shape[0], shape[1], _CODE[dtype], _ptr(r), _ptr(h))
     return (x if r is None else r), h
 
 
@@ -353,37 +365,42 @@ def block_norm_grad(dr: Optional[torch.Tensor], dh: Optional[torch.Tensor], x: t
     given exactly where pre is) -> (dx, dy, dpost, dgate, dpre), None where the input is.  dx and dy are of x's type; dpost,
     dpre and the gradient of a gate per channel or token float32, of a full gate x's type.  accumulate adds the sums
     over tokens (dpost, dpre, a channel gate's) to what ``out`` holds.  dx may be dr, dy may be y or dh."""
-    kind = _norm_inputs(x, y, post, gate, pre)
-    T, d = x.shape
-    dev = x.device
-    for name, t in (("dr", dr), ("dh", dh)):
-        if t is not None:
-            _need(t, name, x.dtype, (T, d), dev)
+    kind, shape, dtype, dev = _norm_inputs(x, y, post, gate, pre)
+    T, d = shape
+    if dr is not None and not _usual(dr, dtype, shape, dev):
+        _need(dr, "dr", dtype, shape, dev)
+    if dh is not None and not _usual(dh, dtype, shape, dev):
+        _need(dh, "dh", dtype, shape, dev)
     if y is None and (post is not None or kind):
         raise ValueError("post and gate need y")
     if (dh is None) != (pre is None):
         raise ValueError("dh must be given exactly where pre is")
     if dr is None and dh is None:
         raise ValueError("dr or dh is required")
-    gate_dtype = x.dtype if kind == 3 else torch.float32
-    want = ((T, d), x.dtype, True), ((T, d), x.dtype, y is not None), ((d,), torch.float32, post is not None), \
-        (None if kind == 0 else tuple(gate.shape), gate_dtype, kind != 0), ((d,), torch.float32, pre is not None)
-    names = "dx", "dy", "dpost", "dgate", "dpre"
+    # what each gradient is like, where its input is
+    row = (d,)
+    want = (shape, dtype), None if y is None else (shape, dtype), None if post is None else (row, torch.float32), \
+        None if kind == 0 else (gate.shape, dtype if kind == 3 else torch.float32), \
+        None if pre is None else (row, torch.float32)
     if out is None:
         if accumulate and (post is not None or pre is not None or kind == 1):
             raise ValueError("accumulate needs out")
-        out = tuple(_new(shape, dtype, dev, stream) if there else None for shape, dtype, there in want)
-    for i, (t, name, (shape, dtype, there)) in enumerate(zip(out, names, want)):
-        if there:
-            _need(t, f"out[{i}] ({name})", dtype, shape, dev)
-        elif t is not None:
-            raise ValueError(f"out[{i}] ({name}) must be None: its input is")
+        out = tuple(None if w is None else _new(*w, dev, stream) for w in want)
+    else:
+        if len(out) != 5:
+            raise ValueError(f"out must hold dx, dy, dpost, dgate and dpre, got {len(out)}")
+        for i, (t, w) in enumerate(zip(out, want)):
+            if w is None:
+                if t is not None:
+                    raise ValueError(f"out[{i}] ({_GRADS[i]}) must be None: its input is")
+            elif not _usual(t, w[1], w[0], dev):
+                _need(t, f"out[{i}] ({_GRADS[i]})", w[1], w[0], dev)
     if scratch is None:
         with _on(stream):
             scratch = BlockNormScratch(T, d, dev)
     _need(scratch.buf, "scratch", torch.uint8, (scratch.nbytes,), dev)
     dx, dy, dpost, dgate, dpre = out
     _call("fm_block_norm_grad", dev, stream, _ptr(dr), _ptr(dh), x.data_ptr(), _ptr(y), _ptr(post), _ptr(gate), kind,
-          scale, _ptr(pre), eps, T, d, _CODE[x.dtype], 1 if accumulate else 0, dx.data_ptr(), _ptr(dy), _ptr(dpost),
+          scale, _ptr(pre), eps, T, d, _CODE[dtype], 1 if accumulate else 0, dx.data_ptr(), _ptr(dy), _ptr(dpost),
           _ptr(dgate), _ptr(dpre), scratch.buf.data_ptr(), scratch.nbytes)
     return out
