@@ -31,7 +31,7 @@ struct NormGradArgs {
   float* dpost;
   void* dgate;
   float* dpre;
-  float* partial;     // [lists][3][d]
+  float* partial;     // [lists][2][d]
 };
 constexpr int kNormLists = 256;   // partial sums at most: a workgroup on every CU
 size_t norm_scratch_bytes(int32_t T_max, int32_t d);

@@ -5,9 +5,9 @@
 // per thread.  Forward: the sum of y^2, then that of r^2.  Gradient (g gate, s
 // scale, ^ a normed row):
 //   dz = dh pre            dr' = dr + (dz - r^ mean(dz r^)) / |r|      = dx
-//   dn = s dr' g           dgate = s dr' n
-//   dz' = dn post          dy = (dz' - y^ mean(dz' y^)) / |y|
-//   dpre = sum over rows of dh r^,  dpost = sum of dn y^
+//   e = s dr'              dgate = e n
+//   dz' = e g post         dy = (dz' - y^ mean(dz' y^)) / |y|
+//   dpre = sum over rows of dh r^,  dpost = sum of e g y^
 // with r and n made again from x and y, which costs one more sum over the row and
 // reads no more than the stored r would.  Memory bounds both.
 #include "fm_device.h"
@@ -202,16 +202,19 @@ __global__ void __launch_bounds__((W > 4 ? W : 4) * kWave) k_norm(NormArgs a) {
 }
 
 // The gradient.  R rows of W wavefronts per workgroup, which takes every
-// gridDim.x-th such group and keeps its share of the sums over rows in registers:
-// dpost, dpre, dgate of a channel.  A row's values stay as they were loaded (bf16 in
-// pairs), so that there is room to send for the next row's before this one's three
-// sums are waited for.  Rows of 16 wavefronts leave the vectors in the caches and the
-// next row where it is.
-template <typename T, int W, int V, int R>
+// gridDim.x-th such group and keeps its share of the sums over rows in registers.
+// With u = post gate and e = scale dr', the inner sums and dy need e u y^ only, and
+// S = sum of e y^ over the rows is both gradients of vectors: dpost = gate S, dgate =
+// post S (of other gates than a channel's: dpost = sum of e gate y^).  A row's values
+// stay as they were loaded (bf16 in pairs), so that there is room to send for the next
+// row's before this one's three sums are waited for.  Rows of 16 wavefronts leave the
+// vectors in the caches and the next row where it is.
+template <typename T, int W, int V, int R, int GATE>
 __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
   using X = Vec<T>;
   constexpr int N = X::N;
   constexpr bool kAhead = W <= 8;
+  constexpr bool kEach = GATE == FM_GATE_EACH, kChannel = GATE == FM_GATE_CHANNEL, kToken = GATE == FM_GATE_TOKEN;
   __shared__ float buf[R][2][W][4];
   __shared__ float joined[R > 1 ? W * kWave * V * N : 1];
   int turn = 0;
@@ -220,31 +223,39 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
   const int part = static_cast<int>(threadIdx.x) % (W * kWave);
   const int vecs = f.d / N;
   const float inv_d = 1.0f / static_cast<float>(f.d);
-  const bool each = f.gate_kind == FM_GATE_EACH, channel = f.gate_kind == FM_GATE_CHANNEL;
   const bool has_y = f.y != nullptr, has_post = f.post != nullptr, has_pre = f.pre != nullptr;
-  uint32x4 post_[V], pre_[V], gate_[V];
-  X sum_post[V], sum_pre[V], sum_gate[V];
+  auto in = [&](int v) __attribute__((always_inline)) { return part + v * W * kWave < vecs; };
+  // post times a channel's gate
+  auto product = [&](int v) __attribute__((always_inline)) {
+    const int64_t i = part + v * W * kWave;
+    X u = wide<T>(take(f.post, i, in(v) && has_post));
+    if (!has_post) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) u.f[j] = 1.0f;
+    }
+    if constexpr (kChannel) {
+      const X g = wide<T>(take(f.gate, i, in(v)));
+#pragma unroll
+      for (int j = 0; j < N; ++j) u.f[j] *= g.f[j];
+    }
+    return u;
+  };
+  uint32x4 pre_[V];
+  X u_[V], sum_y[V], sum_r[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int64_t i = part + v * W * kWave;
-    sum_post[v].zero();
-    sum_pre[v].zero();
-    sum_gate[v].zero();
+    sum_y[v].zero();
+    sum_r[v].zero();
     if constexpr (kAhead) {
-      post_[v] = take(f.post, i, i < vecs && has_post);
-      pre_[v] = take(f.pre, i, i < vecs && has_pre);
-      gate_[v] = take(f.gate, i, i < vecs && channel);
+      pre_[v] = take(f.pre, part + v * W * kWave, in(v) && has_pre);
+      u_[v] = product(v);
     }
   }
-  auto in = [&](int v) __attribute__((always_inline)) { return part + v * W * kWave < vecs; };
-  auto post = [&](int v) __attribute__((always_inline)) {
-    return wide<T>(kAhead ? post_[v] : take(f.post, part + v * W * kWave, in(v) && has_post));
-  };
   auto pre = [&](int v) __attribute__((always_inline)) {
     return wide<T>(kAhead ? pre_[v] : take(f.pre, part + v * W * kWave, in(v) && has_pre));
   };
   struct Row {
-    uint32x4 x[V], y[V], dr[V], dh[V], gate[V];
+    uint32x4 x[V], y[V], dr[V], dh[V], gate[kEach ? V : 1];
     float token;
   };
   auto fetch = [&](Row& w, int64_t t) __attribute__((always_inline)) {
@@ -258,9 +269,9 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
       w.x[v] = take(f.x, i, on);
       w.dh[v] = take(a.dh, i, on && a.dh != nullptr);
       w.dr[v] = take(a.dr, i, on && a.dr != nullptr);
-      if (each) w.gate[v] = take(f.gate, i, on);
+      if constexpr (kEach) w.gate[v] = take(f.gate, i, on);
     }
-    w.token = f.gate_kind == FM_GATE_TOKEN && there ? scalar<T>(f.gate, t) : 1.0f;
+    w.token = kToken && there ? scalar<T>(f.gate, t) : 1.0f;
   };
   const int64_t stride = static_cast<int64_t>(gridDim.x) * R;
   int64_t t = static_cast<int64_t>(blockIdx.x) * R + slot;
@@ -273,20 +284,17 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
     const int64_t row = t * vecs + part;
     if constexpr (kAhead) {
       fetch(next, t + stride);
-      forget(post_);
       forget(pre_);
-      forget(gate_);
     }
-    auto gate = [&](int v) __attribute__((always_inline)) {
-      X g;
-      if (each || channel) {
-        if constexpr (kAhead) g = wide<T>(each ? now.gate[v] : gate_[v]);
-        else g = wide<T>(each ? now.gate[v] : take(f.gate, part + v * W * kWave, in(v)));
-      } else {
+    // u, with the gate of each value
+    auto factor = [&](int v) __attribute__((always_inline)) {
+      X u = kAhead ? u_[v] : product(v);
+      if constexpr (kEach) {
+        const X g = wide<T>(now.gate[v]);
 #pragma unroll
-        for (int j = 0; j < N; ++j) g.f[j] = now.token;
+        for (int j = 0; j < N; ++j) u.f[j] *= g.f[j];
       }
-      return g;
+      return u;
     };
     float inv_y = 1.0f;
     if (has_post) {
@@ -300,37 +308,18 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
       row_sums<W, 1>(s, buf[slot], turn);
       inv_y = rsqrtf(s[0] * inv_d + f.eps);
     }
-    auto again = [&]() __attribute__((always_inline)) {   // between the sums
-      forget(now.y);
-      forget(now.dh);
-      if constexpr (kAhead) {
-        forget(post_);
-        forget(pre_);
-        forget(gate_);
-      }
-    };
-    again();
-    // n: y^ post, or y^ where there is no post
-    auto normed = [&](int v, X& hat, X& n) __attribute__((always_inline)) {
-      hat = wide<T>(now.y[v]);
-      const X w = post(v);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        hat.f[j] *= inv_y;
-        n.f[j] = has_post ? hat.f[j] * w.f[j] : hat.f[j];
-      }
-    };
+    forget(now.y);
     X r[V];
     float s1[2] = {0.0f, 0.0f};
+    const float step = f.scale * now.token;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       r[v] = wide<T>(now.x[v]);
       if (has_y) {
-        X hat, n;
-        normed(v, hat, n);
-        const X g = gate(v);
+        const X y = wide<T>(now.y[v]);
+        const X u = factor(v);
 #pragma unroll
-        for (int j = 0; j < N; ++j) r[v].f[j] += f.scale * g.f[j] * n.f[j];
+        for (int j = 0; j < N; ++j) r[v].f[j] += step * (u.f[j] * (y.f[j] * inv_y));
       }
       if (!in(v)) r[v].zero();
       const X dh = wide<T>(now.dh[v]);
@@ -347,64 +336,75 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
       inv_r = rsqrtf(s1[0] * inv_d + f.eps);
       mean = s1[1] * inv_r * inv_d;
     }
-    again();
-    // r becomes dr'; then dn, and sums of dz' y^ and of dgate
-    float s2[2] = {0.0f, 0.0f};
+    forget(now.y);
+    forget(now.dh);
+    if constexpr (kAhead) forget(pre_);
+    // r becomes dr', then e; the sum of e u y^, which is the gradient of a token's gate
+    float s2[1] = {0.0f};
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       X d = wide<T>(now.dr[v]);
-      if (has_pre && in(v) && live) {
+      const bool on = in(v) && live;
+      if (has_pre && on) {
         const X dh = wide<T>(now.dh[v]);
         const X w = pre(v);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           const float hat = r[v].f[j] * inv_r;
-          sum_pre[v].f[j] += dh.f[j] * hat;
+          sum_r[v].f[j] += dh.f[j] * hat;
           d.f[j] += inv_r * (dh.f[j] * w.f[j] - hat * mean);
         }
       }
-      r[v] = d;
-      if (in(v) && live) d.store(a.dx, row + v * W * kWave);
-      if (!has_y || !in(v) || !live) continue;
-      X hat, n;
-      normed(v, hat, n);
-      const X g = gate(v);
-      const X w = post(v);
+      if (on) d.store(a.dx, row + v * W * kWave);
+      if (!has_y || !on) continue;
+      const X y = wide<T>(now.y[v]);
+      const X u = factor(v);
       X one;
+      if constexpr (kEach) {   // the gate's own gradient is without the gate
+        one = kAhead ? u_[v] : product(v);
+        const X g = wide<T>(now.gate[v]);
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const float e = f.scale * d.f[j];
-        one.f[j] = e * n.f[j];
-        sum_gate[v].f[j] += one.f[j];
-        s2[1] += one.f[j];
-        const float dn = e * g.f[j];
-        sum_post[v].f[j] += dn * hat.f[j];
-        s2[0] += dn * w.f[j] * hat.f[j];
-        r[v].f[j] = dn;
+        for (int j = 0; j < N; ++j) {
+          const float hat = y.f[j] * inv_y;
+          const float e = f.scale * d.f[j];
+          one.f[j] *= e * hat;
+          sum_y[v].f[j] += e * g.f[j] * hat;
+          s2[0] += e * (u.f[j] * hat);
+          r[v].f[j] = e;
+        }
+        one.store(a.dgate, row + v * W * kWave);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const float hat = y.f[j] * inv_y;
+          const float e = f.scale * d.f[j];
+          sum_y[v].f[j] += (kToken ? e * now.token : e) * hat;
+          s2[0] += e * (u.f[j] * hat);
+          r[v].f[j] = e;
+        }
       }
-      if (each) one.store(a.dgate, row + v * W * kWave);
     }
     if (has_y) {
-      if (has_post || f.gate_kind == FM_GATE_TOKEN) row_sums<W, 2>(s2, buf[slot], turn);
-      if (f.gate_kind == FM_GATE_TOKEN && part == 0 && live) static_cast<float*>(a.dgate)[t] = s2[1];
-      again();
-      const float mean_y = s2[0] * inv_d;
+      if (has_post || kToken) row_sums<W, 1>(s2, buf[slot], turn);
+      if (kToken && part == 0 && live) static_cast<float*>(a.dgate)[t] = s2[0];
+      forget(now.y);
+      const float mean_y = has_post ? s2[0] * inv_d * inv_y : 0.0f;
+      const float back = kToken ? inv_y * now.token : inv_y;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        if (has_post) {
-          const X y = wide<T>(now.y[v]);
-          const X w = post(v);
+        const X y = wide<T>(now.y[v]);
+        const X u = factor(v);
+        X d;
 #pragma unroll
-          for (int j = 0; j < N; ++j) r[v].f[j] = inv_y * (r[v].f[j] * w.f[j] - y.f[j] * inv_y * mean_y);
-        }
-        if (in(v) && live) r[v].store(a.dy, row + v * W * kWave);
+        for (int j = 0; j < N; ++j) d.f[j] = back * (r[v].f[j] * u.f[j] - y.f[j] * mean_y);
+        if (in(v) && live) d.store(a.dy, row + v * W * kWave);
       }
     }
     if constexpr (kAhead) now = next;
     else fetch(now, t + stride);
   }
-  // the rows' sums in order, through LDS; then this workgroup's: [gridDim.x][3][d]
-  float* out = a.partial + static_cast<int64_t>(blockIdx.x) * 3 * f.d;
+  // the rows' sums in order, through LDS; then this workgroup's: [gridDim.x][2][d]
+  float* out = a.partial + static_cast<int64_t>(blockIdx.x) * 2 * f.d;
   auto put = [&](int which, X (&s)[V]) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 1; k < R; ++k) {
@@ -433,39 +433,50 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
         *reinterpret_cast<floatx4*>(to + j) = floatx4{s[v].f[j], s[v].f[j + 1], s[v].f[j + 2], s[v].f[j + 3]};
     }
   };
-  if (a.dpost != nullptr) put(0, sum_post);
-  if (channel) put(1, sum_gate);
-  if (a.dpre != nullptr) put(2, sum_pre);
+  if (a.dpost != nullptr || kChannel) put(0, sum_y);
+  if (a.dpre != nullptr) put(1, sum_r);
 }
 
-// The sums over the workgroups, 64 columns of one gradient per workgroup.
+// The sums over the workgroups, 64 columns of one list per workgroup; S times the
+// other vector is the gradient of post and of a channel's gate.
 constexpr int kSumWaves = 16;
-__global__ void __launch_bounds__(kSumWaves* kWave) k_norm_sum(const float* partial, int32_t lists, int32_t d,
-                                                               float* dpost, float* dgate, float* dpre,
-                                                               int32_t accumulate) {
+template <typename T>
+__global__ void __launch_bounds__(kSumWaves* kWave) k_norm_sum(NormGradArgs a, int32_t lists) {
   __shared__ float sums[kSumWaves][kWave];
   const int lane = threadIdx.x % kWave;
   const int wv = threadIdx.x / kWave;
   const int which = blockIdx.y;
-  float* to = which == 0 ? dpost : (which == 1 ? dgate : dpre);
-  if (to == nullptr) return;
+  const int32_t d = a.f.d;
+  const bool channel = a.f.gate_kind == FM_GATE_CHANNEL;
+  if (which == 0 ? a.dpost == nullptr && !channel : a.dpre == nullptr) return;
   const int col = static_cast<int>(blockIdx.x) * kWave + lane;
   float v = 0.0f;
   if (col < d) {
 #pragma unroll 4
-    for (int i = wv; i < lists; i += kSumWaves) v += partial[(static_cast<int64_t>(i) * 3 + which) * d + col];
+    for (int i = wv; i < lists; i += kSumWaves) v += a.partial[(static_cast<int64_t>(i) * 2 + which) * d + col];
   }
   sums[wv][lane] = v;
   __syncthreads();
   if (wv != 0 || col >= d) return;
-  float all = accumulate != 0 ? to[col] : 0.0f;
+  float all = 0.0f;
 #pragma unroll
   for (int w = 0; w < kSumWaves; ++w) all += sums[w][lane];
-  to[col] = all;
+  auto add = [&](float* to, float v) __attribute__((always_inline)) {
+    if (to != nullptr) to[col] = a.accumulate != 0 ? to[col] + v : v;
+  };
+  if (which == 1) {
+    add(a.dpre, all);
+  } else {
+    // (S is zero where there is no row, whatever the vectors hold)
+    const float g = channel && lists > 0 ? scalar<T>(a.f.gate, col) : 1.0f;
+    const float p = a.f.post != nullptr && lists > 0 ? scalar<T>(a.f.post, col) : 1.0f;
+    add(a.dpost, g * all);
+    if (channel) add(static_cast<float*>(a.dgate), p * all);
+  }
 }
 
 // Wavefronts per row and vectors per thread for rows of `vecs` vectors: the fewest
-// wavefronts that hold the row with at most VMAX vectors each.
+// wavefronts that hold the row with at most four vectors each.
 template <typename T>
 hipError_t norm(const NormArgs& a, hipStream_t st) {
   const int vecs = a.d / Vec<T>::N;
@@ -481,8 +492,8 @@ hipError_t norm(const NormArgs& a, hipStream_t st) {
   else if (vecs <= 4 * kWave) go(integral_constant<int, 1>{}, integral_constant<int, 4>{});
   else if (vecs <= 8 * kWave) go(integral_constant<int, 4>{}, integral_constant<int, 2>{});
   else if (vecs <= 16 * kWave) go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
-  else if (vecs <= 32 * kWave) go(integral_constant<int, 16>{}, integral_constant<int, 2>{});
-  else go(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+  else if (sizeof(T) == 2 || vecs <= 32 * kWave) go(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+  else go(integral_constant<int, 16>{}, integral_constant<int, sizeof(T) == 2 ? 2 : 4>{});
   return hipGetLastError();
 }
 
@@ -490,24 +501,31 @@ template <typename T>
 hipError_t norm_grad(const NormGradArgs& a, hipStream_t st) {
   const int vecs = a.f.d / Vec<T>::N;
   int lists = 0;
-  auto go = [&](auto w, auto v, auto r) {
-    constexpr int W = decltype(w)::value, V = decltype(v)::value, R = decltype(r)::value;
+  auto run = [&](auto w, auto v, auto r, auto gate) {
+    constexpr int W = decltype(w)::value, V = decltype(v)::value, R = decltype(r)::value, G = decltype(gate)::value;
     const int64_t want = (static_cast<int64_t>(a.f.T) + R - 1) / R;
     lists = static_cast<int>(want < kNormLists ? want : kNormLists);
-    if (lists > 0) k_norm_grad<T, W, V, R><<<static_cast<unsigned>(lists), W * R * kWave, 0, st>>>(a);
+    if (lists > 0) k_norm_grad<T, W, V, R, G><<<static_cast<unsigned>(lists), W * R * kWave, 0, st>>>(a);
+  };
+  auto go = [&](auto w, auto v, auto r) {
+    switch (a.f.gate_kind) {
+      case FM_GATE_NONE: return run(w, v, r, std::integral_constant<int, FM_GATE_NONE>{});
+      case FM_GATE_CHANNEL: return run(w, v, r, std::integral_constant<int, FM_GATE_CHANNEL>{});
+      case FM_GATE_TOKEN: return run(w, v, r, std::integral_constant<int, FM_GATE_TOKEN>{});
+      default: return run(w, v, r, std::integral_constant<int, FM_GATE_EACH>{});
+    }
   };
   using std::integral_constant;
-  // two vectors of every array per thread; four where no more wavefronts can be had
+  // two vectors of every array per thread; four of float32 rows of more than 8,192
+  // values, which spill registers
   if (vecs <= kWave) go(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, 8>{});
   else if (vecs <= 2 * kWave) go(integral_constant<int, 1>{}, integral_constant<int, 2>{}, integral_constant<int, 8>{});
   else if (vecs <= 8 * kWave) go(integral_constant<int, 4>{}, integral_constant<int, 2>{}, integral_constant<int, 2>{});
   else if (vecs <= 16 * kWave) go(integral_constant<int, 8>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
-  else if (vecs <= 32 * kWave) go(integral_constant<int, 16>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
-  else go(integral_constant<int, 16>{}, integral_constant<int, 4>{}, integral_constant<int, 1>{});
-  const bool channel = a.f.gate_kind == FM_GATE_CHANNEL;
-  if (a.dpost != nullptr || a.dpre != nullptr || channel)
-    k_norm_sum<<<dim3(static_cast<unsigned>((a.f.d + kWave - 1) / kWave), 3), kSumWaves * kWave, 0, st>>>(
-        a.partial, lists, a.f.d, a.dpost, channel ? static_cast<float*>(a.dgate) : nullptr, a.dpre, a.accumulate);
+  else if (sizeof(T) == 2 || vecs <= 32 * kWave) go(integral_constant<int, 16>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
+  else go(integral_constant<int, 16>{}, integral_constant<int, sizeof(T) == 2 ? 2 : 4>{}, integral_constant<int, 1>{});
+  if (a.dpost != nullptr || a.dpre != nullptr || a.f.gate_kind == FM_GATE_CHANNEL)
+    k_norm_sum<T><<<dim3(static_cast<unsigned>((a.f.d + kWave - 1) / kWave), 2), kSumWaves * kWave, 0, st>>>(a, lists);
   return hipGetLastError();
 }
 
@@ -515,7 +533,7 @@ hipError_t norm_grad(const NormGradArgs& a, hipStream_t st) {
 
 size_t norm_scratch_bytes(int32_t T_max, int32_t d) {
   const int64_t lists = T_max < 1 ? 1 : (T_max < kNormLists ? T_max : kNormLists);
-  return align_up(static_cast<size_t>(lists) * 3 * static_cast<size_t>(d) * sizeof(float), kAlign);
+  return align_up(static_cast<size_t>(lists) * 2 * static_cast<size_t>(d) * sizeof(float), kAlign);
 }
 
 hipError_t launch_norm(const NormArgs& a, fm_dtype dt, hipStream_t st) {

@@ -122,8 +122,8 @@ def test_sizes():
     desc.page = 20
     assert lib.fm_kv_scratch_bytes(C.byref(desc)) == 0 and lib.fm_attn_workspace_bytes(C.byref(desc), 8) == 0
     assert lib.fm_kv_scratch_bytes(None) == 0 and lib.fm_attn_workspace_bytes(None, 8) == 0
-    assert lib.fm_block_norm_scratch_bytes(4, 64) == 4 * 3 * 64 * 4
-    assert lib.fm_block_norm_scratch_bytes(0, 64) == 3 * 64 * 4
+    assert lib.fm_block_norm_scratch_bytes(4, 64) == 4 * 2 * 64 * 4
+    assert lib.fm_block_norm_scratch_bytes(0, 64) == 2 * 64 * 4
     for bad in ((-1, 64), (4, 0), (4, 60), (4, 16392)):
         assert lib.fm_block_norm_scratch_bytes(*bad) == 0
 
