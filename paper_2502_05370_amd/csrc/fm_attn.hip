@@ -20,7 +20,8 @@ namespace fm {
 
 namespace {
 
-constexpr int kAttnWaves = 4;
+constexpr int kAttnWaves = 4;     // wavefronts of a workgroup
+constexpr int kFew = 4;   // steps of a tile that a wavefront takes alone whatever stands beside it
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -71,6 +72,8 @@ struct Wave {
   // CU's four wavefronts have 64 KB and more on their way.
   static constexpr int SB = NP >= 8 ? (kBf ? 2 : 1) : (NP >= 4 ? 2 : (NP == 1 ? 8 : 4));
   static constexpr int OT = NP * (kBf ? 2 : 1);   // tiles of 16 dimensions
+  static constexpr bool kTwo = NP <= (kBf ? 5 : 9);      // registers for two workgroups per CU
+  static constexpr bool kNarrow = NP <= 2;   // weighing short rows takes longer than loading them
   uint32x4 q[NP];
   uint32x4 k[SB][NP], v[SB][NP];
   floatx4 o[OT];
@@ -285,9 +288,9 @@ __device__ __forceinline__ void store4(char* out, int64_t i, floatx4 v) {
 }
 
 // Maxima, sums and outputs of a tile's parts, through LDS.
-template <int NP4>   // dimensions of a padded row
+template <int DIMS>   // of a padded row
 struct Joined {
-  static constexpr int kLd = NP4 + 4;
+  static constexpr int kLd = DIMS + 4;
   float m[kAttnWaves][16], l[kAttnWaves][16];
   float o[kAttnWaves][16][kLd];
 };
@@ -306,7 +309,7 @@ __device__ __forceinline__ float share(float m, float l, float top) {
   return m == -__builtin_inff() ? (l == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(m - top);
 }
 
-// Query qi's maximum over the four entries of `sh`, and their sum relative to it.
+// Query qi's maximum over the entries of `sh`, and their sum relative to it.
 template <int DIMS>
 __device__ __forceinline__ float total_of(const Joined<DIMS>& sh, int qi, float (&f)[kAttnWaves], float& top) {
   top = -__builtin_inff();
@@ -328,7 +331,7 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const Joined<DIMS>& sh
     const int qi = i / (DIMS / 4), d = i % (DIMS / 4) * 4;
     if (d >= a.c.head_dim) continue;
     float f[kAttnWaves], top;
-    const float all = total_of<DIMS>(sh, qi, f, top);
+    const float all = total_of(sh, qi, f, top);
     floatx4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < kAttnWaves; ++u) sum += f[u] * *reinterpret_cast<const floatx4*>(&sh.o[u][qi][d]);
@@ -346,7 +349,7 @@ __device__ __forceinline__ void store_part(const Joined<DIMS>& sh, int queries, 
   for (int i = threadIdx.x; i < queries * (DIMS / 4); i += kAttnWaves * kWave) {
     const int qi = i / (DIMS / 4), d = i % (DIMS / 4) * 4;
     float f[kAttnWaves], top;
-    const float all = total_of<DIMS>(sh, qi, f, top);
+    const float all = total_of(sh, qi, f, top);
     floatx4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < kAttnWaves; ++u) sum += f[u] * *reinterpret_cast<const floatx4*>(&sh.o[u][qi][d]);
@@ -364,26 +367,27 @@ __device__ __forceinline__ void store_part(const Joined<DIMS>& sh, int queries, 
 // sums decide how much each counts.
 constexpr int kTurn = 32;   // parts
 struct Weights {
-  float top[16][16];       // by group of threads and query
+  float top[4 * kAttnWaves][16];   // by group of threads and query
   float scale[16];         // of what is there already
   float f[kTurn][16];
 };
 template <int DIMS, typename Part>
 __device__ __forceinline__ void collect(Joined<DIMS>& sh, Weights& wt, int queries, int n, __amdgpu_buffer_rsrc_t rs,
                                         Part part) {
-  constexpr int U = kTurn / kAttnWaves;   // parts of a wavefront
+  constexpr int U = kTurn / kAttnWaves;           // parts of a wavefront
+  constexpr int G = 4 * kAttnWaves, J = kTurn / G;   // groups of 16 threads, and parts whose weights each computes
   constexpr int E = 2;                    // fours of values of a lane in flight, per part
   const int tid = threadIdx.x;
   const int lane = tid % kWave;
   const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int pg = tid / 16, pq = tid % 16;   // weights: parts pg and pg + 16 of a turn, query pq
+  const int pg = tid / 16, pq = tid % 16;   // weights: parts pg + G j of a turn, query pq
   const int quads = queries * (DIMS / 4);
   float l = 0.0f, top = -__builtin_inff();   // of query pq; l: this thread's parts
   for (int p0 = 0; p0 < n; p0 += kTurn) {
-    float m[2], s[2];
+    float m[J], s[J];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int p = p0 + pg + 16 * j;
+    for (int j = 0; j < J; ++j) {
+      const int p = p0 + pg + G * j;
       const bool in = p < n && pq < queries;
       const uint32_t at = in ? part(p) + 4u * pq : kOutside;
       m[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, static_cast<int>(at), 0, kAgent));
@@ -402,16 +406,16 @@ __device__ __forceinline__ void collect(Joined<DIMS>& sh, Weights& wt, int queri
               rs, static_cast<int>(p < n && e0 + e * kWave + lane < quads ? at + e * (16u * kWave) : kOutside), 0, kAgent);
       }
       if (e0 == 0) {
-        wt.top[pg][pq] = fmaxf(m[0], m[1]);
+        wt.top[pg][pq] = fmaxf(m[0], m[J - 1]);
         __syncthreads();
         float now = top;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) now = fmaxf(now, wt.top[j][pq]);
+        for (int j = 0; j < G; ++j) now = fmaxf(now, wt.top[j][pq]);
         l *= share(top, l, now);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < J; ++j) {
           const float f = share(m[j], s[j], now);
-          wt.f[pg + 16 * j][pq] = f;
+          wt.f[pg + G * j][pq] = f;
           l += f * s[j];
         }
         if (pg == 0) wt.scale[pq] = top == now ? 1.0f : share(top, 1.0f, now);
@@ -459,10 +463,12 @@ __device__ __forceinline__ int ratio(int n, int d) {
 // tile is a part; a tile of several workgroups is joined by the last of them that
 // is done (tickets, no wait), in the order of the line.  No part is shorter than
 // kPart steps: a cut closer to an end of its tile moves there.
-constexpr int kWorkers = 256;    // workgroups that the line is cut for: one on every CU
+constexpr int kCus = 256;
+constexpr int kWorkers = 2 * kCus;   // workgroups that the line is cut for at most: two on every CU
 constexpr int kOverhead = 8;     // units of a tile besides its steps
 constexpr int kLeast = 8;        // units of a workgroup at least: few tiles have one each
 constexpr int kPart = 4;
+constexpr int kShort = 64;       // units of a tile on average
 constexpr int64_t kLongest = int64_t{kWorkers} << 30;   // a workgroup's places are int32
 __device__ __forceinline__ int cut(int x, int steps) {   // x: from the tile's first step on
   if (x <= 0) return 0;
@@ -471,7 +477,7 @@ __device__ __forceinline__ int cut(int x, int steps) {   // x: from the tile's f
 }
 
 template <typename T, int NP>
-__global__ void __launch_bounds__(kAttnWaves* kWave, 1)
+__global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1))
     k_attn(AttnArgs a, uint32_t* tickets, char* parts, uint32_t parts_bytes) {
   using W = Wave<T, NP>;
   constexpr int kDims = NP * kRowPiece / static_cast<int>(sizeof(T));
@@ -531,7 +537,11 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, 1)
       if (pass == 1 && passed > from) break;
     }
     if (pass == 1) break;
-    each = static_cast<int>((passed + kWorkers - 1) / kWorkers);
+    // One workgroup per CU, or two: where short tiles, more than CUs, each wait for
+    // their data.
+    const int64_t tiles = static_cast<int64_t>(a.c.n_slots) * per_slot;
+    const bool two = W::kTwo && (W::kNarrow || (tiles > kCus && passed < kShort * tiles));
+    each = static_cast<int>((passed + kWorkers - 1) / kWorkers) * (two ? 1 : 2);
     if (each < kLeast) each = kLeast;
     from = static_cast<int64_t>(each) * blockIdx.x;
     if (from >= passed) return;
@@ -558,6 +568,17 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, 1)
   int head = tile0 / a.tiles, tile = tile0 % a.tiles;
   mine = __builtin_amdgcn_readfirstlane(mine);
   each = __builtin_amdgcn_readfirstlane(each);
+  int turn = 0;        // tiles that a wavefront has alone
+  // Tiles of this slot that were passed in the piece, and those that come in groups of one for each wavefront.
+  int k = 0, groups = 0;
+  auto count_groups = [&]() __attribute__((always_inline)) {
+    const int first = at < 0 ? 1 : 0;   // (begun before the piece)
+    const int here = per_slot - (head * a.tiles + tile);
+    const int whole = ratio(mine - at, kOverhead + steps);
+    k = -first;
+    groups = ((here < whole ? here : whole) - first) / kAttnWaves * kAttnWaves;
+  };
+  count_groups();
   const uint32_t size = part_bytes(a.group, kDims);
   const __amdgpu_buffer_rsrc_t rs = row_buffer(parts, parts_bytes);
   while (at < mine) {
@@ -572,12 +593,31 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, 1)
         store4<T>(a.out, static_cast<int64_t>(row0) * a.c.head_dim + i * 4, floatx4{0.f, 0.f, 0.f, 0.f});
       if (a.lse != nullptr && tid < queries) a.lse[row0 + tid] = -__builtin_inff();
     }
-    if (lo < hi) {
+    // Short tiles cost little but the wait for their data: each wavefront takes tiles
+    // of its own, without barriers and LDS; longer ones only where the piece holds one
+    // for every wavefront, of one length.
+    const bool alone = lo == 0 && hi == steps && (steps <= kFew ? steps == 1 || 2 * (kOverhead + steps) <= each : k >= 0 && k < groups);
+    ++k;
+    if (lo < hi && !(alone && turn++ % kAttnWaves != wv)) {
       W w;
       w.clear();
       load_queries<T, NP>(a, w, slot, head, tile);
-      walk<T, NP>(a, w, slot, head, seen, lo + wv, hi, kAttnWaves, bad);
+      walk<T, NP>(a, w, slot, head, seen, alone ? 0 : lo + wv, hi, alone ? 1 : kAttnWaves, bad);
       const float l = sum_of_groups(w.l);
+      if (alone) {
+        if (c < queries) {
+          const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+          for (int t = 0; t < W::OT; ++t) {
+            const int d = 16 * t + 4 * g;
+            const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+            if (d < a.c.head_dim)
+              store4<T>(a.out, static_cast<int64_t>(row0 + c) * a.c.head_dim + d, l == 0.0f ? zero : w.o[t] * inv);
+          }
+          if (g == 0 && a.lse != nullptr)
+            a.lse[row0 + c] = l == 0.0f ? -__builtin_inff() : (w.m + __builtin_amdgcn_logf(l)) * kLn2;
+        }
+      } else {
       __syncthreads();   // the tile before this one has left LDS
       if (g == 0) {
         sh.m[wv][c] = w.m;
@@ -590,7 +630,7 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, 1)
       if (!ends) {
         // a workgroup has two parts at most: of a tile that began before its piece
         // of the line, and of one that goes on behind it
-        store_part<kDims>(sh, queries, rs, (2 * blockIdx.x + (lo == 0 ? 1u : 0u)) * size);
+        store_part(sh, queries, rs, (2 * blockIdx.x + (lo == 0 ? 1u : 0u)) * size);
         // the workgroups that have the tile's first part and its last
         const int w0 = static_cast<int>(blockIdx.x) + ratio(step0 + kPart - 1, each);
         const int w1 = static_cast<int>(blockIdx.x) + ratio(step0 + steps - kPart, each);
@@ -602,13 +642,14 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, 1)
         __syncthreads();
         ends = is_last != 0;
         if (ends) {
-          collect<kDims>(sh, weights, queries, w1 - w0 + 1, rs, [&](int p) __attribute__((always_inline)) {
+          collect(sh, weights, queries, w1 - w0 + 1, rs, [&](int p) __attribute__((always_inline)) {
             return (2u * static_cast<uint32_t>(w0 + p) + (p == 0 ? 1u : 0u)) * size;
           });
           if (tid == 0) __hip_atomic_store(&tickets[w1], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
       }
-      if (ends) finish<T, kDims>(a, sh, row0, queries);
+      if (ends) finish<T>(a, sh, row0, queries);
+      }
     }
     at += kOverhead + steps;
     if (++tile == a.tiles) {
@@ -619,6 +660,7 @@ __global__ void __launch_bounds__(kAttnWaves* kWave, 1)
         ++slot;
         seen = seen_of(a, slot);
         steps = __builtin_amdgcn_readfirstlane(steps_of(seen));
+        count_groups();
       }
     }
   }
@@ -634,7 +676,7 @@ hipError_t launch(const AttnArgs& a, void* workspace, hipStream_t st) {
   const int64_t longest = kOverhead + 1 + (static_cast<int64_t>(a.c.max_pages) * a.c.page / kBlockTokens + SB) / SB;
   const int64_t line = longest * a.c.n_slots * a.c.heads * a.tiles;
   if (line >= kLongest) return hipErrorInvalidValue;
-  const int64_t pieces = (line + kLeast - 1) / kLeast;
+  const int64_t pieces = (line + kOverhead - 1) / kOverhead;
   uint32_t* tickets = static_cast<uint32_t*>(workspace);
   k_attn<T, NP><<<static_cast<unsigned>(pieces < kWorkers ? pieces : kWorkers), kAttnWaves * kWave, 0, st>>>(
       a, tickets, static_cast<char*>(workspace) + FM_ATTN_TICKET_BYTES,
