@@ -1,7 +1,7 @@
 """Serving iterations of a small mixture-of-experts model whose experts live on
 the host, with the expert-map search deciding what the expert cache holds.
 
-    python examples/moe_iteration.py
+    python examples/moe_iteration.py [--attention]
 
 One iteration of a batch of requests, as the library's operators make it up:
 
@@ -18,7 +18,23 @@ One iteration of a batch of requests, as the library's operators make it up:
        moe_experts         the chosen experts' products, added to the stream
   5. Store.insert          the finished iterations enter the store
 
-Model.tune moves the embeddings of some tokens with embed_grad.  Weights are random and attention is left out: the layers are residual MoE blocks.
+With Config.heads the layers have attention in front of their experts, over a
+paged cache of as many slots as the batch has requests:
+
+       block_norm          the norm before attention
+       kv_write            the new tokens' keys and values, in pages that
+                           kv_resize has found for them
+       attn_decode         each request's new token over its own tokens
+       block_norm          the output normed, gated, added to the stream, and
+                           the norm before the experts
+
+An iteration then takes the tokens of each prompt that the cache does not hold
+yet, one per request at a time.  Model.branch lets requests go on from others
+(kv_fork), Model.end drops some and closes the gaps (kv_resize, kv_compact).
+
+Model.tune moves the embeddings of some tokens with embed_grad, Model.tune_norms the
+weights of a layer's norms with block_norm_grad.  Weights are random; without heads
+the layers are residual MoE blocks.
 """
 from __future__ import annotations
 
@@ -45,6 +61,14 @@ class Config:
     distance: int = 2     # layers between a search and the prefetch it guides
     store: int = 256      # iterations the store holds
     tau: float = 0.9      # share of probability that a prefetch set covers
+    heads: int = 0        # query heads of attention; 0: none
+    kv_heads: int = 2     # key and value heads
+    head_dim: int = 64
+    batch: int = 8        # requests of the cache, and so of an iteration
+    tokens: int = 512     # of a request at most
+    pages: int = 64       # of the cache
+    page: int = 32        # tokens of a page
+    window: int = 0       # tokens that a query sees; 0: all
 
 
 class Layer:
@@ -58,6 +82,13 @@ class Layer:
         self.cache = fm.ExpertCache(c.slots, c.E, c.d, c.f, "bf16")
         self.held = {}    # expert -> slot, in the order of their last use
         self.loads = 0
+        if c.heads:
+            q, kv = c.heads * c.head_dim, c.kv_heads * c.head_dim
+            self.qkv = (torch.randn(c.d, q + 2 * kv, generator=g) / c.d ** 0.5).to(bf).cuda()
+            self.back = (torch.randn(q, c.d, generator=g) / q ** 0.5).to(bf).cuda()
+            # norms before and after attention, its gate, the norm before the experts
+            self.first, self.post, self.gain, self.pre = ((1 + 0.1 * torch.randn(c.d, generator=g)).to(bf).cuda()
+                                                          for _ in range(4))
 
     def bring_in(self, experts, keep=()) -> int:
         """Load the experts that the cache lacks, over the least recently used others.  Returns how many were
@@ -100,15 +131,62 @@ class Model:
         self.table = torch.randn(c.V, c.d, generator=g).to(torch.bfloat16).cuda()
         self.layers = [Layer(c, g) for _ in range(c.L)]
         self.store = fm.Store(c.store, c.L, c.E, c.d, "f32")
+        if c.heads:
+            self.kv = fm.KvCache(c.batch, c.tokens, c.pages, c.L, c.kv_heads, c.head_dim, "bf16", page=c.page)
+            self.taken = [0] * c.batch    # tokens of each request in the cache
+
+    def branch(self, parent):
+        """Request s goes on from what request parent[s] is now (-1: from itself); pages are shared until they change."""
+        fm.kv_fork(self.kv, torch.tensor(parent, dtype=torch.int32, device="cuda"))
+        self.taken = [self.taken[p] if p >= 0 else n for p, n in zip(parent, self.taken)]
+
+    def end(self, requests) -> int:
+        """The requests' tokens leave the cache.  Returns how many pages are still held: the lowest ones."""
+        fm.kv_resize(self.kv, torch.tensor([-2 ** 31 if s in requests else 0 for s in range(self.c.batch)],
+                                           dtype=torch.int32, device="cuda"))
+        self.taken = [0 if s in requests else n for s, n in enumerate(self.taken)]
+        return int(fm.kv_compact(self.kv))
+
+    def _room(self, last):
+        """Room for one token of every request that has one (last [B], -1: none) -> which have it, [B] uint8."""
+        active = fm.kv_resize(self.kv, (last >= 0).to(torch.int32))
+        assert self.kv.check() == 0, "the cache has no page left"
+        return active
+
+    def _attend(self, l, layer, x, active):
+        """Attention in front of a layer's experts -> the stream and the experts' input."""
+        c = self.c
+        _, h = fm.block_norm(x, pre=layer.first)
+        rows = (h @ layer.qkv).view(len(x), c.heads + 2 * c.kv_heads, c.head_dim)
+        q, k, v = rows.split([c.heads, c.kv_heads, c.kv_heads], dim=1)
+        fm.kv_write(self.kv, l, k, v, active=active)
+        y = fm.attn_decode(self.kv, l, q, window=c.window, active=active)
+        return fm.block_norm(x, y.view(len(x), -1) @ layer.back, post=layer.post, gate=layer.gain, pre=layer.pre)
+
+    def _feed(self, last):
+        """One token of every request that has one, through all layers, without the search."""
+        c = self.c
+        active = self._room(last)
+        x = fm.embed_lookup(self.table, last, c.d ** 0.5)
+        for l, layer in enumerate(self.layers):
+            x, h = self._attend(l, layer, x, active)
+            _, ids, weight, chosen = fm.moe_route(h, layer.gate, c.K, renorm=True, active=active)
+            x = self._experts(layer, h, ids, weight, experts_of(chosen), x)
 
     def iteration(self, prompts):
         """One iteration of a batch: prompts is a list of token lists.  Returns the hidden states [B][d], the
         expert maps [B][L][E], and how many chosen experts were found in the cache and loaded on demand."""
         c, B = self.c, len(prompts)
+        if c.heads:
+            assert B == c.batch and all(len(p) > n or not p for p, n in zip(prompts, self.taken))
+            for at in range(max((len(p) - 1 - n for p, n in zip(prompts, self.taken)), default=0)):
+                self._feed(torch.tensor([p[n + at] if n + at < len(p) - 1 else -1 for p, n in zip(prompts, self.taken)],
+                                        dtype=torch.int32, device="cuda"))
+            self.taken = [max(len(p), n) for p, n in zip(prompts, self.taken)]
         tokens = torch.tensor([t for p in prompts for t in p], dtype=torch.int32, device="cuda")
         offsets = torch.tensor(np.cumsum([0] + [len(p) for p in prompts]), dtype=torch.int32, device="cuda")
         last = torch.tensor([p[-1] if p else -1 for p in prompts], dtype=torch.int32, device="cuda")
-        active = (last >= 0).to(torch.uint8)
+        active = self._room(last) if c.heads else (last >= 0).to(torch.uint8)
         scale = c.d ** 0.5
         select = dict(tau=c.tau, k_min=c.K, k_max=c.E)
         maps = torch.empty(B, c.L, c.E, device="cuda")
@@ -124,7 +202,10 @@ class Model:
         search = fm.TrajPass(self.store, B)
         found = loaded = 0
         for l, layer in enumerate(self.layers):
-            h = normed(x)
+            if c.heads:
+                x, h = self._attend(l, layer, x, active)
+            else:
+                h = normed(x)
             _, ids, weight, chosen = fm.moe_route(h, layer.gate, c.K, renorm=True, active=active,
                                                   out=(maps[:, l], *self._choice(B)))
             ahead = l + c.distance
@@ -156,6 +237,18 @@ class Model:
         self.table = (self.table.float() - rate * grad).to(self.table.dtype)
         return 0.5 * float(off.square().sum())
 
+    def tune_norms(self, layer, x, y, wanted, rate: float) -> float:
+        """One step of gradient descent on the norms around a layer's attention (whose output y is for the stream x) that
+        draws the experts' input to the rows of wanted [T][d] (half the squared distance).  Returns the loss before the
+        step."""
+        common = dict(post=layer.post, gate=layer.gain, pre=layer.pre)
+        _, h = fm.block_norm(x, y, **common)
+        off = h.float() - wanted
+        _, _, dpost, dgain, dpre = fm.block_norm_grad(None, off.to(x.dtype), x, y, **common)
+        for w, g in ((layer.post, dpost), (layer.gain, dgain), (layer.pre, dpre)):
+            w.copy_(w.float() - rate * g)
+        return 0.5 * float(off.square().sum())
+
     def _choice(self, B):
         c = self.c
         return (torch.empty(B, c.K, dtype=torch.int32, device="cuda"), torch.empty(B, c.K, device="cuda"),
@@ -175,17 +268,19 @@ class Model:
         return x
 
 
-def main():
-    model = Model()
+def main(heads: int = 0):
+    model = Model(Config(heads=heads))
     rng = np.random.default_rng(0)
     topics = [rng.integers(0, model.c.V, 40) for _ in range(6)]   # prompts repeat their topic's words
     for it in range(5):
         prompts = [list(map(int, rng.choice(topics[rng.integers(6)], rng.integers(5, 30)))) for _ in range(8)]
         _, _, found, missed = model.iteration(prompts)
+        if heads:
+            assert model.end(range(8)) == 0    # the next prompts are other requests
         torch.cuda.synchronize()
         print(f"iteration {it}: {found} of {found + missed} chosen experts were in the cache, {missed} loaded on "
               f"demand; {model.store.size} iterations stored")
 
 
 if __name__ == "__main__":
-    main()
+    main(4 if "--attention" in sys.argv[1:] else 0)

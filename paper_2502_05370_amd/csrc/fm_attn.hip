@@ -469,7 +469,7 @@ constexpr int kOverhead = 8;     // units of a tile besides its steps
 constexpr int kLeast = 8;        // units of a workgroup at least: few tiles have one each
 constexpr int kPart = 4;
 constexpr int kShort = 64;       // units of a tile on average
-constexpr int64_t kLongest = int64_t{kWorkers} << 30;   // a workgroup's places are int32
+constexpr int64_t kLongest = int64_t{kCus} << 29;   // of a line: a workgroup's places are int32
 __device__ __forceinline__ int cut(int x, int steps) {   // x: from the tile's first step on
   if (x <= 0) return 0;
   if (x >= steps) return steps;

@@ -1,0 +1,310 @@
+"""The paged cache, its attention and the norms where memory matters: offsets past
+32 bits, calls on other streams, captured graphs and the workspaces they share, rows
+and slots that a call must leave alone."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer as ref
+from test_gpu_attention import check, drawn, filled
+from test_gpu_kv_pages import _fm, i32
+
+pytestmark = pytest.mark.gpu
+
+
+def _replays(graph, outs, want, between, times=4):
+    """Replay, with the program's own work between, and compare every time."""
+    for _ in range(times):
+        for o in outs:
+            o.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+        between()
+
+
+def test_pages_past_32_bits():
+    """A pool of more than 4 GiB (and 2^31 elements), its last pages in use, in every call."""
+    fm = _fm()
+    rng = np.random.default_rng(1)
+    layers, heads, D, page = 8, 8, 128, 64
+    n = (5 << 30) // fm.kv_page_bytes(layers, heads, D, page)
+    cache = fm.KvCache(3, 4 * page, n, layers, heads, D, page=page)
+    assert cache.pages.numel() > 2 ** 31
+    length = [150, 1, 70]
+    cache.table[0, :3] = i32([n - 1, 0, n - 2])
+    cache.table[1, 0] = n - 3
+    cache.table[2, :2] = i32([n - 5, n - 4])
+    cache.length.copy_(i32(length))
+    cache.refs[[0, n - 1, n - 2, n - 3, n - 4, n - 5]] = 1
+    cache.refs[1:n - 6] = 2                      # held elsewhere: only page n - 6 is free
+    k, kn = drawn(rng, (sum(length), heads, D), "bf16")
+    v, vn = drawn(rng, (sum(length), heads, D), "bf16")
+    off = np.cumsum([0] + length)
+    fm.kv_write(cache, layers - 1, k, v, offsets=i32(off))
+    got = fm.kv_read(cache, layers - 1, T=sum(length), offsets=i32(off))
+    assert torch.equal(got[0], k) and torch.equal(got[1], v)
+    q, qn = drawn(rng, (3, 16, D), "bf16")
+    lse = torch.empty(3, 16, device="cuda")
+    out = fm.attn_decode(cache, layers - 1, q, lse=lse)
+    check(out, lse, qn, np.split(kn, off[1:3]), np.split(vn, off[1:3]), np.float32(D ** -0.5), "bf16")
+    fm.kv_fork(cache, i32([-1, 2, -1]))          # slot 1's page n - 3 is free now too
+    assert fm.kv_resize(cache, i32([0, 1, 0])).tolist() == [0, 1, 0]
+    assert cache.table[1].tolist() == [n - 5, n - 6, -1, -1] and torch.equal(cache.pages[n - 6], cache.pages[n - 4])
+    fm.kv_copy(cache, i32([n - 1]), i32([n - 3]))
+    assert torch.equal(cache.pages[n - 1], cache.pages[n - 3])
+    assert cache.check() == 0
+
+
+def test_norm_rows_past_32_bits():
+    """The last rows of more than 2^31 values, forward and backward."""
+    fm = _fm()
+    T, d = 131075, 16384
+    g = torch.Generator(device="cuda").manual_seed(1)
+    big = [torch.zeros(T, d, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    for t in big:
+        t[-3:] = torch.randn(3, d, generator=g, device="cuda")
+    x, y, dr, dh = big
+    w = torch.randn(d, generator=g, device="cuda").to(torch.bfloat16)
+    small = [t[-3:].clone() for t in big]
+    r, h = fm.block_norm(x, y, post=w, pre=w)
+    want = fm.block_norm(small[0], small[1], post=w, pre=w)
+    assert torch.equal(r[-3:], want[0]) and torch.equal(h[-3:], want[1]) and not r[:3].any()
+    got = fm.block_norm_grad(dr, dh, x, y, post=w, pre=w, out=(r, h, *(torch.empty(d, device="cuda") if i != 1 else None
+                                                                      for i in range(3))))
+    want = fm.block_norm_grad(small[2], small[3], small[0], small[1], post=w, pre=w)
+    assert torch.equal(got[0][-3:], want[0]) and torch.equal(got[1][-3:], want[1])
+    for i in (2, 4):     # three terms, added in another order
+        assert (got[i] - want[i]).abs().max() <= 8 * 2.0 ** -24 * (want[i].abs().max() + 300)
+
+
+def test_a_decode_iteration_as_a_graph():
+    """Growth, writing, attention and norms captured once and replayed token after token, eager work between; the same
+    tokens without a graph give the same bits."""
+    fm = _fm()
+    rng = np.random.default_rng(2)
+    B, heads, D, d = 5, 2, 64, 512
+    rows = [drawn(rng, (B, 8 + 2 * heads, D), "bf16")[0] for _ in range(40)]
+    x0, _ = drawn(rng, (B, d), "bf16")
+    w, _ = drawn(rng, (d,), "bf16")
+    on = i32([1, 1, 0, 1, 1])
+
+    def state():
+        cache = fm.KvCache(B, 128, 40, 2, heads, D, page=16)
+        fm.kv_resize(cache, i32([30, 0, 0, 14, 15]))
+        torch.manual_seed(0)
+        cache.pages.copy_(torch.randn(cache.pages.shape, device="cuda"))
+        return cache
+
+    def step(cache, row, out):
+        active = fm.kv_resize(cache, on, out=out[0])
+        q, k, v = row.split([8, heads, heads], dim=1)
+        for layer in range(2):
+            fm.kv_write(cache, layer, k, v, active=active)
+            y = fm.attn_decode(cache, layer, q, active=active, out=out[1 + layer])
+        fm.block_norm(x0, y.view(B, d), post=w, pre=w, out=out[3:])
+
+    def outputs():
+        return [torch.empty(B, dtype=torch.uint8, device="cuda"),
+                *(torch.empty(B, 8, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)),
+                *(torch.empty_like(x0) for _ in range(2))]
+
+    eager, captured = state(), state()
+    row = rows[0].clone()
+    outs = outputs()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        warm = state()
+        step(warm, row, outs)
+        captured.ensure_workspace(8)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step(captured, row, outs)
+    for r in rows:
+        row.copy_(r)
+        graph.replay()
+        want = outputs()
+        step(eager, r, want)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+        assert torch.equal(captured.table, eager.table) and torch.equal(captured.length, eager.length)
+    assert eager.length.tolist() == [70, 40, 0, 54, 55] and eager.check() == 0 and captured.check() == 0
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Graphs of different calls with one workspace, replayed in turn, and a split sequence in each."""
+    fm = _fm()
+    rng = np.random.default_rng(3)
+    a, *_ = filled(rng, [5000, 40], 2, 64, 16, "bf16")
+    b, *_ = filled(rng, [33, 7000], 2, 64, 16, "bf16")
+    q, _ = drawn(rng, (2, 6, 64), "bf16")
+    ws = fm.AttnWorkspace(a, 6)
+    want = [fm.attn_decode(c, 0, q) for c in (a, b)]
+    outs = [torch.empty_like(w) for w in want]
+    graphs = []
+    for c, o in zip((a, b), outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            fm.attn_decode(c, 0, q, out=o, workspace=ws)
+        graphs.append(g)
+    for turn in range(6):
+        which = [0, 1, 1, 0, 0, 1][turn]
+        outs[which].zero_()
+        graphs[which].replay()
+        eager = fm.attn_decode((b, a)[which], 0, q, workspace=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[which], want[which]) and torch.equal(eager, want[1 - which])
+    from paper_2502_05370_amd import _lib
+    assert not ws.buf[: _lib.FM_ATTN_TICKET_BYTES].any()
+
+
+def test_a_workspace_made_during_a_capture():
+    fm = _fm()
+    rng = np.random.default_rng(4)
+    cache, *_ = filled(rng, [6000, 40], 2, 64, 16, "bf16")
+    q, _ = drawn(rng, (2, 6, 64), "bf16")
+    want = fm.attn_decode(cache, 0, q, workspace=fm.AttnWorkspace(cache, 6))
+    out = torch.empty_like(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fm.attn_decode(cache, 0, q, out=out)
+    _replays(graph, [out], [want], lambda: fm.attn_decode(cache, 0, q, window=100))
+
+
+def test_a_graph_outlives_the_growth_of_the_workspace():
+    """A captured call of few query heads; then calls of more, which need a larger workspace, and memory that other work
+    takes."""
+    fm = _fm()
+    rng = np.random.default_rng(5)
+    cache, *_ = filled(rng, [6000, 40], 2, 64, 16, "bf16")
+    q, _ = drawn(rng, (2, 32, 64), "bf16")
+    few = q[:, :2].contiguous()
+    want = fm.attn_decode(cache, 0, few)
+    out = torch.empty_like(want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        fm.attn_decode(cache, 0, few, out=out)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            fm.attn_decode(cache, 0, few, out=out)
+        small = cache.ensure_workspace(2)
+        fm.attn_decode(cache, 0, q)
+        assert cache.ensure_workspace(32).nbytes > small.nbytes
+        other = [torch.full((small.nbytes // k,), 85, dtype=torch.uint8, device="cuda") for k in (1, 1, 2) for _ in range(8)]
+        _replays(graph, [out], [want], lambda: None)
+        assert all((t == 85).all() for t in other)
+
+
+def test_unordered_streams():
+    """Attention of two layers on two streams at once, on the cache's own workspaces; outputs that a call creates belong
+    to its stream."""
+    fm = _fm()
+    rng = np.random.default_rng(6)
+    cache, *_ = filled(rng, [9000, 300, 20], 2, 64, 16, "bf16", layers=2, layer=1)
+    k, _ = drawn(rng, (9320, 2, 64), "bf16")
+    fm.kv_write(cache, 0, k, k, offsets=i32([0, 9000, 9300, 9320]))
+    q, _ = drawn(rng, (3, 8, 64), "bf16")
+    want = [fm.attn_decode(cache, l, q, workspace=fm.AttnWorkspace(cache, 8)) for l in range(2)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(40):
+        got[0].append(fm.attn_decode(cache, 0, q))
+        got[1].append(fm.attn_decode(cache, 1, q, stream=side))
+    assert cache.ensure_workspace(8) is not cache.ensure_workspace(8, side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, w) for gs, w in zip(got, want) for g in gs)
+    x, _ = drawn(rng, (200, 256), "bf16")
+    w = torch.ones(256, dtype=torch.bfloat16, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    a = [fm.block_norm_grad(x, x, x, x, post=w, pre=w) for _ in range(10)]
+    b = [fm.block_norm_grad(x, x, x, x, post=w, pre=w, stream=side) for _ in range(10)]
+    r = [fm.block_norm(x, x, post=w, pre=w, stream=side) for _ in range(10)]
+    torch.cuda.synchronize()
+    for other in a + b:
+        assert all(p is None or torch.equal(p, o) for p, o in zip(a[0], other))
+    assert all(torch.equal(p, o) for other in r for p, o in zip(fm.block_norm(x, x, post=w, pre=w), other))
+
+
+def test_norms_and_their_gradient_as_a_graph():
+    fm = _fm()
+    rng = np.random.default_rng(7)
+    T, d = 300, 1032
+    x, y, dr, dh = (drawn(rng, (T, d), "bf16")[0] for _ in range(4))
+    w = drawn(rng, (d,), "bf16")[0]
+    common = dict(post=w, gate=w, pre=w)
+    want = [*fm.block_norm(x, y, **common), *fm.block_norm_grad(dr, dh, x, y, **common)]
+    outs = [torch.empty_like(t) for t in want]
+    scratch = fm.BlockNormScratch(T, d)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fm.block_norm(x, y, out=outs[:2], **common)
+        fm.block_norm_grad(dr, dh, x, y, out=outs[2:], scratch=scratch, **common)
+    _replays(graph, outs, want, lambda: fm.block_norm_grad(dr[:7], dh[:7], x[:7], y[:7], scratch=scratch, **common))
+
+
+def test_pages_moves_as_a_graph():
+    """Forks, growth with copies, drops and compaction, captured once and replayed over the state they leave."""
+    fm = _fm()
+    cache = fm.KvCache(6, 160, 50, 2, 1, 32, page=16)
+    cache.pages.copy_(torch.arange(50, device="cuda")[:, None].expand(cache.pages.shape))
+    fm.kv_resize(cache, i32([70, 33, 0, 0, 20, 0]))
+    want = ref.Pages(cache.table.cpu().numpy(), cache.length.cpu().numpy(), cache.refs.cpu().numpy(),
+                     cache.pages.float().cpu().numpy()[:, :1], 16)
+    parent, grow = [-1, -1, 0, 1, -1, 4], [1, 1, 2, 3, -40, 20]
+    p, g = i32(parent), i32(grow)
+    granted, live = torch.empty(6, dtype=torch.uint8, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fm.kv_fork(cache, p)
+        fm.kv_resize(cache, g, out=granted)
+        fm.kv_compact(cache, out=live)
+    for _ in range(6):
+        graph.replay()
+        torch.cuda.synchronize()
+        want.fork(parent)
+        ok, _ = want.resize(grow)
+        n = want.compact()
+        assert granted.tolist() == ok.tolist() and int(live) == n
+        for name in ("table", "length", "refs"):
+            assert (getattr(cache, name).cpu().numpy() == getattr(want, name)).all(), name
+        held = want.refs > 0
+        assert (cache.pages.float().cpu().numpy()[held, :1] == want.content[held]).all()
+
+
+def test_what_a_call_leaves_alone():
+    """Tensors around outputs and states: every call writes within its own."""
+    fm = _fm()
+    rng = np.random.default_rng(8)
+    cache, *_ = filled(rng, [3000, 0, 17], 2, 40, 16, "bf16")
+
+    def framed(shape, dtype, fill=5):
+        raw = torch.full((int(np.prod(shape)) + 512,), fill, dtype=dtype, device="cuda")
+        return raw, raw[256:256 + int(np.prod(shape))].view(shape)
+
+    q, _ = drawn(rng, (3, 6, 40), "bf16")
+    raw, out = framed((3, 6, 40), torch.bfloat16)
+    lraw, lse = framed((3, 6), torch.float32)
+    wraw = torch.full((fm.attn_workspace_bytes(cache, 6) + 1024,), 85, dtype=torch.uint8, device="cuda")
+    ws = fm.AttnWorkspace(cache, 6)
+    at = -wraw.data_ptr() % 256 + 256
+    ws.buf = wraw[at: at + ws.nbytes]
+    ws.buf.zero_()
+    fm.attn_decode(cache, 0, q, out=out, lse=lse, workspace=ws)
+    for t, n in ((raw, out.numel()), (lraw, lse.numel())):
+        assert (t[:256] == 5).all() and (t[256 + n:] == 5).all()
+    assert (wraw[:at] == 85).all() and (wraw[at + ws.nbytes:] == 85).all()
+    for T, d in ((3, 72), (2, 1000), (1, 9000)):
+        x, y, dr, dh = (drawn(rng, (T, d), "bf16")[0] for _ in range(4))
+        w = drawn(rng, (d,), "bf16")[0]
+        shapes = [((T, d), torch.bfloat16), ((T, d), torch.bfloat16), ((d,), torch.float32), ((d,), torch.float32),
+                  ((d,), torch.float32)]
+        frames = [framed(*s) for s in shapes]
+        fm.block_norm(x, y, post=w, gate=w, pre=w, out=(frames[0][1], frames[1][1]))
+        fm.block_norm_grad(dr, dh, x, y, post=w, gate=w, pre=w, out=[f[1] for f in frames])
+        for t, o in frames:
+            assert (t[:256] == 5).all() and (t[256 + o.numel():] == 5).all()
