@@ -1,17 +1,24 @@
 // Attention of one new token per slot over the pages of its sequence.
 //
-// A wavefront takes 32 tokens (float32: 16) of a key head at a time, for up to 16
-// query heads that read it.  The pages hold operands: a piece of 1 KB is one load
-// of 16 bytes a lane, whole lines, and the very registers that the matrix
-// instructions take.
+// A wavefront takes a step of 16 to 128 tokens of a key head at a time, 8 KB of keys
+// or more, for up to 16 query heads that read it.  The pages hold operands: a piece
+// of 1 KB is one load of 16 bytes a lane, whole lines, and the very registers that
+// the matrix instructions take.
 //   scores   S^T = K Q^T: rows are tokens, columns are queries.  Lane 16 g + c gets
 //            tokens 4 g .. 4 g + 3 of each block of 16, for query c.
 //   output   O^T += V^T P^T: the same lane must hold P of query c for four tokens
 //            per block, which are the ones it has, so that the probabilities pass
 //            from accumulators to operands without changing lanes.
 // Running maximum and sum per query; the sums and outputs are scaled only when a
-// maximum has grown.  Memory bounds it: 16 queries per key head cost the matrix
-// units 7% of the time that the keys and values take to arrive.
+// maximum has grown.
+//
+// Memory bounds long batches: with bf16, 16 queries per key head cost the matrix units
+// 7% of the time that the keys and values take to arrive (float32, whose instructions
+// are a tenth as fast, a third).  One request of 131,072 tokens, 32 query heads on 8 of
+// 128: 537 MB stream in 77 us (7.0 TB/s) of 90-98 for the call; 64 requests of 1 to
+// 8,192 tokens: 1.02 GB in 160 us.  Short batches are bound by a chain of waits:
+// lengths, table, keys, joins; three requests of 37 tokens take 7.7 us, one of 4,096
+// tokens 14.
 #include "fm_device.h"
 #include "fm_kv.h"
 #include "fm_mma.h"
@@ -20,9 +27,7 @@ namespace fm {
 
 namespace {
 
-constexpr int kAttnWaves = 4;     // wavefronts of a workgroup
-constexpr int kFew = 4;   // steps of a tile that a wavefront takes alone whatever stands beside it
-constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kAttnWaves = 4;   // wavefronts of a workgroup
 constexpr float kLn2 = 0.693147180559945309f;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -72,8 +77,11 @@ struct Wave {
   // CU's four wavefronts have 64 KB and more on their way.
   static constexpr int SB = NP >= 8 ? (kBf ? 2 : 1) : (NP >= 4 ? 2 : (NP == 1 ? 8 : 4));
   static constexpr int OT = NP * (kBf ? 2 : 1);   // tiles of 16 dimensions
-  static constexpr bool kTwo = NP <= (kBf ? 5 : 9);      // registers for two workgroups per CU
-  static constexpr bool kNarrow = NP <= 2;   // weighing short rows takes longer than loading them
+  static constexpr bool kTwo = NP <= (kBf ? 5 : 9);   // registers for two workgroups per CU
+  // Rows so short that weighing a step takes longer than loading it: a second workgroup
+  // fills the time (64 slots of 2,048 tokens, 8 heads of 32 bf16: 47 us and 37; of 64
+  // float32: 101 and 91; heads of 64 bf16, 4,096 tokens: 96 and 93).
+  static constexpr bool kNarrow = NP <= (kBf ? 2 : 4);
   uint32x4 q[NP];
   uint32x4 k[SB][NP], v[SB][NP];
   floatx4 o[OT];
@@ -177,16 +185,32 @@ struct Wave {
   }
 };
 
+// Page numbers of a slot, one per lane: of its table's entries from `base` on.
+struct Known {
+  int base, ids;
+  __device__ __forceinline__ void take(const AttnArgs& a, int slot, int entry) {
+    const int mine = entry + static_cast<int>(threadIdx.x % kWave);
+    base = entry;
+    ids = a.c.table[static_cast<int64_t>(slot) * a.c.max_pages + (mine < a.c.max_pages ? mine : a.c.max_pages - 1)];
+  }
+  // of the first visible token on: sent for as soon as the slot is known
+  __device__ __forceinline__ void begin(const AttnArgs& a, int slot, Seen seen) {
+    if (!seen.none()) take(a, slot, entry_of(a, seen.lo / kBlockTokens));
+  }
+  static __device__ __forceinline__ int entry_of(const AttnArgs& a, int block) {
+    return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(block)) * a.per_page_inv) >> 32);
+  }
+};
+
 // A wavefront's steps [first, last) with a stride of a slot's blocks, counted from
 // the block of the first visible token.
 template <typename T, int NP>
-__device__ __forceinline__ void walk(const AttnArgs& a, Wave<T, NP>& w, int slot, int head, Seen seen, int first,
-                                     int last, int stride, uint32_t& bad) {
+__device__ __forceinline__ void walk(const AttnArgs& a, Wave<T, NP>& w, int slot, int head, Seen seen, Known& known,
+                                     int first, int last, int stride, uint32_t& bad) {
   using W = Wave<T, NP>;
   constexpr int SB = W::SB;
   const int per_page = a.c.page / kBlockTokens;
   const int block_bytes = NP * kPieceBytes;
-  const int32_t* row = a.c.table + static_cast<int64_t>(slot) * a.c.max_pages;
   const char* keys = a.c.pages + a.c.head_offset(a.layer, 0, head);
   const int64_t to_values = a.c.head_offset(0, 1, 0);
   // (through an instruction of its own: a plain load next to a vector product is
@@ -197,21 +221,14 @@ __device__ __forceinline__ void walk(const AttnArgs& a, Wave<T, NP>& w, int slot
 
   // where block b lies, and which of its tokens are seen: none of one that does
   // not exist or whose page does not, which stands at another's place
-  int base = 0, ids = 0;   // a page number per lane, of the table's entries from base on
-  bool filled = false;
   auto locate = [&](int step, const char* (&at)[SB], int (&lo)[SB], int (&hi)[SB]) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < SB; ++i) {
       const int b = b0 + step * SB + i;
       const int bb = b < b1 ? b : b1 - 1;
-      const int entry = static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(bb)) * a.per_page_inv) >> 32);
-      if (!filled || entry >= base + kWave) {
-        base = entry;
-        filled = true;
-        const int mine = entry + static_cast<int>(threadIdx.x % kWave);
-        ids = row[mine < a.c.max_pages ? mine : a.c.max_pages - 1];
-      }
-      int page = __builtin_amdgcn_readlane(ids, entry - base);
+      const int entry = Known::entry_of(a, bb);
+      if (entry < known.base || entry >= known.base + kWave) known.take(a, slot, entry);
+      int page = __builtin_amdgcn_readlane(known.ids, entry - known.base);
       lo[i] = seen.lo - b * kBlockTokens;
       hi[i] = b < b1 ? seen.hi - b * kBlockTokens : 0;
       if (!a.c.valid(page)) {
@@ -463,13 +480,27 @@ __device__ __forceinline__ int ratio(int n, int d) {
 // tile is a part; a tile of several workgroups is joined by the last of them that
 // is done (tickets, no wait), in the order of the line.  No part is shorter than
 // kPart steps: a cut closer to an end of its tile moves there.
+//
+// One workgroup per CU does for long tiles, whose parts it has few of to join: 64
+// requests of 1 to 8,192 tokens 160 us, with two 170; one of 131,072 95 and 100.
+// Where there are more tiles than CUs and they are short, each is a wait for its data
+// and two per CU pay: 64 slots of 8 heads of 128 bf16, mean lengths of 128 / 512 /
+// 1,024 / 2,048 tokens: one 18.9 / 37.0 / 55.0 / 87.9 us, two 15.3 / 33.7 / 52.7 / 90.3
+// (kShort lies between the last two).
 constexpr int kCus = 256;
-constexpr int kWorkers = 2 * kCus;   // workgroups that the line is cut for at most: two on every CU
-constexpr int kOverhead = 8;     // units of a tile besides its steps
-constexpr int kLeast = 8;        // units of a workgroup at least: few tiles have one each
-constexpr int kPart = 4;
-constexpr int kShort = 64;       // units of a tile on average
-constexpr int64_t kLongest = int64_t{kCus} << 29;   // of a line: a workgroup's places are int32
+constexpr int kWorkers = 2 * kCus;   // workgroups that the line is cut for at most
+constexpr int kShort = 64;           // units of a tile on average
+// Units of a tile besides its steps: 64 requests as above 171 us with 4, 160 with 8,
+// 161 with 12.
+constexpr int kOverhead = 8;
+// Units of a workgroup at least, so that few tiles have a workgroup each and long ones
+// are cut fine: one request of 2,160 tokens on one key head 14.4 us with 8, 17.7 with
+// 16, 22.8 with 24.
+constexpr int kLeast = 8;
+constexpr int kPart = 4;             // (8: 26.1 us for 24.4, 23 requests with a window of 1,000)
+// Steps up to which a tile that shares a piece is a wavefront's alone: 103 slots of 4
+// tokens, 32 heads of 128 bf16: 17 us, 35 without; 225 of 2, 3 heads of 256: 12 and 24.
+constexpr int kFew = 4;
 __device__ __forceinline__ int cut(int x, int steps) {   // x: from the tile's first step on
   if (x <= 0) return 0;
   if (x >= steps) return steps;
@@ -555,6 +586,8 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
   int slot = __builtin_amdgcn_readfirstlane(static_cast<int>(where[0]));
   uint32_t bad = 0;
   Seen seen = begin;
+  Known known;
+  known.begin(a, slot, seen);
   int steps = __builtin_amdgcn_readfirstlane(steps_of(seen));
   // the tile that the piece begins in, and where it begins itself: places are
   // counted from the piece's begin
@@ -569,7 +602,8 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
   mine = __builtin_amdgcn_readfirstlane(mine);
   each = __builtin_amdgcn_readfirstlane(each);
   int turn = 0;        // tiles that a wavefront has alone
-  // Tiles of this slot that were passed in the piece, and those that come in groups of one for each wavefront.
+  // Tiles of this slot that the piece has passed, and those that it holds in whole
+  // groups of one for each wavefront.
   int k = 0, groups = 0;
   auto count_groups = [&]() __attribute__((always_inline)) {
     const int first = at < 0 ? 1 : 0;   // (begun before the piece)
@@ -596,13 +630,15 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
     // Short tiles cost little but the wait for their data: each wavefront takes tiles
     // of its own, without barriers and LDS; longer ones only where the piece holds one
     // for every wavefront, of one length.
-    const bool alone = lo == 0 && hi == steps && (steps <= kFew ? steps == 1 || 2 * (kOverhead + steps) <= each : k >= 0 && k < groups);
+    bool alone = lo == 0 && hi == steps;
+    if (steps <= kFew) alone = alone && (steps == 1 || 2 * (kOverhead + steps) <= each);
+    else alone = alone && k >= 0 && k < groups;
     ++k;
     if (lo < hi && !(alone && turn++ % kAttnWaves != wv)) {
       W w;
       w.clear();
       load_queries<T, NP>(a, w, slot, head, tile);
-      walk<T, NP>(a, w, slot, head, seen, alone ? 0 : lo + wv, hi, alone ? 1 : kAttnWaves, bad);
+      walk<T, NP>(a, w, slot, head, seen, known, alone ? 0 : lo + wv, hi, alone ? 1 : kAttnWaves, bad);
       const float l = sum_of_groups(w.l);
       if (alone) {
         if (c < queries) {
@@ -618,37 +654,37 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
             a.lse[row0 + c] = l == 0.0f ? -__builtin_inff() : (w.m + __builtin_amdgcn_logf(l)) * kLn2;
         }
       } else {
-      __syncthreads();   // the tile before this one has left LDS
-      if (g == 0) {
-        sh.m[wv][c] = w.m;
-        sh.l[wv][c] = l;
-      }
-#pragma unroll
-      for (int t = 0; t < W::OT; ++t) *reinterpret_cast<floatx4*>(&sh.o[wv][c][16 * t + 4 * g]) = w.o[t];
-      __syncthreads();
-      bool ends = lo == 0 && hi == steps;
-      if (!ends) {
-        // a workgroup has two parts at most: of a tile that began before its piece
-        // of the line, and of one that goes on behind it
-        store_part(sh, queries, rs, (2 * blockIdx.x + (lo == 0 ? 1u : 0u)) * size);
-        // the workgroups that have the tile's first part and its last
-        const int w0 = static_cast<int>(blockIdx.x) + ratio(step0 + kPart - 1, each);
-        const int w1 = static_cast<int>(blockIdx.x) + ratio(step0 + steps - kPart, each);
-        wait_vmcnt<0>();
-        __syncthreads();
-        if (tid == 0)
-          is_last = __hip_atomic_fetch_add(&tickets[w1], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-                    static_cast<uint32_t>(w1 - w0);
-        __syncthreads();
-        ends = is_last != 0;
-        if (ends) {
-          collect(sh, weights, queries, w1 - w0 + 1, rs, [&](int p) __attribute__((always_inline)) {
-            return (2u * static_cast<uint32_t>(w0 + p) + (p == 0 ? 1u : 0u)) * size;
-          });
-          if (tid == 0) __hip_atomic_store(&tickets[w1], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();   // the tile before this one has left LDS
+        if (g == 0) {
+          sh.m[wv][c] = w.m;
+          sh.l[wv][c] = l;
         }
-      }
-      if (ends) finish<T>(a, sh, row0, queries);
+#pragma unroll
+        for (int t = 0; t < W::OT; ++t) *reinterpret_cast<floatx4*>(&sh.o[wv][c][16 * t + 4 * g]) = w.o[t];
+        __syncthreads();
+        bool ends = lo == 0 && hi == steps;
+        if (!ends) {
+          // a workgroup has two parts at most: of a tile that began before its piece
+          // of the line, and of one that goes on behind it
+          store_part(sh, queries, rs, (2 * blockIdx.x + (lo == 0 ? 1u : 0u)) * size);
+          // the workgroups that have the tile's first part and its last
+          const int w0 = static_cast<int>(blockIdx.x) + ratio(step0 + kPart - 1, each);
+          const int w1 = static_cast<int>(blockIdx.x) + ratio(step0 + steps - kPart, each);
+          wait_vmcnt<0>();
+          __syncthreads();
+          if (tid == 0)
+            is_last = __hip_atomic_fetch_add(&tickets[w1], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                      static_cast<uint32_t>(w1 - w0);
+          __syncthreads();
+          ends = is_last != 0;
+          if (ends) {
+            collect(sh, weights, queries, w1 - w0 + 1, rs, [&](int p) __attribute__((always_inline)) {
+              return (2u * static_cast<uint32_t>(w0 + p) + (p == 0 ? 1u : 0u)) * size;
+            });
+            if (tid == 0) __hip_atomic_store(&tickets[w1], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          }
+        }
+        if (ends) finish<T>(a, sh, row0, queries);
       }
     }
     at += kOverhead + steps;
@@ -659,6 +695,7 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
         if (at >= mine) break;
         ++slot;
         seen = seen_of(a, slot);
+        known.begin(a, slot, seen);
         steps = __builtin_amdgcn_readfirstlane(steps_of(seen));
         count_groups();
       }
@@ -674,9 +711,7 @@ hipError_t launch(const AttnArgs& a, void* workspace, hipStream_t st) {
   // no more workgroups than the longest line would have pieces
   constexpr int SB = Wave<T, NP>::SB;
   const int64_t longest = kOverhead + 1 + (static_cast<int64_t>(a.c.max_pages) * a.c.page / kBlockTokens + SB) / SB;
-  const int64_t line = longest * a.c.n_slots * a.c.heads * a.tiles;
-  if (line >= kLongest) return hipErrorInvalidValue;
-  const int64_t pieces = (line + kOverhead - 1) / kOverhead;
+  const int64_t pieces = (longest * a.c.n_slots * a.c.heads * a.tiles + kLeast - 1) / kLeast;
   uint32_t* tickets = static_cast<uint32_t*>(workspace);
   k_attn<T, NP><<<static_cast<unsigned>(pieces < kWorkers ? pieces : kWorkers), kAttnWaves * kWave, 0, st>>>(
       a, tickets, static_cast<char*>(workspace) + FM_ATTN_TICKET_BYTES,
@@ -687,6 +722,13 @@ hipError_t launch(const AttnArgs& a, void* workspace, hipStream_t st) {
 }  // namespace
 
 static_assert(kWorkers * sizeof(uint32_t) <= FM_ATTN_TICKET_BYTES && FM_ATTN_TICKET_BYTES % kAlign == 0, "tickets");
+
+bool attn_fits(const fm_kv_cache& c, int32_t q_heads) {
+  // a workgroup's places on the line are int32, of a step per block at most
+  const int64_t tile = kOverhead + 1 + static_cast<int64_t>(c.max_pages) * c.page / kBlockTokens;
+  const int64_t tiles = static_cast<int64_t>(c.n_slots) * c.heads * ((q_heads / c.heads + 15) / 16);
+  return tiles <= (int64_t{kCus} << 29) / tile;
+}
 
 size_t attn_workspace_bytes(const fm_kv_cache& c, int32_t q_heads) {
   const int dims = kv_pieces(c.head_dim, c.dtype) * kRowPiece / (c.dtype == FM_BF16 ? 2 : 4);

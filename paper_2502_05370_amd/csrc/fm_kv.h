@@ -81,6 +81,7 @@ struct AttnArgs {
   float* lse;              // [n_slots][q_heads] or null
   uint32_t* flags;
 };
+bool attn_fits(const fm_kv_cache& c, int32_t q_heads);   // whether its sizes can be handled
 size_t attn_workspace_bytes(const fm_kv_cache& c, int32_t q_heads);
 hipError_t launch_attn(const AttnArgs& a, fm_dtype dt, void* workspace, hipStream_t st);
 

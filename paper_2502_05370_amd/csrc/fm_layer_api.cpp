@@ -116,6 +116,9 @@ fm_status check_attn(const fm_kv_cache* c, int32_t q_heads) {
   if (q_heads < 1 || q_heads > 1024) return fail(FM_ERR_INVALID, "q_heads=%d outside [1, 1024]", q_heads);
   if (q_heads % c->heads != 0)
     return fail(FM_ERR_INVALID, "q_heads=%d is not a multiple of heads=%d", q_heads, c->heads);
+  if (!fm::attn_fits(*c, q_heads))
+    return fail(FM_ERR_UNSUPPORTED, "n_slots=%d of %d pages, q_heads=%d: more work than 2^37 blocks", c->n_slots,
+                c->max_pages, q_heads);
   return FM_OK;
 }
 
@@ -224,7 +227,8 @@ fm_status fm_attn_decode(const fm_kv_cache* c, int32_t layer, const void* q, int
   if (fm_status st = check_flags(flags)) return st;
   if (fm_status st = check_rows(q, q_stride, static_cast<int64_t>(q_heads) * c->head_dim, c->dtype, "q")) return st;
   if (window < 0) return fail(FM_ERR_INVALID, "window=%d: 0 (none) or more", window);
-  if (!std::isfinite(scale)) return fail(FM_ERR_INVALID, "scale=%g must be finite", scale);
+  const float scale2 = scale * 1.44269504088896341f;   // log2(e): weights are powers of two
+  if (!std::isfinite(scale2)) return fail(FM_ERR_INVALID, "scale=%g must be finite, with log2(e) times it", scale);
   if (out == nullptr || !aligned(out, 16)) return fail(FM_ERR_INVALID, "out must be non-NULL and 16-byte aligned");
   if (!aligned(first, 4) || !aligned(lse_out, 4)) return fail(FM_ERR_INVALID, "first and lse_out must be 4-byte aligned");
   if (fm_status st = check_buffer(workspace, workspace_bytes, fm::attn_workspace_bytes(*c, q_heads), "workspace"))
@@ -239,7 +243,7 @@ fm_status fm_attn_decode(const fm_kv_cache* c, int32_t layer, const void* q, int
                        (group + 15) / 16,
                        layer,
                        window,
-                       scale * 1.44269504088896341f,
+                       scale2,
                        ((uint64_t{1} << 32) + per_page - 1) / per_page,
                        first,
                        active,

@@ -452,7 +452,7 @@ __global__ void __launch_bounds__(kSumWaves* kWave) k_norm_sum(NormGradArgs a, i
   const int col = static_cast<int>(blockIdx.x) * kWave + lane;
   float v = 0.0f;
   if (col < d) {
-#pragma unroll 4
+#pragma unroll 16   // (all of 256 lists on their way)
     for (int i = wv; i < lists; i += kSumWaves) v += a.partial[(static_cast<int64_t>(i) * 2 + which) * d + col];
   }
   sums[wv][lane] = v;

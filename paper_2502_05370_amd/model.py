@@ -29,7 +29,9 @@ def _call(name: str, device: torch.device, stream, *args) -> None:
     if device.type != "cuda":
         raise ValueError(f"tensors are on {device}, not on a GPU")
     if device.index == torch.cuda.current_device():
-        status = getattr(_LIBRARY, name)(*args, _stream(stream))
+        # (the current stream by the device just looked up, not by another question for it)
+        handle = _raw_stream(device.index) if stream is None and _raw_stream is not None else _stream(stream)
+        status = getattr(_LIBRARY, name)(*args, handle)
     else:
         with torch.cuda.device(device):
             status = getattr(_LIBRARY, name)(*args, _stream(stream))

@@ -57,7 +57,7 @@ def test_cache_refused(fn, change, status):
     ("fm_attn_decode", dict(q_stride=511), 1), ("fm_attn_decode", dict(q_stride=516), 1),
     ("fm_attn_decode", dict(q_heads=0), 1), ("fm_attn_decode", dict(q_heads=7), 1),
     ("fm_attn_decode", dict(q_heads=1026, q_stride=1 << 20), 1), ("fm_attn_decode", dict(window=-1), 1),
-    ("fm_attn_decode", dict(scale=float("nan")), 1), ("fm_attn_decode", dict(scale=float("inf")), 1),
+    ("fm_attn_decode", dict(scale=3e38), 1), ("fm_attn_decode", dict(scale=float("nan")), 1), ("fm_attn_decode", dict(scale=float("inf")), 1),
     ("fm_attn_decode", dict(first=P + 2), 1), ("fm_attn_decode", dict(lse=P + 2), 1), ("fm_attn_decode", dict(out=None), 1),
     ("fm_attn_decode", dict(out=P + 8), 1), ("fm_attn_decode", dict(workspace=None), 1),
     ("fm_attn_decode", dict(workspace=P + 16), 1), ("fm_attn_decode", dict(workspace_bytes=0), 1)])
@@ -65,6 +65,15 @@ def test_calls_refused(fn, change, status):
     desc = L.KvCacheDesc(*CACHE.values())
     assert getattr(lib, fn)(C.byref(desc), *{**ON_CACHE[fn], **change}.values()) == status
     assert (lib.fm_last_error().decode() != "") == (status != 0)
+
+
+def test_more_work_than_places():
+    desc = L.KvCacheDesc(*{**CACHE, "n_slots": 65536, "max_pages": 4096, "page": 1024, "heads": 128}.values())
+    desc.layers, desc.head_dim = 1, 8
+    call = {**ATTN, "q_stride": 4096, "q_heads": 128}
+    assert lib.fm_attn_workspace_bytes(C.byref(desc), 128) == 0
+    assert lib.fm_attn_decode(C.byref(desc), *call.values()) == L.FM_ERR_UNSUPPORTED
+    assert lib.fm_kv_scratch_bytes(C.byref(desc)) > 0
 
 
 @pytest.mark.parametrize("fn", list(ON_CACHE))
