@@ -9,7 +9,11 @@
 //   dz' = e g post         dy = (dz' - y^ mean(dz' y^)) / |y|
 //   dpre = sum over rows of dh r^,  dpost = sum of e g y^
 // with r and n made again from x and y, which costs one more sum over the row and
-// reads no more than the stored r would.  Memory bounds both.
+// reads no more than the stored r would.  Memory bounds both: with a channel's gate and
+// both norms, 8,192 rows of 4,096 in bf16 take 51 us forward (268 MB, 5.2 TB/s; a copy
+// reaches 5.1) and 79 us backward (403 MB, 5.1 TB/s, the sums over the rows 4 of them).
+// Few rows cost their chain of launch, loads, sums and barriers: one row of 1,536 4.5 us,
+// 64 rows of 4,096 backward 8.6.
 #include "fm_device.h"
 #include "fm_norm.h"
 
@@ -516,13 +520,22 @@ hipError_t norm_grad(const NormGradArgs& a, hipStream_t st) {
     }
   };
   using std::integral_constant;
-  // two vectors of every array per thread; four of float32 rows of more than 8,192
-  // values, which spill registers
+  // As few wavefronts as hold the row with one vector of every array per thread, or
+  // two where that leaves one row to a workgroup and lanes idle, or needs more than
+  // eight.  In bf16, with one and with two: 64 rows of 1,024 7.1 us and 10.2, of 4,096
+  // 8.5 and 9.6, 8,192 rows of 4,096 81 and 84; but of 2,304 62 and 53, of 8,192 198
+  // and 157.  67 MB in rows of 1,280 take 93 us on 4 wavefronts and 113 on 4 of two
+  // vectors each.  float32 rows of more than 8,192 values need three or four vectors,
+  // and four spill registers: 700 rows of 12,288 take 74 us with three and 102 with four.
   if (vecs <= kWave) go(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, 8>{});
-  else if (vecs <= 2 * kWave) go(integral_constant<int, 1>{}, integral_constant<int, 2>{}, integral_constant<int, 8>{});
-  else if (vecs <= 8 * kWave) go(integral_constant<int, 4>{}, integral_constant<int, 2>{}, integral_constant<int, 2>{});
+  else if (vecs <= 2 * kWave) go(integral_constant<int, 2>{}, integral_constant<int, 1>{}, integral_constant<int, 4>{});
+  else if (vecs <= 4 * kWave) go(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
+  else if (vecs <= 6 * kWave) go(integral_constant<int, 3>{}, integral_constant<int, 2>{}, integral_constant<int, 2>{});
+  else if (vecs <= 8 * kWave) go(integral_constant<int, 8>{}, integral_constant<int, 1>{}, integral_constant<int, 1>{});
+  else if (vecs <= 12 * kWave) go(integral_constant<int, 6>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
   else if (vecs <= 16 * kWave) go(integral_constant<int, 8>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
   else if (sizeof(T) == 2 || vecs <= 32 * kWave) go(integral_constant<int, 16>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
+  else if (vecs <= 48 * kWave) go(integral_constant<int, 16>{}, integral_constant<int, sizeof(T) == 2 ? 2 : 3>{}, integral_constant<int, 1>{});
   else go(integral_constant<int, 16>{}, integral_constant<int, sizeof(T) == 2 ? 2 : 4>{}, integral_constant<int, 1>{});
   if (a.dpost != nullptr || a.dpre != nullptr || a.f.gate_kind == FM_GATE_CHANNEL)
     k_norm_sum<T><<<dim3(static_cast<unsigned>((a.f.d + kWave - 1) / kWave), 2), kSumWaves * kWave, 0, st>>>(a, lists);
