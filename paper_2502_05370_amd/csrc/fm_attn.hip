@@ -70,7 +70,8 @@ __device__ __forceinline__ Seen seen_of(const AttnArgs& a, int s) {
   return Seen{lo, len};
 }
 
-template <typename T, int NP>
+// ALONE: no other workgroup reads these keys.
+template <typename T, int NP, bool ALONE>
 struct Wave {
   static constexpr bool kBf = sizeof(T) == 2;
   // Blocks of a step: 8 KB of keys or more (bf16 takes blocks in pairs), so that a
@@ -93,10 +94,16 @@ struct Wave {
 #pragma unroll
     for (int t = 0; t < OT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
+  // What no other workgroup reads passes the caches by: with 32 query heads on 8, 64
+  // requests of 1 to 8,192 tokens 160 us, 181 through them; with 24 on each of 4, 133
+  // past them and 127 through them.
   static __device__ __forceinline__ void load(const char* at, uint32x4 (&r)[NP]) {
     const uint32x4* p = reinterpret_cast<const uint32x4*>(at) + threadIdx.x % kWave;
 #pragma unroll
-    for (int t = 0; t < NP; ++t) r[t] = __builtin_nontemporal_load(p + t * (kPieceBytes / 16));
+    for (int t = 0; t < NP; ++t) {
+      if constexpr (ALONE) r[t] = __builtin_nontemporal_load(p + t * (kPieceBytes / 16));
+      else r[t] = p[t * (kPieceBytes / 16)];
+    }
   }
   __device__ __forceinline__ void scores(floatx4 (&s)[SB]) const {
 #pragma unroll
@@ -204,10 +211,10 @@ struct Known {
 
 // A wavefront's steps [first, last) with a stride of a slot's blocks, counted from
 // the block of the first visible token.
-template <typename T, int NP>
-__device__ __forceinline__ void walk(const AttnArgs& a, Wave<T, NP>& w, int slot, int head, Seen seen, Known& known,
+template <typename T, int NP, bool ALONE>
+__device__ __forceinline__ void walk(const AttnArgs& a, Wave<T, NP, ALONE>& w, int slot, int head, Seen seen, Known& known,
                                      int first, int last, int stride, uint32_t& bad) {
-  using W = Wave<T, NP>;
+  using W = Wave<T, NP, ALONE>;
   constexpr int SB = W::SB;
   const int per_page = a.c.page / kBlockTokens;
   const int block_bytes = NP * kPieceBytes;
@@ -279,12 +286,12 @@ __device__ __forceinline__ void walk(const AttnArgs& a, Wave<T, NP>& w, int slot
   }
 }
 
-// Queries of one key head and tile: lane 16 g + c holds 16 bytes of query c per 64.
-template <typename T, int NP>
-__device__ __forceinline__ void load_queries(const AttnArgs& a, Wave<T, NP>& w, int slot, int head, int tile) {
+// Queries of a tile of one key head: lane 16 g + c holds 16 bytes of query c per 64.
+template <typename T, int NP, bool ALONE>
+__device__ __forceinline__ void load_queries(const AttnArgs& a, Wave<T, NP, ALONE>& w, int slot, int head, int query0) {
   constexpr int N = 16 / static_cast<int>(sizeof(T));
   const int lane = threadIdx.x % kWave;
-  const int c = lane % 16 + tile * 16, g = lane / 16;
+  const int c = lane % 16 + query0, g = lane / 16;
   const char* row = a.q + slot * a.q_row + static_cast<int64_t>(head * a.group + c) * a.c.head_dim * sizeof(T);
 #pragma unroll
   for (int t = 0; t < NP; ++t) {
@@ -474,19 +481,29 @@ __device__ __forceinline__ int ratio(int n, int d) {
   return q;
 }
 
-// The batch's work is a line: slot after slot, in it key head after key head (and
-// tile after tile of its queries), in it kOverhead units and one per step.  Every
-// workgroup takes as much of the line, whatever the lengths are.  What it has of a
-// tile is a part; a tile of several workgroups is joined by the last of them that
-// is done (tickets, no wait), in the order of the line.  No part is shorter than
-// kPart steps: a cut closer to an end of its tile moves there.
+// The batch's work is a line: slot after slot, in it key head after key head, in it
+// kOverhead units and one per step.  Every workgroup takes as much of the line,
+// whatever the lengths are.  What it has of a tile, the 16 queries of a key head, is a
+// part; a tile of several workgroups is joined by the last of them that is done
+// (tickets, no wait), in the order of the line.  No part is shorter than kPart steps: a
+// cut closer to an end of its tile moves there.
+//
+// More than 16 queries of a key head are tiles side by side: a piece of the line is
+// taken by a workgroup for each, on one XCD, so that the keys that the first brings are
+// in its L2 for the others: 64 requests of 1 to 8,192 tokens, 24 queries on each of 4
+// bf16 heads of 128 or 256, 127 or 242 us.  One tile behind the other, which reads the
+// keys from memory again, 173 or 345; both in one wavefront's registers 115 or 268, but
+// float32 heads of 256 spill to twice the time, and 8 requests of 1,000 tokens take 25
+// us for 19.  More than kSide tiles take turns.
 //
 // One workgroup per CU does for long tiles, whose parts it has few of to join: 64
 // requests of 1 to 8,192 tokens 160 us, with two 170; one of 131,072 95 and 100.
 // Where there are more tiles than CUs and they are short, each is a wait for its data
 // and two per CU pay: 64 slots of 8 heads of 128 bf16, mean lengths of 128 / 512 /
 // 1,024 / 2,048 tokens: one 18.9 / 37.0 / 55.0 / 87.9 us, two 15.3 / 33.7 / 52.7 / 90.3
-// (kShort lies between the last two).
+// (kShort lies between the last two).  Workgroups side by side are two per CU where
+// registers allow it, so that as many bytes are on their way: 64 requests of 1 to 8,192
+// tokens, 24 queries on each of 4 heads of 128 bf16: one 158 us, two 133.
 constexpr int kCus = 256;
 constexpr int kWorkers = 2 * kCus;   // workgroups that the line is cut for at most
 constexpr int kShort = 64;           // units of a tile on average
@@ -497,6 +514,8 @@ constexpr int kOverhead = 8;
 // are cut fine: one request of 2,160 tokens on one key head 14.4 us with 8, 17.7 with
 // 16, 22.8 with 24.
 constexpr int kLeast = 8;
+constexpr int kSide = 8;             // tiles side by side
+constexpr int kXcds = 8;             // that take workgroups in turn
 constexpr int kPart = 4;             // (8: 26.1 us for 24.4, 23 requests with a window of 1,000)
 // Steps up to which a tile that shares a piece is a wavefront's alone: 103 slots of 4
 // tokens, 32 heads of 128 bf16: 17 us, 35 without; 225 of 2, 3 heads of 256: 12 and 24.
@@ -507,10 +526,21 @@ __device__ __forceinline__ int cut(int x, int steps) {   // x: from the tile's f
   return x < kPart ? 0 : (x > steps - kPart ? steps : x);
 }
 
-template <typename T, int NP>
-__global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1))
-    k_attn(AttnArgs a, uint32_t* tickets, char* parts, uint32_t parts_bytes) {
-  using W = Wave<T, NP>;
+struct Sides {
+  int32_t turns, side;   // tiles of a key head: turns x side or a few less
+  int32_t pieces;        // that the line is cut into at most, of which `side` workgroups take each
+};
+Sides sides_of(int32_t group) {
+  const int32_t tiles = (group + 15) / 16;
+  const int32_t turns = (tiles + kSide - 1) / kSide;
+  const int32_t side = (tiles + turns - 1) / turns;
+  return Sides{turns, side, kWorkers / side / kXcds * kXcds};
+}
+
+template <typename T, int NP, bool ALONE>
+__global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP, ALONE>::kTwo ? 2 : 1))
+    k_attn(AttnArgs a, Sides sides_given, uint32_t* tickets, char* parts, uint32_t parts_bytes) {
+  using W = Wave<T, NP, ALONE>;
   constexpr int kDims = NP * kRowPiece / static_cast<int>(sizeof(T));
   constexpr int NT = kAttnWaves * kWave;
   __shared__ Joined<kDims> sh;
@@ -523,7 +553,11 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
   const int lane = tid % kWave;
   const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int c = lane % 16, g = lane / 16;
-  const int per_slot = a.c.heads * a.tiles;
+  const Sides sides = ALONE ? Sides{1, 1, kWorkers} : sides_given;
+  const int per_slot = a.c.heads * sides.turns;
+  const int piece =
+      static_cast<int>(ALONE ? blockIdx.x : blockIdx.x / (kXcds * sides.side) * kXcds + blockIdx.x % kXcds);
+  const int beside = static_cast<int>(ALONE ? 0 : blockIdx.x / kXcds % sides.side);
   auto steps_of = [&](Seen w) __attribute__((always_inline)) {
     const int blocks = w.none() ? 0 : (w.hi + kBlockTokens - 1) / kBlockTokens - w.lo / kBlockTokens;
     return (blocks + W::SB - 1) / W::SB;
@@ -571,10 +605,10 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
     // One workgroup per CU, or two: where short tiles, more than CUs, each wait for
     // their data.
     const int64_t tiles = static_cast<int64_t>(a.c.n_slots) * per_slot;
-    const bool two = W::kTwo && (W::kNarrow || (tiles > kCus && passed < kShort * tiles));
-    each = static_cast<int>((passed + kWorkers - 1) / kWorkers) * (two ? 1 : 2);
+    const bool two = W::kTwo && (W::kNarrow || !ALONE || (tiles > kCus && passed < kShort * tiles));
+    each = static_cast<int>((passed + sides.pieces - 1) / sides.pieces) * (two ? 1 : 2);
     if (each < kLeast) each = kLeast;
-    from = static_cast<int64_t>(each) * blockIdx.x;
+    from = static_cast<int64_t>(each) * piece;
     if (from >= passed) return;
     mine = passed - from < each ? static_cast<int>(passed - from) : each;
     if (a.c.n_slots <= NT) {
@@ -598,7 +632,7 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
   tile0 = __builtin_amdgcn_readfirstlane(tile0);
   int at = __builtin_amdgcn_readfirstlane(
       static_cast<int>(static_cast<int64_t>(tile0) * (kOverhead + steps) - back));
-  int head = tile0 / a.tiles, tile = tile0 % a.tiles;
+  int head = tile0 / sides.turns, round = tile0 % sides.turns;
   mine = __builtin_amdgcn_readfirstlane(mine);
   each = __builtin_amdgcn_readfirstlane(each);
   int turn = 0;        // tiles that a wavefront has alone
@@ -607,22 +641,28 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
   int k = 0, groups = 0;
   auto count_groups = [&]() __attribute__((always_inline)) {
     const int first = at < 0 ? 1 : 0;   // (begun before the piece)
-    const int here = per_slot - (head * a.tiles + tile);
+    const int here = per_slot - (head * sides.turns + round);
     const int whole = ratio(mine - at, kOverhead + steps);
     k = -first;
     groups = ((here < whole ? here : whole) - first) / kAttnWaves * kAttnWaves;
   };
   count_groups();
+  // a workgroup has two parts at most: of a tile that began before its piece of the
+  // line, and of one that goes on behind it
   const uint32_t size = part_bytes(a.group, kDims);
+  auto part_at = [&](int of, bool goes_on) __attribute__((always_inline)) {
+    return (2u * static_cast<uint32_t>(of * sides.side + beside) + (goes_on ? 1u : 0u)) * size;
+  };
   const __amdgpu_buffer_rsrc_t rs = row_buffer(parts, parts_bytes);
   while (at < mine) {
-    const int queries = a.group - tile * 16 < 16 ? a.group - tile * 16 : 16;
-    const int row0 = slot * a.q_heads + head * a.group + tile * 16;
+    const int query0 = (round * sides.side + beside) * 16;
+    const int queries = a.group - query0 < 16 ? a.group - query0 : 16;   // (none: zero or less)
+    const int row0 = slot * a.q_heads + head * a.group + query0;
     // this workgroup's steps of the tile
     const int step0 = at + kOverhead;
     const int lo = cut(-step0, steps);
     const int hi = cut(mine - step0, steps);
-    if (steps == 0 && at >= 0) {
+    if (steps == 0 && at >= 0) {   // (no turn of a loop where there are no queries)
       for (int i = tid; i < queries * a.c.head_dim / 4; i += NT)
         store4<T>(a.out, static_cast<int64_t>(row0) * a.c.head_dim + i * 4, floatx4{0.f, 0.f, 0.f, 0.f});
       if (a.lse != nullptr && tid < queries) a.lse[row0 + tid] = -__builtin_inff();
@@ -634,11 +674,11 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
     if (steps <= kFew) alone = alone && (steps == 1 || 2 * (kOverhead + steps) <= each);
     else alone = alone && k >= 0 && k < groups;
     ++k;
-    if (lo < hi && !(alone && turn++ % kAttnWaves != wv)) {
+    if (lo < hi && queries > 0 && !(alone && turn++ % kAttnWaves != wv)) {
       W w;
       w.clear();
-      load_queries<T, NP>(a, w, slot, head, tile);
-      walk<T, NP>(a, w, slot, head, seen, known, alone ? 0 : lo + wv, hi, alone ? 1 : kAttnWaves, bad);
+      load_queries(a, w, slot, head, query0);
+      walk(a, w, slot, head, seen, known, alone ? 0 : lo + wv, hi, alone ? 1 : kAttnWaves, bad);
       const float l = sum_of_groups(w.l);
       if (alone) {
         if (c < queries) {
@@ -664,32 +704,31 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
         __syncthreads();
         bool ends = lo == 0 && hi == steps;
         if (!ends) {
-          // a workgroup has two parts at most: of a tile that began before its piece
-          // of the line, and of one that goes on behind it
-          store_part(sh, queries, rs, (2 * blockIdx.x + (lo == 0 ? 1u : 0u)) * size);
+          store_part(sh, queries, rs, part_at(piece, lo == 0));
           // the workgroups that have the tile's first part and its last
-          const int w0 = static_cast<int>(blockIdx.x) + ratio(step0 + kPart - 1, each);
-          const int w1 = static_cast<int>(blockIdx.x) + ratio(step0 + steps - kPart, each);
+          const int w0 = piece + ratio(step0 + kPart - 1, each);
+          const int w1 = piece + ratio(step0 + steps - kPart, each);
+          uint32_t* ticket = tickets + (w1 * sides.side + beside);
           wait_vmcnt<0>();
           __syncthreads();
           if (tid == 0)
-            is_last = __hip_atomic_fetch_add(&tickets[w1], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+            is_last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
                       static_cast<uint32_t>(w1 - w0);
           __syncthreads();
           ends = is_last != 0;
           if (ends) {
             collect(sh, weights, queries, w1 - w0 + 1, rs, [&](int p) __attribute__((always_inline)) {
-              return (2u * static_cast<uint32_t>(w0 + p) + (p == 0 ? 1u : 0u)) * size;
+              return part_at(w0 + p, p == 0);
             });
-            if (tid == 0) __hip_atomic_store(&tickets[w1], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (tid == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
           }
         }
         if (ends) finish<T>(a, sh, row0, queries);
       }
     }
     at += kOverhead + steps;
-    if (++tile == a.tiles) {
-      tile = 0;
+    if (++round == sides.turns) {
+      round = 0;
       if (++head == a.c.heads) {
         head = 0;
         if (at >= mine) break;
@@ -706,17 +745,29 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP>::kTwo ? 2 : 1
 
 uint32_t parts_bytes(int32_t group, int dims) { return 2u * kWorkers * part_bytes(group, dims); }
 
-template <typename T, int NP>
+template <typename T, int NP, bool ALONE>
 hipError_t launch(const AttnArgs& a, void* workspace, hipStream_t st) {
+  const Sides sides = sides_of(a.group);
   // no more workgroups than the longest line would have pieces
-  constexpr int SB = Wave<T, NP>::SB;
+  constexpr int SB = Wave<T, NP, ALONE>::SB;
   const int64_t longest = kOverhead + 1 + (static_cast<int64_t>(a.c.max_pages) * a.c.page / kBlockTokens + SB) / SB;
-  const int64_t pieces = (longest * a.c.n_slots * a.c.heads * a.tiles + kLeast - 1) / kLeast;
+  const int64_t pieces = (longest * a.c.n_slots * a.c.heads * sides.turns + kLeast - 1) / kLeast;
+  const int64_t taken = pieces < sides.pieces ? (pieces + kXcds - 1) / kXcds * kXcds : sides.pieces;
   uint32_t* tickets = static_cast<uint32_t*>(workspace);
-  k_attn<T, NP><<<static_cast<unsigned>(pieces < kWorkers ? pieces : kWorkers), kAttnWaves * kWave, 0, st>>>(
-      a, tickets, static_cast<char*>(workspace) + FM_ATTN_TICKET_BYTES,
+  k_attn<T, NP, ALONE><<<static_cast<unsigned>(taken * sides.side), kAttnWaves * kWave, 0, st>>>(
+      a, sides, tickets, static_cast<char*>(workspace) + FM_ATTN_TICKET_BYTES,
       parts_bytes(a.group, NP * kRowPiece / static_cast<int>(sizeof(T))));
   return hipGetLastError();
+}
+
+template <typename T, int NP = 1>
+hipError_t launch_pieces(const AttnArgs& a, void* workspace, hipStream_t st) {
+  if constexpr (NP > kMaxHeadDim * static_cast<int>(sizeof(T)) / kRowPiece)
+    return hipErrorInvalidValue;
+  else if (a.c.pieces != NP)
+    return launch_pieces<T, NP + 1>(a, workspace, st);
+  else
+    return a.group <= 16 ? launch<T, NP, true>(a, workspace, st) : launch<T, NP, false>(a, workspace, st);
 }
 
 }  // namespace
@@ -726,8 +777,9 @@ static_assert(kWorkers * sizeof(uint32_t) <= FM_ATTN_TICKET_BYTES && FM_ATTN_TIC
 bool attn_fits(const fm_kv_cache& c, int32_t q_heads) {
   // a workgroup's places on the line are int32, of a step per block at most
   const int64_t tile = kOverhead + 1 + static_cast<int64_t>(c.max_pages) * c.page / kBlockTokens;
-  const int64_t tiles = static_cast<int64_t>(c.n_slots) * c.heads * ((q_heads / c.heads + 15) / 16);
-  return tiles <= (int64_t{kCus} << 29) / tile;
+  const Sides sides = sides_of(q_heads / c.heads);
+  const int64_t tiles = static_cast<int64_t>(c.n_slots) * c.heads * sides.turns;
+  return tiles <= (static_cast<int64_t>(sides.pieces) << 28) / tile;
 }
 
 size_t attn_workspace_bytes(const fm_kv_cache& c, int32_t q_heads) {
@@ -736,38 +788,7 @@ size_t attn_workspace_bytes(const fm_kv_cache& c, int32_t q_heads) {
 }
 
 hipError_t launch_attn(const AttnArgs& a, fm_dtype dt, void* workspace, hipStream_t st) {
-  if (dt == FM_BF16) {
-    switch (a.c.pieces) {
-      case 1: return launch<uint16_t, 1>(a, workspace, st);
-      case 2: return launch<uint16_t, 2>(a, workspace, st);
-      case 3: return launch<uint16_t, 3>(a, workspace, st);
-      case 4: return launch<uint16_t, 4>(a, workspace, st);
-      case 5: return launch<uint16_t, 5>(a, workspace, st);
-      case 6: return launch<uint16_t, 6>(a, workspace, st);
-      case 7: return launch<uint16_t, 7>(a, workspace, st);
-      case 8: return launch<uint16_t, 8>(a, workspace, st);
-      default: return hipErrorInvalidValue;
-    }
-  }
-  switch (a.c.pieces) {
-    case 1: return launch<float, 1>(a, workspace, st);
-    case 2: return launch<float, 2>(a, workspace, st);
-    case 3: return launch<float, 3>(a, workspace, st);
-    case 4: return launch<float, 4>(a, workspace, st);
-    case 5: return launch<float, 5>(a, workspace, st);
-    case 6: return launch<float, 6>(a, workspace, st);
-    case 7: return launch<float, 7>(a, workspace, st);
-    case 8: return launch<float, 8>(a, workspace, st);
-    case 9: return launch<float, 9>(a, workspace, st);
-    case 10: return launch<float, 10>(a, workspace, st);
-    case 11: return launch<float, 11>(a, workspace, st);
-    case 12: return launch<float, 12>(a, workspace, st);
-    case 13: return launch<float, 13>(a, workspace, st);
-    case 14: return launch<float, 14>(a, workspace, st);
-    case 15: return launch<float, 15>(a, workspace, st);
-    case 16: return launch<float, 16>(a, workspace, st);
-    default: return hipErrorInvalidValue;
-  }
+  return dt == FM_BF16 ? launch_pieces<uint16_t>(a, workspace, st) : launch_pieces<float>(a, workspace, st);
 }
 
 }  // namespace fm

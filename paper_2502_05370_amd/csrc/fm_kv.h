@@ -9,6 +9,7 @@ namespace fm {
 constexpr int kBlockTokens = 16;     // tokens of a block
 constexpr int kPieceBytes = 1024;    // 64 bytes of each of its rows
 constexpr int kRowPiece = 64;        // bytes of a row in a piece
+constexpr int kMaxHeadDim = 256;
 
 // A cache as the kernels take it.  rows of a head are `pieces` x 64 bytes.
 struct KvArgs {
@@ -71,7 +72,6 @@ struct AttnArgs {
   const char* q;
   int64_t q_row;           // bytes
   int32_t q_heads, group;  // query heads, and those per key head
-  int32_t tiles;           // of 16 query heads per key head
   int32_t layer, window;
   float scale2;            // scale times log2(e)
   uint64_t per_page_inv;   // 2^32 over the blocks of a page, rounded up: exact for up to 2^26 blocks

@@ -31,8 +31,8 @@ fm_status check_page(int32_t layers, int32_t heads, int32_t head_dim, int32_t pa
   if (layers < 1 || layers > 1024) return fail(FM_ERR_INVALID, "layers=%d outside [1, 1024]", layers);
   if (heads < 1 || heads > 1024) return fail(FM_ERR_INVALID, "heads=%d outside [1, 1024]", heads);
   if (head_dim < 1 || page < 1) return fail(FM_ERR_INVALID, "head_dim=%d page=%d: at least 1", head_dim, page);
-  if (head_dim % 8 != 0 || head_dim > 256)
-    return fail(FM_ERR_UNSUPPORTED, "head_dim=%d is not a multiple of 8 up to 256", head_dim);
+  if (head_dim % 8 != 0 || head_dim > fm::kMaxHeadDim)
+    return fail(FM_ERR_UNSUPPORTED, "head_dim=%d is not a multiple of 8 up to %d", head_dim, fm::kMaxHeadDim);
   if (page % 16 != 0 || page > 1024) return fail(FM_ERR_UNSUPPORTED, "page=%d is not a multiple of 16 up to 1024", page);
   if (fm::kv_page_bytes(layers, heads, head_dim, page, dt) > kMaxPageBytes)
     return fail(FM_ERR_UNSUPPORTED, "a page of %d tokens exceeds %lld bytes", page,
@@ -240,7 +240,6 @@ fm_status fm_attn_decode(const fm_kv_cache* c, int32_t layer, const void* q, int
                        q_stride * static_cast<int64_t>(elem(c->dtype)),
                        q_heads,
                        group,
-                       (group + 15) / 16,
                        layer,
                        window,
                        scale2,

@@ -9,10 +9,10 @@
 //   dz' = e g post         dy = (dz' - y^ mean(dz' y^)) / |y|
 //   dpre = sum over rows of dh r^,  dpost = sum of e g y^
 // with r and n made again from x and y, which costs one more sum over the row and
-// reads no more than the stored r would.  Memory bounds both: with a channel's gate and
+// reads no more than the stored r would.  Memory bounds both: with a gate and
 // both norms, 8,192 rows of 4,096 in bf16 take 51 us forward (268 MB, 5.2 TB/s; a copy
 // reaches 5.1) and 79 us backward (403 MB, 5.1 TB/s, the sums over the rows 4 of them).
-// Few rows cost their chain of launch, loads, sums and barriers: one row of 1,536 4.5 us,
+// Few rows cost their chain of launch, loads, sums and barriers: one row of 2,048 4.5 us,
 // 64 rows of 4,096 backward 8.6.
 #include "fm_device.h"
 #include "fm_norm.h"

@@ -101,6 +101,25 @@ def test_windows_first_tokens_and_idle_slots(window, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group,heads,head_dim", [
+    (17, 1, 32), (24, 2, 64), (31, 1, 72), (32, 2, 96), (33, 1, 128), (48, 1, 128), (24, 1, 160), (17, 2, 176),
+    (50, 1, 200), (20, 1, 224), (32, 1, 256), (128, 1, 64), (24, 1, 16), (18, 1, 56), (40, 1, 208)])
+def test_more_than_sixteen_queries_per_key_head(group, heads, head_dim, dtype):
+    """Tiles of 32 queries, whole and not; sequences that are one wavefront's, a workgroup's, and cut."""
+    print(f"group={group} heads={heads} head_dim={head_dim} {dtype}", flush=True)
+    rng = np.random.default_rng(group + head_dim)
+    for length, window in (([1, 0, 16, 37, 250, 3], 0), ([5000, 2, 1300], 0), ([700, 90], 333)):
+        cache, k, v = filled(rng, length, heads, head_dim, 32, dtype)
+        q, qn = drawn(rng, (len(length), group * heads, head_dim), dtype)
+        lse = torch.empty(len(length), group * heads, device="cuda")
+        got = _fm().attn_decode(cache, 0, q, window=window, lse=lse)
+        lo = [max(0, n - window) if window else 0 for n in length]
+        check(got, lse, qn, k, v, np.float32(head_dim ** -0.5), dtype, lo)
+        assert cache.check() == 0
+        assert torch.equal(got, _fm().attn_decode(cache, 0, q, window=window))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("scale,spread", [(2.0, 4.0), (-1.5, 2.0), (0.0, 1.0), (1e-4, 1.0), (30.0, 3.0)])
 def test_scores_of_any_size(scale, spread, dtype):
     """Sharp and flat weights, negative scales; scores in the thousands."""
