@@ -20,6 +20,9 @@ It is a plain, slow, obviously correct restatement of what the paper defines:
 * ``operators`` the model operators around the search (embedding lookup, pooling
   and gradient, an MoE layer's gate and experts), with bounds on what a float32
   computation may be off by.
+* ``layer``    the attention half of a serving iteration's layer (a cache's pages,
+  one token's attention over them, the norms around a block and their gradient),
+  whose values carry such bounds along.
 
 Every function is pinned by the ``-m "not gpu"`` tests against closed forms,
 invariants and brute force, including the similarity-weighted blend with
