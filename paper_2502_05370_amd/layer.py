@@ -135,13 +135,18 @@ def attn_workspace_bytes(cache: KvCache, q_heads: int) -> int:
 
 class AttnWorkspace:
     """Device scratch for attn_decode calls of q_heads query heads on a cache.  Calls sharing one must be ordered; all
-    layers may share one.  Its first bytes count parts of split sequences: zeros between calls."""
+    layers may share one.  Its first bytes count parts of split sequences: zeros between calls.  The zeros of one that is
+    made during a graph's capture come with that graph's replays only, so every call with it brings its own."""
 
     def __init__(self, cache: KvCache, q_heads: int):
         self.nbytes = attn_workspace_bytes(cache, q_heads)
         if self.nbytes == 0:
             raise ValueError(f"invalid workspace request q_heads={q_heads} for {cache.heads} heads")
         self.buf = _aligned_bytes(self.nbytes, cache.device)
+        self.in_capture = cache.device.type == "cuda" and torch.cuda.is_current_stream_capturing()
+        self.clear()
+
+    def clear(self) -> None:
         self.buf[:_lib.FM_ATTN_TICKET_BYTES].zero_()
 
 
@@ -254,8 +259,9 @@ def attn_decode(cache: KvCache, layer: int, q: torch.Tensor, scale: Optional[flo
     parts of longer ones) -> [slots][q_heads][head_dim].  scale defaults to head_dim ** -0.5; the last ``window`` tokens
     are seen (0: all), from place first[s] on (int32 [slots]); slots where active [slots] uint8 is 0, and queries that
     see no token, give zeros.  ``lse`` [slots][q_heads] float32 takes the log of each query's sum of weights.  Without
-    ``workspace`` the cache's own of the stream serves the call; replays of a graph that captured such a call must be
-    ordered with each other and with the later calls on the stream of the capture."""
+    ``workspace`` the cache's own of the stream serves the call (cache.ensure_workspace before a capture saves it a fill per
+    call); replays of a graph that captured such a call must be ordered with each other and with the later calls on the
+    stream of the capture."""
     dev = cache.device
     q_ptr, q_stride, _, q_heads = _rows(q, "q", cache.dtype, cache.slots, None, cache.head_dim, dev)
     if out is None:
@@ -275,6 +281,9 @@ def attn_decode(cache: KvCache, layer: int, q: torch.Tensor, scale: Optional[flo
             raise ValueError(f"q has {q_heads} heads, not a multiple of the cache's {cache.heads}")
         workspace = cache.ensure_workspace(q_heads, stream)
     _need(workspace.buf, "workspace", torch.uint8, (workspace.nbytes,), dev)
+    if workspace.in_capture:
+        with _on(stream):
+            workspace.clear()
     _call("fm_attn_decode", dev, stream, cache.desc, layer, q_ptr, q_stride, q_heads,
           cache.head_dim ** -0.5 if scale is None else scale, window, _ptr(first), _ptr(active), out.data_ptr(),
           _ptr(lse), _flags(cache.flags, dev), workspace.buf.data_ptr(), workspace.nbytes)

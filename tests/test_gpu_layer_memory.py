@@ -173,6 +173,37 @@ def test_a_workspace_made_during_a_capture():
     _replays(graph, [out], [want], lambda: fm.attn_decode(cache, 0, q, window=100))
 
 
+def test_graphs_and_calls_with_a_workspace_of_another_graphs_capture():
+    """A workspace that the first of two captures made: the second graph runs first, then an eager call on the stream of
+    the capture, whatever that memory held."""
+    fm = _fm()
+    rng = np.random.default_rng(14)
+    cache, *_ = filled(rng, [6000, 40], 2, 64, 16, "bf16")
+    q, _ = drawn(rng, (2, 6, 64), "bf16")
+    want = fm.attn_decode(cache, 0, q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs, outs = [], []
+    for _ in range(2):
+        outs.append(torch.zeros_like(want))
+        graphs.append(torch.cuda.CUDAGraph())
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graphs[-1], stream=side):
+            fm.attn_decode(cache, 0, q, out=outs[-1])
+    for which in (1, None, 0, 1, None):
+        with torch.cuda.stream(side):
+            cache.ensure_workspace(6).buf.fill_(1)   # what memory that nothing has cleared might hold
+            out = torch.zeros_like(want)
+            if which is None:
+                fm.attn_decode(cache, 0, q, out=out)
+            else:
+                outs[which].zero_()
+                graphs[which].replay()
+                out.copy_(outs[which])
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), which
+
+
 def test_a_graph_outlives_the_growth_of_the_workspace():
     """A captured call of few query heads; then calls of more, which need a larger workspace, and memory that other work
     takes."""
