@@ -107,6 +107,7 @@ fm_status rows_call(const fm_kv_cache* c, int32_t layer, void* k, int64_t k_stri
   const int64_t width = static_cast<int64_t>(c->heads) * c->head_dim;
   if (fm_status st = check_rows(k, k_stride, width, c->dtype, "k")) return st;
   if (fm_status st = check_rows(v, v_stride, width, c->dtype, "v")) return st;
+  if (read && k == v) return fail(FM_ERR_INVALID, "k and v must not be the same");
   const fm::KvRows r{k, v, k_stride, v_stride, offsets, T, layer, active, flags};
   const hipError_t e = fm::launch_kv_rows(*c, r, read, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, read ? "cache read launch" : "cache write launch");
@@ -230,6 +231,7 @@ fm_status fm_attn_decode(const fm_kv_cache* c, int32_t layer, const void* q, int
   const float scale2 = scale * 1.44269504088896341f;   // log2(e): weights are powers of two
   if (!std::isfinite(scale2)) return fail(FM_ERR_INVALID, "scale=%g must be finite, with log2(e) times it", scale);
   if (out == nullptr || !aligned(out, 16)) return fail(FM_ERR_INVALID, "out must be non-NULL and 16-byte aligned");
+  if (out == q) return fail(FM_ERR_INVALID, "out must not be q");
   if (!aligned(first, 4) || !aligned(lse_out, 4)) return fail(FM_ERR_INVALID, "first and lse_out must be 4-byte aligned");
   if (fm_status st = check_buffer(workspace, workspace_bytes, fm::attn_workspace_bytes(*c, q_heads), "workspace"))
     return st;
@@ -262,6 +264,7 @@ fm_status fm_block_norm(const void* x, const void* y, const void* post, const vo
   if ((y == nullptr) != (r_out == nullptr)) return fail(FM_ERR_INVALID, "r_out must be given exactly where y is");
   if ((pre == nullptr) != (h_out == nullptr)) return fail(FM_ERR_INVALID, "h_out must be given exactly where pre is");
   if (!aligned(r_out, 16) || !aligned(h_out, 16)) return fail(FM_ERR_INVALID, "outputs must be 16-byte aligned");
+  if (r_out == h_out) return fail(FM_ERR_INVALID, "r_out and h_out must not be the same");
   const fm::NormArgs a{x, y, post, gate, pre, gate_kind, scale, eps, T, d, r_out, h_out};
   const hipError_t e = fm::launch_norm(a, dtype, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ok() : hip_fail(e, "norm launch");
@@ -290,6 +293,10 @@ fm_status fm_block_norm_grad(const void* dr, const void* dh, const void* x, cons
   if (!aligned(dr, 16) || !aligned(dh, 16) || !aligned(dx, 16) || !aligned(dy, 16) || !aligned(dpost, 4) ||
       !aligned(dpre, 4) || !aligned(dgate, gate_kind == FM_GATE_EACH ? 16 : 4))
     return fail(FM_ERR_INVALID, "gradients of [T][d] must be 16-byte aligned, the others 4-byte aligned");
+  const void* outs[] = {dx, dy, dpost, dgate, dpre};
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < i; ++j)
+      if (outs[i] != nullptr && outs[i] == outs[j]) return fail(FM_ERR_INVALID, "no two gradients may be the same");
   if (fm_status st = check_buffer(scratch, scratch_bytes, fm::norm_scratch_bytes(T, d), "scratch")) return st;
   const fm::NormGradArgs a{{x, y, post, gate, pre, gate_kind, scale, eps, T, d, nullptr, nullptr},
                            dr, dh, accumulate, dx, dy, dpost, dgate, dpre, static_cast<float*>(scratch)};

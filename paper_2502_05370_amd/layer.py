@@ -210,6 +210,13 @@ def _rows(t, name: str, dtype, T: Optional[int], heads: Optional[int], head_dim:
     return t.data_ptr(), row if T > 1 else H * D, T, H
 
 
+def _int32(n: int, name: str) -> int:
+    """n, which ctypes would cut to 32 bits."""
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name}={n} does not fit 32 bits")
+    return n
+
+
 def _token_rows(name: str, cache: KvCache, layer: int, k, v, offsets, active, stream) -> None:
     dev = cache.device
     slots = cache.slots if offsets is None else None
@@ -221,7 +228,7 @@ def _token_rows(name: str, cache: KvCache, layer: int, k, v, offsets, active, st
         _need(offsets, "offsets", torch.int32, (cache.slots + 1,), dev)
     if active is not None:
         _need(active, "active", torch.uint8, (cache.slots,), dev)
-    _call(name, dev, stream, cache.desc, layer, k_ptr, k_stride, v_ptr, v_stride, _ptr(offsets), T, _ptr(active),
+    _call(name, dev, stream, cache.desc, _int32(layer, "layer"), k_ptr, k_stride, v_ptr, v_stride, _ptr(offsets), T, _ptr(active),
           _flags(cache.flags, dev))
 
 
@@ -284,8 +291,8 @@ def attn_decode(cache: KvCache, layer: int, q: torch.Tensor, scale: Optional[flo
     if workspace.in_capture:
         with _on(stream):
             workspace.clear()
-    _call("fm_attn_decode", dev, stream, cache.desc, layer, q_ptr, q_stride, q_heads,
-          cache.head_dim ** -0.5 if scale is None else scale, window, _ptr(first), _ptr(active), out.data_ptr(),
+    _call("fm_attn_decode", dev, stream, cache.desc, _int32(layer, "layer"), q_ptr, q_stride, q_heads,
+          cache.head_dim ** -0.5 if scale is None else scale, _int32(window, "window"), _ptr(first), _ptr(active), out.data_ptr(),
           _ptr(lse), _flags(cache.flags, dev), workspace.buf.data_ptr(), workspace.nbytes)
     return out
 
@@ -345,6 +352,8 @@ def block_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None, post: Optional
         h = _new(shape, dtype, dev, stream)
     elif not _usual(h, dtype, shape, dev):
         _need(h, "out[1] (h)", dtype, shape, dev)
+    if out is not None and r is not None and h is not None and r.data_ptr() == h.data_ptr() != 0:
+        raise ValueError("out must be two tensors, not the same twice")
     _call("fm_block_norm", dev, stream, x.data_ptr(), _ptr(y), _ptr(post), _ptr(gate), kind, scale, _ptr(pre), eps,
           shape[0], shape[1], _CODE[dtype], _ptr(r), _ptr(h))
     return (x if r is None else r), h
@@ -404,6 +413,9 @@ def block_norm_grad(dr: Optional[torch.Tensor], dh: Optional[torch.Tensor], x: t
                     raise ValueError(f"out[{i}] ({_GRADS[i]}) must be None: its input is")
             elif not _usual(t, w[1], w[0], dev):
                 _need(t, f"out[{i}] ({_GRADS[i]})", w[1], w[0], dev)
+        places = [t.data_ptr() for t in out if t is not None and t.numel() != 0]
+        if len(set(places)) != len(places):
+            raise ValueError("out must be different tensors, not the same twice")
     if scratch is None:
         with _on(stream):
             scratch = BlockNormScratch(T, d, dev)

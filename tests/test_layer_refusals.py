@@ -18,8 +18,8 @@ RESIZE = dict(delta=P, granted=None, flags=None, scratch=P, scratch_bytes=1 << 2
 FORK = dict(parent=P, flags=None, scratch=P, scratch_bytes=1 << 20, stream=None)
 COMPACT = dict(live=None, flags=None, scratch=P, scratch_bytes=1 << 20, stream=None)
 COPY = dict(src=P, dst=P, n=3, flags=None, scratch=P, scratch_bytes=1 << 20, stream=None)
-ROWS = dict(layer=1, k=P, k_stride=128, v=P, v_stride=128, offsets=None, T=4, active=None, flags=None, stream=None)
-ATTN = dict(layer=0, q=P, q_stride=512, q_heads=8, scale=0.1, window=0, first=None, active=None, out=P, lse=None,
+ROWS = dict(layer=1, k=P, k_stride=128, v=2 * P, v_stride=128, offsets=None, T=4, active=None, flags=None, stream=None)
+ATTN = dict(layer=0, q=P, q_stride=512, q_heads=8, scale=0.1, window=0, first=None, active=None, out=2 * P, lse=None,
             flags=None, workspace=P, workspace_bytes=1 << 28, stream=None)
 ON_CACHE = {"fm_kv_resize": RESIZE, "fm_kv_fork": FORK, "fm_kv_compact": COMPACT, "fm_kv_copy": COPY,
             "fm_kv_write": ROWS, "fm_kv_read": ROWS, "fm_attn_decode": ATTN}
@@ -52,14 +52,14 @@ def test_cache_refused(fn, change, status):
     ("fm_kv_write", dict(T=3), 1), ("fm_kv_write", dict(T=-1, offsets=P), 1), ("fm_kv_write", dict(offsets=P + 2), 1),
     ("fm_kv_write", dict(T=0, offsets=P, k=None, v=None), 0), ("fm_kv_write", dict(flags=P + 2), 1),
     ("fm_kv_write", dict(T=(1 << 24) + 1, offsets=P), 1),
-    ("fm_kv_read", dict(layer=2), 1), ("fm_kv_read", dict(k=None), 1), ("fm_kv_read", dict(T=3), 1),
+    ("fm_kv_read", dict(v=P), 1), ("fm_kv_read", dict(layer=2), 1), ("fm_kv_read", dict(k=None), 1), ("fm_kv_read", dict(T=3), 1),
     ("fm_attn_decode", dict(layer=2), 1), ("fm_attn_decode", dict(q=None), 1), ("fm_attn_decode", dict(q=P + 8), 1),
     ("fm_attn_decode", dict(q_stride=511), 1), ("fm_attn_decode", dict(q_stride=516), 1),
     ("fm_attn_decode", dict(q_heads=0), 1), ("fm_attn_decode", dict(q_heads=7), 1),
     ("fm_attn_decode", dict(q_heads=1026, q_stride=1 << 20), 1), ("fm_attn_decode", dict(window=-1), 1),
     ("fm_attn_decode", dict(scale=3e38), 1), ("fm_attn_decode", dict(scale=float("nan")), 1), ("fm_attn_decode", dict(scale=float("inf")), 1),
     ("fm_attn_decode", dict(first=P + 2), 1), ("fm_attn_decode", dict(lse=P + 2), 1), ("fm_attn_decode", dict(out=None), 1),
-    ("fm_attn_decode", dict(out=P + 8), 1), ("fm_attn_decode", dict(workspace=None), 1),
+    ("fm_attn_decode", dict(out=P + 8), 1), ("fm_attn_decode", dict(out=P), 1), ("fm_attn_decode", dict(workspace=None), 1),
     ("fm_attn_decode", dict(workspace=P + 16), 1), ("fm_attn_decode", dict(workspace_bytes=0), 1)])
 def test_calls_refused(fn, change, status):
     desc = L.KvCacheDesc(*CACHE.values())
@@ -81,9 +81,9 @@ def test_null_cache(fn):
     assert getattr(lib, fn)(None, *ON_CACHE[fn].values()) == L.FM_ERR_INVALID
 
 
-NORM = dict(x=P, y=P, post=P, gate=P, kind=1, scale=1.0, pre=P, eps=1e-6, T=4, d=64, dtype=1, r=P, h=P, stream=None)
+NORM = dict(x=P, y=P, post=P, gate=P, kind=1, scale=1.0, pre=P, eps=1e-6, T=4, d=64, dtype=1, r=P, h=2 * P, stream=None)
 GRAD = dict(dr=P, dh=P, x=P, y=P, post=P, gate=P, kind=1, scale=1.0, pre=P, eps=1e-6, T=4, d=64, dtype=1, accumulate=0,
-            dx=P, dy=P, dpost=P, dgate=P, dpre=P, scratch=P, scratch_bytes=1 << 24, stream=None)
+            dx=P, dy=2 * P, dpost=3 * P, dgate=4 * P, dpre=5 * P, scratch=P, scratch_bytes=1 << 24, stream=None)
 
 
 @pytest.mark.parametrize("change,status", [
@@ -99,7 +99,8 @@ def test_norms_refused(change, status):
 
 @pytest.mark.parametrize("fn,change,status", [
     ("fm_block_norm", dict(r=None), 1), ("fm_block_norm", dict(h=None), 1), ("fm_block_norm", dict(pre=None), 1),
-    ("fm_block_norm", dict(r=P + 8), 1), ("fm_block_norm", dict(h=P + 8), 1),
+    ("fm_block_norm", dict(h=P), 1), ("fm_block_norm_grad", dict(dy=P), 1), ("fm_block_norm_grad", dict(dpre=3 * P), 1),
+    ("fm_block_norm_grad", dict(kind=3, dgate=2 * P), 1), ("fm_block_norm", dict(r=P + 8), 1), ("fm_block_norm", dict(h=P + 8), 1),
     ("fm_block_norm", dict(y=None, post=None, gate=None, kind=0), 1),
     ("fm_block_norm", dict(y=None, post=None, gate=None, kind=0, r=None, pre=None, h=None), 1),
     ("fm_block_norm", dict(T=0, x=None, y=None, gate=None, r=None, h=None), 0),
@@ -187,6 +188,9 @@ def test_tensors_refused():
         (lambda: fm.attn_decode(cache, 0, torch.zeros(4, 7, 64, dtype=BF)), "not a multiple"),
         (lambda: fm.attn_decode(cache, 0, q, out=q), "out must not be q"),
         (lambda: fm.attn_decode(cache, 0, q, out=q[:, :4]), "out must have"),
+        (lambda: fm.attn_decode(cache, 0, q, window=2 ** 32 + 5), "window=4294967301 does not fit"),
+        (lambda: fm.attn_decode(cache, 2 ** 32, q), "layer=4294967296 does not fit"),
+        (lambda: fm.kv_write(cache, -2 ** 40, k, k), "layer=-1099511627776 does not fit"),
         (lambda: fm.attn_decode(cache, 0, q, first=on), "first must"),
         (lambda: fm.attn_decode(cache, 0, q, active=four), "active must"),
         (lambda: fm.attn_decode(cache, 0, q, lse=torch.zeros(4, 7)), "lse must"),
@@ -226,6 +230,8 @@ def test_norm_tensors_refused():
         (lambda: fm.block_norm_grad(x, None, x, x, post=w, out=(x, x, w, None, None)), "dpost"),
         (lambda: fm.block_norm_grad(x, None, x, x, out=(x, x, f, None, None)), "must be None: its input"),
         (lambda: fm.block_norm_grad(x, None, x, x, gate=x[:, :1].contiguous(), out=(x, x, None, f, None)), "dgate"),
+        (lambda: fm.block_norm(x, x, pre=w, out=(x, x)), "not the same"),
+        (lambda: fm.block_norm_grad(x, None, x, x, out=(x, x, None, None, None)), "not the same"),
         (lambda: fm.BlockNormScratch(4, 60, "cpu"), "invalid scratch"),
         (lambda: fm.block_norm(x, x, pre=w), "not on a GPU"),
         (lambda: fm.block_norm_grad(x, None, x, x), "not on a GPU")]
