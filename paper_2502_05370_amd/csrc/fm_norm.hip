@@ -134,7 +134,8 @@ __global__ void __launch_bounds__((W > 4 ? W : 4) * kWave) k_norm(NormArgs a) {
   __shared__ float buf[2][W][4];
   int turn = 0;
   const int part = static_cast<int>(threadIdx.x) % (W * kWave);
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / (W * kWave);
+  const int64_t t =
+      (static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x) * kRows + threadIdx.x / (W * kWave);
   if (t >= a.T) return;   // (whole wavefronts, and no barrier where W < 4)
   const int vecs = a.d / N;
   const int64_t row = t * vecs;
@@ -481,14 +482,19 @@ __global__ void __launch_bounds__(kSumWaves* kWave) k_norm_sum(NormGradArgs a, i
 
 // Wavefronts per row and vectors per thread for rows of `vecs` vectors: the fewest
 // wavefronts that hold the row with at most four vectors each.
+constexpr int64_t kGridRow = 1 << 16;
+
 template <typename T>
 hipError_t norm(const NormArgs& a, hipStream_t st) {
   const int vecs = a.d / Vec<T>::N;
   auto go = [&](auto w, auto v) {
     constexpr int W = decltype(w)::value, V = decltype(v)::value;
     constexpr int kRows = W > 4 ? 1 : 4 / W;
-    const int64_t grid = (static_cast<int64_t>(a.T) + kRows - 1) / kRows;
-    k_norm<T, W, V><<<static_cast<unsigned>(grid), (W > 4 ? W : 4) * kWave, 0, st>>>(a);
+    // (in two dimensions: one of them holds fewer than 2^32 threads)
+    const int64_t groups = (static_cast<int64_t>(a.T) + kRows - 1) / kRows;
+    const int64_t gx = groups < kGridRow ? groups : kGridRow;
+    const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>((groups + gx - 1) / gx));
+    k_norm<T, W, V><<<grid, (W > 4 ? W : 4) * kWave, 0, st>>>(a);
   };
   using std::integral_constant;
   if (vecs <= kWave) go(integral_constant<int, 1>{}, integral_constant<int, 1>{});

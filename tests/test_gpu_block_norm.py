@@ -42,6 +42,22 @@ SIZES = [(1, 8), (3, 64), (5, 512), (1, 520), (9, 1000), (2, 1024), (7, 1032), (
          (9, 1536), (1100, 1536), (5, 1544), (3, 2600), (3, 6144), (2, 6152), (2, 9768), (3, 12288), (2, 12296)]
 
 
+@pytest.mark.parametrize("T,d", [(4 * 65536 + 5, 8), (65536 + 3, 2056), (65536 + 2, 8200)])
+def test_more_workgroups_than_a_row_of_the_grid(T, d):
+    """Rows on either side of the border, against the same rows in a call of their own."""
+    fm = _fm()
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn(T, d, generator=g, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn(d, generator=g, device="cuda", dtype=torch.bfloat16)
+    y = x.flip(0)
+    r, h = fm.block_norm(x, y, post=w, pre=w)
+    for at in (0, 65530, T - 9):
+        rows = slice(at, at + 9)
+        for got, want in zip((r, h), fm.block_norm(x[rows], y[rows], post=w, pre=w)):
+            assert torch.equal(got[rows], want)
+    assert torch.isfinite(r).all() and torch.isfinite(h).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,d", SIZES)
 def test_norm_and_gradient(T, d, dtype):
