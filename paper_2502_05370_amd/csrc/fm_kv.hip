@@ -508,18 +508,18 @@ __global__ void __launch_bounds__(kRowWaves* kWave) k_kv_rows(KvArgs a, KvRows r
   const int lane = tid % kWave;
   const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
   uint32_t bad = 0;
-  int unit = static_cast<int>(blockIdx.x);
-  int total = 0;   // blocks of all slots, where this workgroup counts them all
+  int64_t unit = blockIdx.x;
+  int64_t total = 0;   // blocks of all slots, where this workgroup counts them all
   for (;;) {
-    int slot = unit, block = 0;
+    int slot = static_cast<int>(unit), block = 0;
     if (r.offsets != nullptr) {
-      int before = 0;
+      int64_t before = 0;
       if (tid == 0) where[0] = -1;
       for (int s0 = 0; s0 < a.n_slots; s0 += NT) {
         uint32_t range = 0;
         const int n = s0 + tid < a.n_slots ? span_of(a, r, s0 + tid, range).blocks() : 0;
         if (unit == 0 && blockIdx.y == 0) bad |= range;
-        int upto = n;
+        int upto = n;   // (of one turn: 256 slots of up to 2^20 blocks)
 #pragma unroll
         for (int m = 1; m < kWave; m <<= 1) {
           const int o = __shfl_up(upto, m, kWave);
@@ -528,7 +528,7 @@ __global__ void __launch_bounds__(kRowWaves* kWave) k_kv_rows(KvArgs a, KvRows r
         __syncthreads();
         if (lane == kWave - 1) sums[wv] = upto;
         __syncthreads();
-        int at = before + upto - n;
+        int64_t at = before + upto - n;
 #pragma unroll
         for (int w = 0; w < kRowWaves; ++w) {
           at += w < wv ? sums[w] : 0;
@@ -536,7 +536,7 @@ __global__ void __launch_bounds__(kRowWaves* kWave) k_kv_rows(KvArgs a, KvRows r
         }
         if (unit >= at && unit < at + n) {
           where[0] = s0 + tid;
-          where[1] = unit - at;
+          where[1] = static_cast<int32_t>(unit - at);
         }
         if (before > unit && unit != 0) break;
       }
@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(kRowWaves* kWave) k_kv_rows(KvArgs a, KvRows r
     // The grid has a workgroup for every block of ascending offsets.  Spans that
     // overlap have more: the first workgroup, which has counted them, takes those.
     if (blockIdx.x != 0) break;
-    unit = unit == 0 ? static_cast<int>(gridDim.x) : unit + 1;
+    unit = unit == 0 ? gridDim.x : unit + 1;
     if (unit >= total) break;
   }
   if (bad != 0) set_flags(r.flags, bad);

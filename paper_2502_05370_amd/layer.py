@@ -352,8 +352,6 @@ def block_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None, post: Optional
         h = _new(shape, dtype, dev, stream)
     elif not _usual(h, dtype, shape, dev):
         _need(h, "out[1] (h)", dtype, shape, dev)
-    if out is not None and r is not None and h is not None and r.data_ptr() == h.data_ptr() != 0:
-        raise ValueError("out must be two tensors, not the same twice")
     _call("fm_block_norm", dev, stream, x.data_ptr(), _ptr(y), _ptr(post), _ptr(gate), kind, scale, _ptr(pre), eps,
           shape[0], shape[1], _CODE[dtype], _ptr(r), _ptr(h))
     return (x if r is None else r), h
@@ -413,9 +411,6 @@ def block_norm_grad(dr: Optional[torch.Tensor], dh: Optional[torch.Tensor], x: t
                     raise ValueError(f"out[{i}] ({_GRADS[i]}) must be None: its input is")
             elif not _usual(t, w[1], w[0], dev):
                 _need(t, f"out[{i}] ({_GRADS[i]})", w[1], w[0], dev)
-        places = [t.data_ptr() for t in out if t is not None and t.numel() != 0]
-        if len(set(places)) != len(places):
-            raise ValueError("out must be different tensors, not the same twice")
     if scratch is None:
         with _on(stream):
             scratch = BlockNormScratch(T, d, dev)
