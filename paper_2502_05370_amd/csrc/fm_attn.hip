@@ -387,20 +387,25 @@ __device__ __forceinline__ void store_part(const Joined<DIMS>& sh, int queries, 
 }
 
 // n parts of a tile (part(i) their offsets) into `sh`, a wavefront every fourth of
-// them: 32 parts at a time, whose values are on their way while their maxima and
+// them: 4 U parts at a time, whose values are on their way while their maxima and
 // sums decide how much each counts.
-constexpr int kTurn = 32;   // parts
+constexpr int kTurn = 32;   // parts at most
+// Parts up to which more of each are on their way instead: 291 tokens, 16 queries on 2
+// heads of 256 bf16 18.1 us in turns of 32 parts, 14.8 in turns of 8; 7 slots of 177, 48
+// on 2, 25.1 and 19.2.  (A third form for 16 parts: 28.5 us -> 25.0 at 2,000 tokens on
+// one head of 256 float32, but its code costs every call of 128 bf16 0.1-4 us.)
+constexpr int kFewParts = 8;
 struct Weights {
   float top[4 * kAttnWaves][16];   // by group of threads and query
   float scale[16];         // of what is there already
   float f[kTurn][16];
 };
-template <int DIMS, typename Part>
+template <int U, int DIMS, typename Part>
 __device__ __forceinline__ void collect(Joined<DIMS>& sh, Weights& wt, int queries, int n, __amdgpu_buffer_rsrc_t rs,
                                         Part part) {
-  constexpr int U = kTurn / kAttnWaves;           // parts of a wavefront
-  constexpr int G = 4 * kAttnWaves, J = kTurn / G;   // groups of 16 threads, and parts whose weights each computes
-  constexpr int E = 2;                    // fours of values of a lane in flight, per part
+  constexpr int kTurn = U * kAttnWaves;
+  constexpr int G = 4 * kAttnWaves, J = (kTurn + G - 1) / G;   // groups of 16 threads, and parts whose weights each computes
+  constexpr int E = 16 / U;               // fours of values of a lane in flight, per part
   const int tid = threadIdx.x;
   const int lane = tid % kWave;
   const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -412,7 +417,7 @@ __device__ __forceinline__ void collect(Joined<DIMS>& sh, Weights& wt, int queri
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int p = p0 + pg + G * j;
-      const bool in = p < n && pq < queries;
+      const bool in = pg + G * j < kTurn && p < n && pq < queries;
       const uint32_t at = in ? part(p) + 4u * pq : kOutside;
       m[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, static_cast<int>(at), 0, kAgent));
       s[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, static_cast<int>(in ? at + 64u : at), 0, kAgent));
@@ -439,7 +444,7 @@ __device__ __forceinline__ void collect(Joined<DIMS>& sh, Weights& wt, int queri
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           const float f = share(m[j], s[j], now);
-          wt.f[pg + G * j][pq] = f;
+          if (pg + G * j < kTurn) wt.f[pg + G * j][pq] = f;
           l += f * s[j];
         }
         if (pg == 0) wt.scale[pq] = top == now ? 1.0f : share(top, 1.0f, now);
@@ -717,9 +722,10 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP, ALONE>::kTwo 
           __syncthreads();
           ends = is_last != 0;
           if (ends) {
-            collect(sh, weights, queries, w1 - w0 + 1, rs, [&](int p) __attribute__((always_inline)) {
-              return part_at(w0 + p, p == 0);
-            });
+            const int n = w1 - w0 + 1;
+            auto part = [&](int p) __attribute__((always_inline)) { return part_at(w0 + p, p == 0); };
+            if (n <= kFewParts) collect<kFewParts / kAttnWaves>(sh, weights, queries, n, rs, part);
+            else collect<kTurn / kAttnWaves>(sh, weights, queries, n, rs, part);
             if (tid == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
           }
         }
