@@ -85,10 +85,12 @@ def test_random_calls(slots, W, pages, page):
     assert refusals > 0 or pages >= 400   # (the two largest pools may suffice)
 
 
-def test_forks_of_any_shape():
-    """One parent of many, chains, cycles, itself, parents out of range, empty parents."""
+@pytest.mark.parametrize("max_tokens", [160, 2048, 4096, 4112, 6000])
+def test_forks_of_any_shape(max_tokens):
+    """One parent of many, chains, cycles, itself, parents out of range, empty parents; tables that a workgroup holds
+    and larger ones."""
     fm = _fm()
-    cache, want = pair(8, 160, 60)
+    cache, want = pair(8, max_tokens, 60)
     delta = [5, 16, 33, 100, 0, 1, 48, 47]
     fm.kv_resize(cache, i32(delta)), want.resize(delta)
     for parent in ([1, 2, 3, 0, -1, -1, -1, -1], [3] * 8, [0, 1, 2, 3, 4, 5, 6, 7], [4, 4, -1, -1, -1, 0, 1, 5],
