@@ -212,16 +212,20 @@ __global__ void __launch_bounds__((W > 4 ? W : 4) * kWave) k_norm(NormArgs a) {
 // S = sum of e y^ over the rows is both gradients of vectors: dpost = gate S, dgate =
 // post S (of other gates than a channel's: dpost = sum of e gate y^).  A row's values
 // stay as they were loaded (bf16 in pairs), so that there is room to send for the next
-// row's before this one's three sums are waited for.  Rows of 16 wavefronts leave the
-// vectors in the caches and the next row where it is.
+// row's before this one's three sums are waited for.  Rows of 16 wavefronts, whose
+// threads have 128 registers, leave the vectors in the caches and the next row where it
+// is, and keep their sums in LDS: 2,048 rows of 16,384 bf16 127 us, 141 with the sums in
+// registers (and with the next row sent for as well); 700 of float32 99 and 133.
 template <typename T, int W, int V, int R, int GATE>
 __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
   using X = Vec<T>;
   constexpr int N = X::N;
   constexpr bool kAhead = W <= 8;
+  constexpr bool kWide = W == 16;
   constexpr bool kEach = GATE == FM_GATE_EACH, kChannel = GATE == FM_GATE_CHANNEL, kToken = GATE == FM_GATE_TOKEN;
   __shared__ float buf[R][2][W][4];
   __shared__ float joined[R > 1 ? W * kWave * V * N : 1];
+  __shared__ floatx4 wide_sums[kWide ? 2 * V * N / 4 : 1][kWide ? W * kWave : 1];
   int turn = 0;
   const NormArgs& f = a.f;
   const int slot = static_cast<int>(threadIdx.x) / (W * kWave);
@@ -246,11 +250,31 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
     return u;
   };
   uint32x4 pre_[V];
-  X u_[V], sum_y[V], sum_r[V];
+  X u_[V], sum_y[kWide ? 1 : V], sum_r[kWide ? 1 : V];
+  // (a lane's own places in LDS, where registers are short)
+  auto sum_at = [&](int which, int v, int q) __attribute__((always_inline)) -> floatx4& {
+    return wide_sums[kWide ? (which * V + v) * (N / 4) + q : 0][kWide ? threadIdx.x : 0];
+  };
+  auto add_sum = [&](int which, int v, const X& x) __attribute__((always_inline)) {
+    if constexpr (kWide) {
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q)
+        sum_at(which, v, q) += floatx4{x.f[4 * q], x.f[4 * q + 1], x.f[4 * q + 2], x.f[4 * q + 3]};
+    } else {
+      X& to = which == 0 ? sum_y[v] : sum_r[v];
+#pragma unroll
+      for (int j = 0; j < N; ++j) to.f[j] += x.f[j];
+    }
+  };
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    sum_y[v].zero();
-    sum_r[v].zero();
+    if constexpr (kWide) {
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q) sum_at(0, v, q) = sum_at(1, v, q) = floatx4{0.f, 0.f, 0.f, 0.f};
+    } else {
+      sum_y[v].zero();
+      sum_r[v].zero();
+    }
     if constexpr (kAhead) {
       pre_[v] = take(f.pre, part + v * W * kWave, in(v) && has_pre);
       u_[v] = product(v);
@@ -353,18 +377,20 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
       if (has_pre && on) {
         const X dh = wide<T>(now.dh[v]);
         const X w = pre(v);
+        X part_r;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           const float hat = r[v].f[j] * inv_r;
-          sum_r[v].f[j] += dh.f[j] * hat;
+          part_r.f[j] = dh.f[j] * hat;
           d.f[j] += inv_r * (dh.f[j] * w.f[j] - hat * mean);
         }
+        add_sum(1, v, part_r);
       }
       if (on) d.store(a.dx, row + v * W * kWave);
       if (!has_y || !on) continue;
       const X y = wide<T>(now.y[v]);
       const X u = factor(v);
-      X one;
+      X one, part_y;
       if constexpr (kEach) {   // the gate's own gradient is without the gate
         one = kAhead ? u_[v] : product(v);
         const X g = wide<T>(now.gate[v]);
@@ -373,7 +399,7 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
           const float hat = y.f[j] * inv_y;
           const float e = f.scale * d.f[j];
           one.f[j] *= e * hat;
-          sum_y[v].f[j] += e * g.f[j] * hat;
+          part_y.f[j] = e * g.f[j] * hat;
           s2[0] += e * (u.f[j] * hat);
           r[v].f[j] = e;
         }
@@ -383,11 +409,12 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
         for (int j = 0; j < N; ++j) {
           const float hat = y.f[j] * inv_y;
           const float e = f.scale * d.f[j];
-          sum_y[v].f[j] += (kToken ? e * now.token : e) * hat;
+          part_y.f[j] = (kToken ? e * now.token : e) * hat;
           s2[0] += e * (u.f[j] * hat);
           r[v].f[j] = e;
         }
       }
+      add_sum(0, v, part_y);
     }
     if (has_y) {
       if (has_post || kToken) row_sums<W, 1>(s2, buf[slot], turn);
@@ -410,7 +437,7 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
   }
   // the rows' sums in order, through LDS; then this workgroup's: [gridDim.x][2][d]
   float* out = a.partial + static_cast<int64_t>(blockIdx.x) * 2 * f.d;
-  auto put = [&](int which, X (&s)[V]) __attribute__((always_inline)) {
+  auto put = [&](int which, X (&s)[kWide ? 1 : V]) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 1; k < R; ++k) {
       __syncthreads();
@@ -419,14 +446,14 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           float* at = joined + (v * N + j) * (W * kWave) + part;
-          if (slot == k) *at = s[v].f[j];
+          if (slot == k) *at = s[kWide ? 0 : v].f[j];
         }
       __syncthreads();
 #pragma unroll
       for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int j = 0; j < N; ++j)
-          if (slot == 0) s[v].f[j] += joined[(v * N + j) * (W * kWave) + part];
+          if (slot == 0) s[kWide ? 0 : v].f[j] += joined[(v * N + j) * (W * kWave) + part];
     }
     if (slot != 0) return;
 #pragma unroll
@@ -434,8 +461,11 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
       if (!in(v)) continue;
       float* to = out + static_cast<int64_t>(which) * f.d + static_cast<int64_t>(part + v * W * kWave) * N;
 #pragma unroll
-      for (int j = 0; j < N; j += 4)
-        *reinterpret_cast<floatx4*>(to + j) = floatx4{s[v].f[j], s[v].f[j + 1], s[v].f[j + 2], s[v].f[j + 3]};
+      for (int j = 0; j < N; j += 4) {
+        const X& x = s[kWide ? 0 : v];
+        *reinterpret_cast<floatx4*>(to + j) =
+            kWide ? sum_at(which, v, j / 4) : floatx4{x.f[j], x.f[j + 1], x.f[j + 2], x.f[j + 3]};
+      }
     }
   };
   if (a.dpost != nullptr || kChannel) put(0, sum_y);
@@ -531,8 +561,8 @@ hipError_t norm_grad(const NormGradArgs& a, hipStream_t st) {
   // eight.  In bf16, with one and with two: 64 rows of 1,024 7.1 us and 10.2, of 4,096
   // 8.5 and 9.6, 8,192 rows of 4,096 81 and 84; but of 2,304 62 and 53, of 8,192 198
   // and 157.  67 MB in rows of 1,280 take 93 us on 4 wavefronts and 113 on 4 of two
-  // vectors each.  float32 rows of more than 8,192 values need three or four vectors,
-  // and four spill registers: 700 rows of 12,288 take 74 us with three and 102 with four.
+  // vectors each.  float32 rows of more than 8,192 values need three or four vectors:
+  // 700 rows of 12,288 take 65 us with three and 79 with four.
   if (vecs <= kWave) go(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, 8>{});
   else if (vecs <= 2 * kWave) go(integral_constant<int, 2>{}, integral_constant<int, 1>{}, integral_constant<int, 4>{});
   else if (vecs <= 4 * kWave) go(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
