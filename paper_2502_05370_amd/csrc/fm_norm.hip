@@ -212,16 +212,17 @@ __global__ void __launch_bounds__((W > 4 ? W : 4) * kWave) k_norm(NormArgs a) {
 // S = sum of e y^ over the rows is both gradients of vectors: dpost = gate S, dgate =
 // post S (of other gates than a channel's: dpost = sum of e gate y^).  A row's values
 // stay as they were loaded (bf16 in pairs), so that there is room to send for the next
-// row's before this one's three sums are waited for.  Rows of 16 wavefronts, whose
-// threads have 128 registers, leave the vectors in the caches and the next row where it
-// is, and keep their sums in LDS: 2,048 rows of 16,384 bf16 127 us, 141 with the sums in
-// registers (and with the next row sent for as well); 700 of float32 99 and 133.
+// row's before this one's three sums are waited for.  The sums of wide rows are in LDS:
+// 1,024 rows of 12,288 bf16 46 us, 64 with the sums in registers and the next row where
+// it is.  Rows of 16 wavefronts, whose threads have 128 registers, leave the vectors in
+// the caches too, and the next row: 700 rows of 16,384 float32 99 us, 162 with it sent
+// for, 133 with the sums in registers.
 template <typename T, int W, int V, int R, int GATE>
 __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
   using X = Vec<T>;
   constexpr int N = X::N;
-  constexpr bool kAhead = W <= 8;
-  constexpr bool kWide = W == 16;
+  constexpr bool kAhead = W <= 12;
+  constexpr bool kWide = W >= 12 || (sizeof(T) == 2 && V == 4);
   constexpr bool kEach = GATE == FM_GATE_EACH, kChannel = GATE == FM_GATE_CHANNEL, kToken = GATE == FM_GATE_TOKEN;
   __shared__ float buf[R][2][W][4];
   __shared__ float joined[R > 1 ? W * kWave * V * N : 1];
@@ -539,10 +540,14 @@ hipError_t norm(const NormArgs& a, hipStream_t st) {
 
 template <typename T>
 hipError_t norm_grad(const NormGradArgs& a, hipStream_t st) {
+  constexpr bool kBf = sizeof(T) == 2;
   const int vecs = a.f.d / Vec<T>::N;
   int lists = 0;
   auto run = [&](auto w, auto v, auto r, auto gate) {
-    constexpr int W = decltype(w)::value, V = decltype(v)::value, R = decltype(r)::value, G = decltype(gate)::value;
+    constexpr int R = decltype(r)::value, G = decltype(gate)::value;
+    // (four vectors of a fifth array spill: 64 rows of 16,384 bf16 20.2 us for 17.6)
+    constexpr bool kFifth = kBf && decltype(v)::value == 4 && G == FM_GATE_EACH;
+    constexpr int W = kFifth ? 16 : decltype(w)::value, V = kFifth ? 2 : decltype(v)::value;
     const int64_t want = (static_cast<int64_t>(a.f.T) + R - 1) / R;
     lists = static_cast<int>(want < kNormLists ? want : kNormLists);
     if (lists > 0) k_norm_grad<T, W, V, R, G><<<static_cast<unsigned>(lists), W * R * kWave, 0, st>>>(a);
@@ -561,8 +566,11 @@ hipError_t norm_grad(const NormGradArgs& a, hipStream_t st) {
   // eight.  In bf16, with one and with two: 64 rows of 1,024 7.1 us and 10.2, of 4,096
   // 8.5 and 9.6, 8,192 rows of 4,096 81 and 84; but of 2,304 62 and 53, of 8,192 198
   // and 157.  67 MB in rows of 1,280 take 93 us on 4 wavefronts and 113 on 4 of two
-  // vectors each.  float32 rows of more than 8,192 values need three or four vectors:
-  // 700 rows of 12,288 take 65 us with three and 79 with four.
+  // vectors each.  Wider rows: no more than 12 wavefronts,
+  // whose threads have registers for the next row, take four vectors of float32 up to
+  // 8,192 values (2,048 rows: 89 us, 109 on 16 wavefronts of two) and, with the sums in
+  // LDS, of bf16 beyond 12,288 (16,384: 102 and 127).  float32 rows of more than 8,192
+  // need 16: 700 rows of 12,288 take 65 us with three vectors and 79 with four.
   if (vecs <= kWave) go(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, 8>{});
   else if (vecs <= 2 * kWave) go(integral_constant<int, 2>{}, integral_constant<int, 1>{}, integral_constant<int, 4>{});
   else if (vecs <= 4 * kWave) go(integral_constant<int, 4>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{});
@@ -570,9 +578,10 @@ hipError_t norm_grad(const NormGradArgs& a, hipStream_t st) {
   else if (vecs <= 8 * kWave) go(integral_constant<int, 8>{}, integral_constant<int, 1>{}, integral_constant<int, 1>{});
   else if (vecs <= 12 * kWave) go(integral_constant<int, 6>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
   else if (vecs <= 16 * kWave) go(integral_constant<int, 8>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
-  else if (sizeof(T) == 2 || vecs <= 32 * kWave) go(integral_constant<int, 16>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
-  else if (vecs <= 48 * kWave) go(integral_constant<int, 16>{}, integral_constant<int, sizeof(T) == 2 ? 2 : 3>{}, integral_constant<int, 1>{});
-  else go(integral_constant<int, 16>{}, integral_constant<int, sizeof(T) == 2 ? 2 : 4>{}, integral_constant<int, 1>{});
+  else if (kBf && vecs <= 24 * kWave) go(integral_constant<int, kBf ? 12 : 8>{}, integral_constant<int, 2>{}, integral_constant<int, 1>{});
+  else if (kBf || vecs <= 32 * kWave) go(integral_constant<int, 8>{}, integral_constant<int, 4>{}, integral_constant<int, 1>{});
+  else if (vecs <= 48 * kWave) go(integral_constant<int, kBf ? 8 : 16>{}, integral_constant<int, kBf ? 4 : 3>{}, integral_constant<int, 1>{});
+  else go(integral_constant<int, kBf ? 8 : 16>{}, integral_constant<int, 4>{}, integral_constant<int, 1>{});
   if (a.dpost != nullptr || a.dpre != nullptr || a.f.gate_kind == FM_GATE_CHANNEL)
     k_norm_sum<T><<<dim3(static_cast<unsigned>((a.f.d + kWave - 1) / kWave), 2), kSumWaves * kWave, 0, st>>>(a, lists);
   return hipGetLastError();

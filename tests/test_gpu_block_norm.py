@@ -39,7 +39,8 @@ def inputs(rng, T, d, kind, post, pre, dtype):
 
 SIZES = [(1, 8), (3, 64), (5, 512), (1, 520), (9, 1000), (2, 1024), (7, 1032), (4, 2048), (2, 2056), (3, 4096), (2, 4104),
          (1, 8192), (3, 8200), (2, 16384), (600, 136), (1100, 1032), (2100, 64),
-         (9, 1536), (1100, 1536), (5, 1544), (3, 2600), (3, 6144), (2, 6152), (2, 9768), (3, 12288), (2, 12296)]
+         (9, 1536), (1100, 1536), (5, 1544), (3, 2600), (3, 6144), (2, 6152), (2, 9768), (3, 12288), (2, 12296),
+         (3, 12296), (300, 4104), (300, 9768), (300, 12296)]
 
 
 @pytest.mark.parametrize("T,d", [(4 * 65536 + 5, 8), (65536 + 3, 2056), (65536 + 2, 8200)])
