@@ -10,7 +10,7 @@
 // TB/s; a copy reaches 5.1).  Eight slots forked in four, each grown past a shared page:
 // 2.3 us of new tables, 1.7 to put them in place, 7.0 to decide, 15 to copy 32 pages (100
 // MB, 6.6 TB/s: the memory-side cache holds some).  Rows of 8,192 tokens on 8 heads of 128
-// bf16: 67 MB in 18 us (3.6 TB/s; 25 with rows that no cache holds); of 8 tokens 3.4 us.
+// bf16: 67 MB in 18 us (3.7 TB/s); of 8 tokens 3.4 us.
 #include "fm_device.h"
 #include "fm_kv.h"
 
@@ -515,11 +515,19 @@ struct Piece {
         if (quad[j] && column(a, piece, i)) v[4 * i + j] = vrow[j * r.v_stride + 16 * i];
       }
   }
+  // MANY: past the caches, which many rows would turn over: pages of 8,192 tokens that no
+  // cache holds 18.1 us, 29.5 through them; one token of each of 256 slots, 32 heads of
+  // 128 bf16, 14.7 and 16.4.  A few tokens stay there for the attention that follows.
+  template <bool MANY>
   __device__ __forceinline__ void to_page(char* kp, char* vp) const {
+    auto store = [](uint32x4 x, uint32x4* p) __attribute__((always_inline)) {
+      if constexpr (MANY) __builtin_nontemporal_store(x, p);
+      else *p = x;
+    };
     const int lane = threadIdx.x % kWave;
-    if (has) reinterpret_cast<uint32x4*>(kp)[lane] = k;
+    if (has) store(k, reinterpret_cast<uint32x4*>(kp) + lane);
     if (quad[0] && quad[3]) {
-      reinterpret_cast<uint32x4*>(vp)[lane] = *reinterpret_cast<const uint32x4*>(v);
+      store(*reinterpret_cast<const uint32x4*>(v), reinterpret_cast<uint32x4*>(vp) + lane);
     } else {
 #pragma unroll
       for (int e = 0; e < N; ++e)
@@ -544,7 +552,7 @@ struct Piece {
 // A workgroup takes blocks of 16 tokens; blocks are counted through the slots
 // (each workgroup sums the slots' counts until it finds its own), the pieces of all
 // heads are dealt to the wavefronts and to grid.y.
-template <typename T, bool READ>
+template <typename T, bool READ, bool MANY>
 __global__ void __launch_bounds__(kRowWaves* kWave) k_kv_rows(KvArgs a, KvRows r) {
   constexpr int NT = kRowWaves * kWave;
   __shared__ int32_t sums[kRowWaves];
@@ -615,7 +623,7 @@ __global__ void __launch_bounds__(kRowWaves* kWave) k_kv_rows(KvArgs a, KvRows r
             p.to_rows(a, r, piece);
           } else {
             p.from_rows(a, r, piece);   // (on their way while the table's entry is)
-            if (valid && !shared) p.to_page(kp, vp);
+            if (valid && !shared) p.template to_page<MANY>(kp, vp);
           }
         }
       }
@@ -686,15 +694,17 @@ hipError_t launch_kv_rows(const fm_kv_cache& c, const KvRows& r, bool read, hipS
   // workgroups look for their block (us of 1 and 4: 8 tokens of 8 heads of 128 4.1 and
   // 5.8, 8,192 tokens 22.6 and 19.4).
   const int64_t pieces = static_cast<int64_t>(c.heads) * a.pieces;
-  const int64_t per_group = kRowWaves * (most * pieces >= 16384 ? 4 : 1);
+  const bool many = most * pieces >= 16384;
+  const int64_t per_group = kRowWaves * (many ? 4 : 1);
   const dim3 grid(static_cast<unsigned>(most), static_cast<unsigned>((pieces + per_group - 1) / per_group));
-  if (c.dtype == FM_BF16) {
-    if (read) k_kv_rows<uint16_t, true><<<grid, kRowWaves * kWave, 0, st>>>(a, r);
-    else k_kv_rows<uint16_t, false><<<grid, kRowWaves * kWave, 0, st>>>(a, r);
-  } else {
-    if (read) k_kv_rows<uint32_t, true><<<grid, kRowWaves * kWave, 0, st>>>(a, r);
-    else k_kv_rows<uint32_t, false><<<grid, kRowWaves * kWave, 0, st>>>(a, r);
-  }
+  auto go = [&](auto t) {
+    using T = decltype(t);
+    if (read) k_kv_rows<T, true, false><<<grid, kRowWaves * kWave, 0, st>>>(a, r);
+    else if (many) k_kv_rows<T, false, true><<<grid, kRowWaves * kWave, 0, st>>>(a, r);
+    else k_kv_rows<T, false, false><<<grid, kRowWaves * kWave, 0, st>>>(a, r);
+  };
+  if (c.dtype == FM_BF16) go(uint16_t{});
+  else go(uint32_t{});
   return hipGetLastError();
 }
 
