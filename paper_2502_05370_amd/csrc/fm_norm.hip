@@ -420,6 +420,10 @@ __global__ void __launch_bounds__(W* R* kWave) k_norm_grad(NormGradArgs a) {
     if (has_y) {
       if (has_post || kToken) row_sums<W, 1>(s2, buf[slot], turn);
       if (kToken && part == 0 && live) static_cast<float*>(a.dgate)[t] = s2[0];
+      if (!has_post) {   // y has no part in dy, also where it is infinite or NaN
+#pragma unroll
+        for (int v = 0; v < V; ++v) now.y[v] = uint32x4{0u, 0u, 0u, 0u};
+      }
       forget(now.y);
       const float mean_y = has_post ? s2[0] * inv_d * inv_y : 0.0f;
       const float back = kToken ? inv_y * now.token : inv_y;
