@@ -596,9 +596,12 @@ size_t fm_attn_workspace_bytes(const fm_kv_cache* cache, int32_t q_heads);
  * of p_j, for joining with attention over other tokens.  A query that sees no
  * token, or only tokens whose score is minus infinity, gives zeros and -inf;
  * tokens outside the range have no part in the result, whatever their pages
- * hold; other infinities and NaN follow the formula.  bf16 caches: p_j meets
- * v_j as two bf16 (2^-15 relative).  Calls sharing a workspace must be
- * ordered. */
+ * hold; other infinities and NaN follow the formula, but that a score of plus
+ * infinity gives a lse_out of NaN.  bf16 caches: p_j meets v_j as two bf16
+ * (2^-15 relative, or 2^-133 where that is more).  p_j and their sums with v_j
+ * are float32, relative to the largest score that a part of the tokens has: below
+ * 2^-126 p_j is zero, and values of which a sum passes 3.4e38 give infinities or
+ * NaN.  Calls sharing a workspace must be ordered. */
 fm_status fm_attn_decode(const fm_kv_cache* cache, int32_t layer, const void* q, int64_t q_stride, int32_t q_heads,
                          float scale, int32_t window, const int32_t* first, const uint8_t* active, void* out,
                          float* lse_out, uint32_t* flags, void* workspace, size_t workspace_bytes, void* stream);

@@ -51,8 +51,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{a, b}, bf16x2));
 }
 
-// What p cut to `cut` leaves (NaN stays NaN in the cut part).
-__device__ __forceinline__ float rest(float p, uint32_t cut) { return fmaxf(p - __uint_as_float(cut), 0x1p-126f); }
+// What p cut to `cut` leaves: at least the least bf16 above zero, or nothing where p is
+// zero (NaN stays NaN in the cut part).  The median, since 0 <= p - cut <= p.
+__device__ __forceinline__ float rest(float p, uint32_t cut) {
+  return __builtin_amdgcn_fmed3f(p - __uint_as_float(cut), p, 0x1p-133f);
+}
 
 // The tokens that a slot's query sees.
 struct Seen {
@@ -163,8 +166,9 @@ struct Wave {
   __device__ __forceinline__ void add(const floatx4 (&p)[SB]) {
     if constexpr (kBf) {
       // p as two bf16, so that the result is off by its own rounding alone: p cut
-      // towards zero, and the rest.  2^-126 stands for a rest of zero, so that an
-      // infinite value gives infinity and not the NaN of infinity times zero.
+      // towards zero, and the rest.  2^-133 stands for a rest of zero, so that an
+      // infinite value gives infinity and not the NaN of infinity times zero; a weight of
+      // zero is zero in both parts.
       uint32x4 hi, lo;
 #pragma unroll
       for (int b = 0; b < SB; b += 2) {
