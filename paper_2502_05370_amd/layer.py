@@ -18,8 +18,16 @@ from .model import _CODE, _call, _flags, _float_rows, _new, _on
 _GRADS = "dx", "dy", "dpost", "dgate", "dpre"
 
 
+def _int32(n: int, name: str) -> int:
+    """n, which ctypes would cut to 32 bits."""
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name}={n} does not fit 32 bits")
+    return n
+
+
 def kv_page_bytes(layers: int, heads: int, head_dim: int, page: int = 64, dtype: str = "bf16") -> int:
-    return int(_lib.load().fm_kv_page_bytes(layers, heads, head_dim, page, _DTYPES[dtype]))
+    return int(_lib.load().fm_kv_page_bytes(_int32(layers, "layers"), _int32(heads, "heads"),
+                                            _int32(head_dim, "head_dim"), _int32(page, "page"), _DTYPES[dtype]))
 
 
 class KvCache:
@@ -32,13 +40,13 @@ class KvCache:
 
     def __init__(self, slots: int, max_tokens: int, pages: int, layers: int, heads: int, head_dim: int,
                  dtype: str = "bf16", page: int = 64, device="cuda"):
-        self.slots, self.n_pages, self.page = int(slots), int(pages), int(page)
+        self.slots, self.n_pages, self.page = _int32(int(slots), "slots"), _int32(int(pages), "pages"), int(page)
         self.layers, self.heads, self.head_dim = int(layers), int(heads), int(head_dim)
         self.dtype = _TORCH[_DTYPES[dtype]]
         self.page_bytes = kv_page_bytes(self.layers, self.heads, self.head_dim, self.page, dtype)
         if self.page_bytes == 0:
             raise ValueError(f"invalid cache page={page} layers={layers} heads={heads} head_dim={head_dim}")
-        self.max_pages = (int(max_tokens) + self.page - 1) // self.page
+        self.max_pages = _int32((int(max_tokens) + self.page - 1) // self.page, "max_pages")
         self._desc = _lib.KvCacheDesc(self.slots, self.max_pages, self.n_pages, self.page, self.layers, self.heads,
                                       self.head_dim, _DTYPES[dtype], None, None, None, None)
         self.desc = C.byref(self._desc)
@@ -130,7 +138,7 @@ class KvCache:
 
 
 def attn_workspace_bytes(cache: KvCache, q_heads: int) -> int:
-    return int(_lib.load().fm_attn_workspace_bytes(cache.desc, q_heads))
+    return int(_lib.load().fm_attn_workspace_bytes(cache.desc, _int32(q_heads, "q_heads")))
 
 
 class AttnWorkspace:
@@ -189,7 +197,7 @@ def kv_copy(cache: KvCache, src: torch.Tensor, dst: torch.Tensor, stream=None) -
     named twice, or that name no page, are left out and flagged."""
     _need(src, "src", torch.int32, (None,), cache.device)
     _need(dst, "dst", torch.int32, (src.shape[0],), cache.device)
-    _change("fm_kv_copy", cache, stream, src.data_ptr(), dst.data_ptr(), src.shape[0])
+    _change("fm_kv_copy", cache, stream, src.data_ptr(), dst.data_ptr(), _int32(src.shape[0], "n"))
 
 
 def _rows(t, name: str, dtype, T: Optional[int], heads: Optional[int], head_dim: int, device) -> Tuple[int, int, int, int]:
@@ -210,13 +218,6 @@ def _rows(t, name: str, dtype, T: Optional[int], heads: Optional[int], head_dim:
     return t.data_ptr(), row if T > 1 else H * D, T, H
 
 
-def _int32(n: int, name: str) -> int:
-    """n, which ctypes would cut to 32 bits."""
-    if not -2 ** 31 <= n < 2 ** 31:
-        raise ValueError(f"{name}={n} does not fit 32 bits")
-    return n
-
-
 def _token_rows(name: str, cache: KvCache, layer: int, k, v, offsets, active, stream) -> None:
     dev = cache.device
     slots = cache.slots if offsets is None else None
@@ -228,8 +229,8 @@ def _token_rows(name: str, cache: KvCache, layer: int, k, v, offsets, active, st
         _need(offsets, "offsets", torch.int32, (cache.slots + 1,), dev)
     if active is not None:
         _need(active, "active", torch.uint8, (cache.slots,), dev)
-    _call(name, dev, stream, cache.desc, _int32(layer, "layer"), k_ptr, k_stride, v_ptr, v_stride, _ptr(offsets), T, _ptr(active),
-          _flags(cache.flags, dev))
+    _call(name, dev, stream, cache.desc, _int32(layer, "layer"), k_ptr, k_stride, v_ptr, v_stride, _ptr(offsets),
+          _int32(T, "T"), _ptr(active), _flags(cache.flags, dev))
 
 
 def kv_write(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, offsets: Optional[torch.Tensor] = None,
@@ -291,9 +292,9 @@ def attn_decode(cache: KvCache, layer: int, q: torch.Tensor, scale: Optional[flo
     if workspace.in_capture:
         with _on(stream):
             workspace.clear()
-    _call("fm_attn_decode", dev, stream, cache.desc, _int32(layer, "layer"), q_ptr, q_stride, q_heads,
-          cache.head_dim ** -0.5 if scale is None else scale, _int32(window, "window"), _ptr(first), _ptr(active), out.data_ptr(),
-          _ptr(lse), _flags(cache.flags, dev), workspace.buf.data_ptr(), workspace.nbytes)
+    _call("fm_attn_decode", dev, stream, cache.desc, _int32(layer, "layer"), q_ptr, q_stride,
+          _int32(q_heads, "q_heads"), cache.head_dim ** -0.5 if scale is None else scale, _int32(window, "window"),
+          _ptr(first), _ptr(active), out.data_ptr(), _ptr(lse), _flags(cache.flags, dev), workspace.buf.data_ptr(), workspace.nbytes)
     return out
 
 
@@ -353,12 +354,12 @@ def block_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None, post: Optional
     elif not _usual(h, dtype, shape, dev):
         _need(h, "out[1] (h)", dtype, shape, dev)
     _call("fm_block_norm", dev, stream, x.data_ptr(), _ptr(y), _ptr(post), _ptr(gate), kind, scale, _ptr(pre), eps,
-          shape[0], shape[1], _CODE[dtype], _ptr(r), _ptr(h))
+          _int32(shape[0], "T"), _int32(shape[1], "d"), _CODE[dtype], _ptr(r), _ptr(h))
     return (x if r is None else r), h
 
 
 def block_norm_scratch_bytes(T_max: int, d: int) -> int:
-    return int(_lib.load().fm_block_norm_scratch_bytes(T_max, d))
+    return int(_lib.load().fm_block_norm_scratch_bytes(_int32(T_max, "T_max"), _int32(d, "d")))
 
 
 class BlockNormScratch:
@@ -417,6 +418,6 @@ def block_norm_grad(dr: Optional[torch.Tensor], dh: Optional[torch.Tensor], x: t
     _need(scratch.buf, "scratch", torch.uint8, (scratch.nbytes,), dev)
     dx, dy, dpost, dgate, dpre = out
     _call("fm_block_norm_grad", dev, stream, _ptr(dr), _ptr(dh), x.data_ptr(), _ptr(y), _ptr(post), _ptr(gate), kind,
-          scale, _ptr(pre), eps, T, d, _CODE[dtype], 1 if accumulate else 0, dx.data_ptr(), _ptr(dy), _ptr(dpost),
-          _ptr(dgate), _ptr(dpre), scratch.buf.data_ptr(), scratch.nbytes)
+          scale, _ptr(pre), eps, _int32(T, "T"), _int32(d, "d"), _CODE[dtype], 1 if accumulate else 0, dx.data_ptr(),
+          _ptr(dy), _ptr(dpost), _ptr(dgate), _ptr(dpre), scratch.buf.data_ptr(), scratch.nbytes)
     return out
