@@ -141,6 +141,14 @@ def attn_workspace_bytes(cache: KvCache, q_heads: int) -> int:
     return int(_lib.load().fm_attn_workspace_bytes(cache.desc, _int32(q_heads, "q_heads")))
 
 
+def _capturing(device: torch.device) -> bool:
+    """Whether the current stream of the device, which need not be the current one, records a graph."""
+    if device.type != "cuda":
+        return False
+    with torch.cuda.device(device):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class AttnWorkspace:
     """Device scratch for attn_decode calls of q_heads query heads on a cache.  Calls sharing one must be ordered; all
     layers may share one.  Its first bytes count parts of split sequences: zeros between calls.  The zeros of one that is
@@ -151,7 +159,7 @@ class AttnWorkspace:
         if self.nbytes == 0:
             raise ValueError(f"invalid workspace request q_heads={q_heads} for {cache.heads} heads")
         self.buf = _aligned_bytes(self.nbytes, cache.device)
-        self.in_capture = cache.device.type == "cuda" and torch.cuda.is_current_stream_capturing()
+        self.in_capture = _capturing(cache.device)
         self.clear()
 
     def clear(self) -> None:
