@@ -15,9 +15,9 @@
 // Memory bounds long batches: with bf16, 16 queries per key head cost the matrix units
 // 7% of the time that the keys and values take to arrive (float32, whose instructions
 // are a tenth as fast, a third).  One request of 131,072 tokens, 32 query heads on 8 of
-// 128: 537 MB stream in 77 us (7.0 TB/s) of 90-98 for the call; 64 requests of 1 to
+// 128: 537 MB stream in 77 us (7.0 TB/s) of 88 for the call; 64 requests of 1 to
 // 8,192 tokens: 1.02 GB in 160 us.  Short batches are bound by a chain of waits:
-// lengths, table, keys, joins; three requests of 37 tokens take 7.7 us, one of 4,096
+// lengths, table, keys, joins; three requests of 37 tokens take 7.9 us, one of 4,096
 // tokens 14.
 #include "fm_device.h"
 #include "fm_kv.h"
@@ -83,8 +83,8 @@ struct Wave {
   static constexpr int OT = NP * (kBf ? 2 : 1);   // tiles of 16 dimensions
   static constexpr bool kTwo = NP <= (kBf ? 5 : 9);   // registers for two workgroups per CU
   // Rows so short that weighing a step takes longer than loading it: a second workgroup
-  // fills the time (64 slots of 2,048 tokens, 8 heads of 32 bf16: 47 us and 37; of 64
-  // float32: 101 and 91; heads of 64 bf16, 4,096 tokens: 96 and 93).
+  // fills the time (64 slots of 2,048 tokens, 8 heads of 32 bf16: 47 us and 36; of 64
+  // float32: 106 and 95; heads of 64 bf16, 4,096 tokens: 96 and 93).
   static constexpr bool kNarrow = NP <= (kBf ? 2 : 4);
   uint32x4 q[NP];
   uint32x4 k[SB][NP], v[SB][NP];
@@ -98,8 +98,8 @@ struct Wave {
     for (int t = 0; t < OT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
   // What no other workgroup reads passes the caches by: with 32 query heads on 8, 64
-  // requests of 1 to 8,192 tokens 160 us, 181 through them; with 24 on each of 4, 133
-  // past them and 127 through them.
+  // requests of 1 to 8,192 tokens 160 us, 181 through them; with 24 on each of 4, 127
+  // past them and 120 through them.
   static __device__ __forceinline__ void load(const char* at, uint32x4 (&r)[NP]) {
     const uint32x4* p = reinterpret_cast<const uint32x4*>(at) + threadIdx.x % kWave;
 #pragma unroll
@@ -395,8 +395,8 @@ __device__ __forceinline__ void store_part(const Joined<DIMS>& sh, int queries, 
 // sums decide how much each counts.
 constexpr int kTurn = 32;   // parts at most
 // Parts up to which more of each are on their way instead: 291 tokens, 16 queries on 2
-// heads of 256 bf16 18.1 us in turns of 32 parts, 14.8 in turns of 8; 7 slots of 177, 48
-// on 2, 25.1 and 19.2.  (A third form for 16 parts: 28.5 us -> 25.0 at 2,000 tokens on
+// heads of 256 bf16 19.0 us in turns of 32 parts, 16.4 in turns of 8; 7 slots of 177, 48
+// on 2, 24.4 and 19.1.  (A third form for 16 parts: 28.5 us -> 25.0 at 2,000 tokens on
 // one head of 256 float32, but its code costs every call of 128 bf16 0.1-4 us.)
 constexpr int kFewParts = 8;
 struct Weights {
@@ -500,34 +500,38 @@ __device__ __forceinline__ int ratio(int n, int d) {
 // More than 16 queries of a key head are tiles side by side: a piece of the line is
 // taken by a workgroup for each, on one XCD, so that the keys that the first brings are
 // in its L2 for the others: 64 requests of 1 to 8,192 tokens, 24 queries on each of 4
-// bf16 heads of 128 or 256, 127 or 242 us.  One tile behind the other, which reads the
-// keys from memory again, 173 or 345; both in one wavefront's registers 115 or 268, but
-// float32 heads of 256 spill to twice the time, and 8 requests of 1,000 tokens take 25
-// us for 19.  More than kSide tiles take turns.
+// bf16 heads of 128 or 256, 120 or 216 us.  One tile behind the other, which reads the
+// keys from memory again, 169 or 321.  (A dropped form with both tiles in one
+// wavefront's registers took 0.9 or 1.1 of the time side by side, but float32 heads of
+// 256 spilled to twice it, and 8 requests of 1,000 tokens took 25 us for 19.)  More
+// than kSide tiles take turns: 128 queries on one head of 128 79 us, 300 155.
 //
 // One workgroup per CU does for long tiles, whose parts it has few of to join: 64
-// requests of 1 to 8,192 tokens 160 us, with two 170; one of 131,072 95 and 100.
+// requests of 1 to 8,192 tokens 160 us, with two 167; one of 131,072 88 and 93.
 // Where there are more tiles than CUs and they are short, each is a wait for its data
 // and two per CU pay: 64 slots of 8 heads of 128 bf16, mean lengths of 128 / 512 /
-// 1,024 / 2,048 tokens: one 18.9 / 37.0 / 55.0 / 87.9 us, two 15.3 / 33.7 / 52.7 / 90.3
+// 1,024 / 2,048 tokens: one 19.1 / 38.4 / 53.5 / 91.6 us, two 15.6 / 34.8 / 52.0 / 93.6
 // (kShort lies between the last two).  Workgroups side by side are two per CU where
 // registers allow it, so that as many bytes are on their way: 64 requests of 1 to 8,192
-// tokens, 24 queries on each of 4 heads of 128 bf16: one 158 us, two 133.
+// tokens, 24 queries on each of 4 heads of 128 bf16: one 152 us, two 120.
 constexpr int kCus = 256;
 constexpr int kWorkers = 2 * kCus;   // workgroups that the line is cut for at most
 constexpr int kShort = 64;           // units of a tile on average
-// Units of a tile besides its steps: 64 requests as above 171 us with 4, 160 with 8,
-// 161 with 12.
+// Units of a tile besides its steps: three requests of 37 tokens 10.7 us with 4, 7.9
+// with 8 and 12; 64 requests as above 160 with 4 and 8, 162 with 12; with a window of
+// 1,000 (kPart) 22.6, 24.0 and 24.1.
 constexpr int kOverhead = 8;
 // Units of a workgroup at least, so that few tiles have a workgroup each and long ones
-// are cut fine: one request of 2,160 tokens on one key head 14.4 us with 8, 17.7 with
-// 16, 22.8 with 24.
+// are cut fine: one request of 2,160 tokens on one key head 13.4 us with 8, 15.6 with
+// 16, 19.1 with 24.
 constexpr int kLeast = 8;
 constexpr int kSide = 8;             // tiles side by side
 constexpr int kXcds = 8;             // that take workgroups in turn
-constexpr int kPart = 4;             // (8: 26.1 us for 24.4, 23 requests with a window of 1,000)
+// Steps of a part at least: 23 requests of 3,000 tokens with a window of 1,000, heads of
+// 80 float32, 26.8 us with 8 and 24.0 with 4, but 7 slots of 177 as above 15.0 and 19.1.
+constexpr int kPart = 4;
 // Steps up to which a tile that shares a piece is a wavefront's alone: 103 slots of 4
-// tokens, 32 heads of 128 bf16: 17 us, 35 without; 225 of 2, 3 heads of 256: 12 and 24.
+// tokens, 32 heads of 128 bf16: 16 us, 34 without; 225 of 2, 3 heads of 256: 12 and 22.
 constexpr int kFew = 4;
 __device__ __forceinline__ int cut(int x, int steps) {   // x: from the tile's first step on
   if (x <= 0) return 0;
@@ -678,7 +682,8 @@ __global__ void __launch_bounds__(kAttnWaves * kWave, (Wave<T, NP, ALONE>::kTwo 
     }
     // Short tiles cost little but the wait for their data: each wavefront takes tiles
     // of its own, without barriers and LDS; longer ones only where the piece holds one
-    // for every wavefront, of one length.
+    // for every wavefront, of one length (200 slots of 350 tokens, 16 heads of 16 bf16:
+    // 55 us, 63 without; 128 of 400, 32 heads of 72: 122 and 120).
     bool alone = lo == 0 && hi == steps;
     if (steps <= kFew) alone = alone && (steps == 1 || 2 * (kOverhead + steps) <= each);
     else alone = alone && k >= 0 && k < groups;

@@ -10,7 +10,13 @@
 // TB/s; a copy reaches 5.1).  Eight slots forked in four, each grown past a shared page:
 // 2.3 us of new tables, 1.7 to put them in place, 7.0 to decide, 15 to copy 32 pages (100
 // MB, 6.6 TB/s: the memory-side cache holds some).  Rows of 8,192 tokens on 8 heads of 128
-// bf16: 67 MB in 18 us (3.7 TB/s); of 8 tokens 3.4 us.
+// bf16, which the caches hold since they were made: 67 MB in 18 us (3.7 TB/s), from
+// memory 26; of 8 tokens 3.3 us.
+//
+// One workgroup decides for a pool of any size, reading its counts: growth takes 9 us
+// up to a thousand pages, 41 in one of 131,072 whose free pages are the last, 267 and
+// 4,300 of 2^20 and 2^24; a compaction that moves nothing 11, 102, 974 and 15,700.
+// (131,072 pages of 2.2 MB are 288 GB.)
 #include "fm_device.h"
 #include "fm_kv.h"
 
@@ -515,9 +521,11 @@ struct Piece {
         if (quad[j] && column(a, piece, i)) v[4 * i + j] = vrow[j * r.v_stride + 16 * i];
       }
   }
-  // MANY: past the caches, which many rows would turn over: pages of 8,192 tokens that no
-  // cache holds 18.1 us, 29.5 through them; one token of each of 256 slots, 32 heads of
-  // 128 bf16, 14.7 and 16.4.  A few tokens stay there for the attention that follows.
+  // MANY: past the caches, which many rows would turn over: 8,192 tokens of 8 heads of 128
+  // bf16 to pages that no cache holds 17.6 us, 19.2 through them (26 and 29 where the
+  // rows come from memory too); one token of each of 256 slots, 32 heads of 128, 15.8
+  // and 16.2, float32 20.7 and 25.0.  A few tokens stay there for the attention that
+  // follows.
   template <bool MANY>
   __device__ __forceinline__ void to_page(char* kp, char* vp) const {
     auto store = [](uint32x4 x, uint32x4* p) __attribute__((always_inline)) {
@@ -691,8 +699,9 @@ hipError_t launch_kv_rows(const fm_kv_cache& c, const KvRows& r, bool read, hipS
                            ? c.n_slots
                            : r.T / kBlockTokens + 2 * static_cast<int64_t>(c.n_slots < r.T ? c.n_slots : r.T);
   // Pieces of a wavefront: one where the batch is small, or four, so that fewer
-  // workgroups look for their block (us of 1 and 4: 8 tokens of 8 heads of 128 4.1 and
-  // 5.8, 8,192 tokens 22.6 and 19.4).
+  // workgroups look for their block (us of 1 and 4, 8 heads of 128 bf16: 8 tokens 3.3
+  // and 5.1, 4,096, which are 9,216 pieces, 14.5 and 15.5, 8,192, 17,408 pieces, 21.1 and
+  // 17.6; reading those 21.3 and 18.5).
   const int64_t pieces = static_cast<int64_t>(c.heads) * a.pieces;
   const bool many = most * pieces >= 16384;
   const int64_t per_group = kRowWaves * (many ? 4 : 1);

@@ -12,7 +12,7 @@
 // reads no more than the stored r would.  Memory bounds both: with a gate and
 // both norms, 8,192 rows of 4,096 in bf16 take 51 us forward (268 MB, 5.2 TB/s; a copy
 // reaches 5.1) and 79 us backward (403 MB, 5.1 TB/s, the sums over the rows 4 of them).
-// Few rows cost their chain of launch, loads, sums and barriers: one row of 2,048 4.5 us,
+// Few rows cost their chain of launch, loads, sums and barriers: one row of 2,048 3.4 us,
 // 64 rows of 4,096 backward 8.6.
 #include "fm_device.h"
 #include "fm_norm.h"
@@ -515,8 +515,17 @@ __global__ void __launch_bounds__(kSumWaves* kWave) k_norm_sum(NormGradArgs a, i
   }
 }
 
-// Wavefronts per row and vectors per thread for rows of `vecs` vectors: the fewest
-// wavefronts that hold the row with at most four vectors each.
+// Wavefronts per row and vectors per thread for rows of `vecs` vectors: one wavefront, four
+// or sixteen, the fewest that hold the row with at most four vectors per thread (bf16
+// with two on sixteen; two wavefronts would share a barrier with another row, which may
+// not be there).  67 MB of bf16, us, wavefronts x vectors: rows of 512 1x1 46.5, 1x2 46.7;
+// 1,024 1x2 47.6, 4x1 53.6; 2,048 1x4 49.0, 4x1 47.1; 2,304 4x2 51.2, 8x1 51.9; 4,096 4x2
+// 52.5, 8x1 48.2; 8,192 4x4 55.5, 8x2 52.7, 16x1 49.7; 12,288 16x2 54.5, 12x2 52.4, 16x4
+// 74.2; 16,384 16x2 54.7, 8x4 57.1.  float32: 512 1x2 47.4, 4x1 52.9; 1,024 1x4 49.0, 4x1
+// 48.0; 2,048 4x2 51.9, 8x1 48.8; 4,096 4x4 53.6, 16x1 50.5; 8,192 16x2 55.0, 8x4 53.9.
+// 64 rows of 2,048 bf16: 1x4 3.8, 4x1 2.8; of 8,192: 4x4 4.7, 16x1 3.8.  So the rule is up
+// to 12%, and 1 us of a small call, behind the best.  Rows below 512 leave lanes idle:
+// of 128 values 91 us, of 64 162.
 constexpr int64_t kGridRow = 1 << 16;
 
 template <typename T>

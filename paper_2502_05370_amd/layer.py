@@ -275,9 +275,9 @@ def attn_decode(cache: KvCache, layer: int, q: torch.Tensor, scale: Optional[flo
     parts of longer ones) -> [slots][q_heads][head_dim].  scale defaults to head_dim ** -0.5; the last ``window`` tokens
     are seen (0: all), from place first[s] on (int32 [slots]); slots where active [slots] uint8 is 0, and queries that
     see no token, give zeros.  ``lse`` [slots][q_heads] float32 takes the log of each query's sum of weights.  Without
-    ``workspace`` the cache's own of the stream serves the call (cache.ensure_workspace before a capture saves it a fill per
-    call); replays of a graph that captured such a call must be ordered with each other and with the later calls on the
-    stream of the capture."""
+    ``workspace`` the cache's own of the stream serves the call (cache.ensure_workspace before a capture saves it a fill
+    per call); replays of all graphs that captured such calls on one stream must be ordered with each other and with the
+    later calls on that stream."""
     dev = cache.device
     q_ptr, q_stride, _, q_heads = _rows(q, "q", cache.dtype, cache.slots, None, cache.head_dim, dev)
     if out is None:
